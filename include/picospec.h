@@ -16,6 +16,11 @@
  *   picospec_pack_uplink / picospec_unpack_uplink / picospec_pack_downlink / picospec_unpack_downlink
  *                            the two messages of a round as contiguous, in-place addressable buffers
  *
+ * and beside the round, for the drafter:
+ *
+ *   picospec_distill / picospec_distill_grad
+ *                            its divergence from the target's Top-K records and the gradient
+ *
  * Conventions shared by all calls
  *   - Every data pointer is a DEVICE pointer (HBM) unless marked "host".  The caller owns all
  *     buffers; the library neither allocates nor frees nor synchronises.  Work is enqueued on
@@ -414,6 +419,34 @@ int picospec_pack_uplink(int32_t B, int32_t n_draft, const int32_t* seq_off, con
  */
 int picospec_unpack_uplink(const void* wire, int64_t wire_bytes, int32_t B, int32_t n_max,
                            int32_t* seq_off, int32_t* draft_tok, float* q_scalar, uint32_t* status, void* stream);
+
+/*
+ * ---- Beside the round: the drafter ---------------------------------------------------------------
+ *
+ * Distillation on the target's Top-K records (what picospec_compress makes of the target's rows): for each of n_rows rows of
+ * the drafter's logits, q = softmax(z / T), the Kullback-Leibler divergence of q from the record (id_j, p_j), j < count:
+ *   tail 0   loss = sum_j ph_j (ln ph_j - ln q_j),  ph_j = p_j / sum p
+ *   tail 1   loss = sum_j p_j (ln p_j - ln q_j) + pt (ln pt - ln qt),  pt = max(0, 1 - sum p) and qt = the mass of q off the record
+ * and accept = sum_j min(p_j, q_j), the probability with which a token drawn from q is accepted against the record's p.
+ *   logits [n_rows, ld]; idx, prob [n_rows, k], count [n_rows]: k in 1..min(V, picospec_limit(MAX_K)), count clamped to
+ *            0..k, p_j >= 0; the ids of a record differ; entries whose id lies outside [0, V) are passed over        in
+ *   weight [n_rows], nullable (1): the factor of each row's gradient                                                 in
+ *   loss, accept [n_rows] fp32, accept nullable                                                                      out
+ *   stats [n_rows, 4] fp64, nullable, on a 16-byte boundary: what picospec_distill_grad takes                        out
+ *   grad [n_rows, ld_grad] in the logits' dtype, ld_grad >= V, nullable: weight * d loss / d logits, rounded once; may not overlap
+ *            the logits                                                                                              out
+ * Rows with count 0 (positions that are not trained on) and rows without a logit above -inf have loss, accept and gradient 0.
+ * A record id whose logit is -inf has loss +inf (its gradient is finite); NaN and +inf logits make a row's results NaN.
+ * picospec_distill_grad forms the gradient alone, from the stats of an earlier picospec_distill of the same logits and
+ * records: what a framework with a tape calls backwards.
+ */
+int picospec_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
+                     const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,
+                     float* loss, float* accept, double* stats, void* grad, int64_t ld_grad, void* stream);
+
+int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
+                          const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,
+                          const double* stats, void* grad, int64_t ld_grad, void* stream);
 
 /*
  * host: memory-safety check of the streaming row loads.  For a row of V elements whose first byte lies

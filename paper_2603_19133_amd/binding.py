@@ -35,6 +35,7 @@ WIRE_BAD_HEADER, WIRE_BAD_BATCH, WIRE_CLAMPED, WIRE_TRUNCATED = 1, 2, 4, 8
 EXPORTS = ("picospec_round", "picospec_verify_sample", "picospec_verify_sample_static", "picospec_static_scratch_bytes", "picospec_compress", "picospec_sample_draft", "picospec_verify", "picospec_verify_range", "picospec_sample_residual", "picospec_sample_residual_ws",
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
+           "picospec_distill", "picospec_distill_grad",
            "picospec_downlink_bytes_max", "picospec_uplink_bytes", "picospec_max_load_byte", "picospec_check_device", "picospec_probe_clock",
            "picospec_workspace_bytes", "picospec_scratch_bytes", "picospec_one_launch_bytes", "picospec_limit", "picospec_strerror", "picospec_version")
 
@@ -79,6 +80,8 @@ lib.picospec_pack_downlink.argtypes = [_i32, _p, _p, _p, _p, _p, _p, _i32, C.c_i
 lib.picospec_unpack_downlink.argtypes = [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p]
 lib.picospec_pack_uplink.argtypes = [_i32, _i32, _p, _p, _p, C.c_int, _p, _i64, _p, _p]
 lib.picospec_unpack_uplink.argtypes = [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p]
+lib.picospec_distill.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _p, _p, _i64, _p]
+lib.picospec_distill_grad.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _i64, _p]
 lib.picospec_downlink_bytes_max.argtypes = [_i32, _i32, C.c_int]
 lib.picospec_downlink_bytes_max.restype = _i64
 lib.picospec_uplink_bytes.argtypes = [_i32, _i32, C.c_int]
@@ -102,7 +105,7 @@ lib.picospec_strerror.restype = C.c_char_p
 for _n in ("picospec_compress", "picospec_sample_draft", "picospec_verify", "picospec_sample_residual", "picospec_sample_residual_ws",
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse", "picospec_version",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
-           "picospec_verify_range", "picospec_round"):
+           "picospec_verify_range", "picospec_round", "picospec_distill", "picospec_distill_grad"):
     getattr(lib, _n).restype = C.c_int
 
 
@@ -376,6 +379,45 @@ def resample_sparse(draft_logits: torch.Tensor, V: int, temperature: float, seq_
     _check(_nat.resample_sparse(draft_logits, dt, ld, V, temperature, B, n_draft, seq_off, n_accept, draft_max, draft_sum,
                               p.idx, p.prob, p.count, p.mass, p.k, renorm, uniforms, out.out_tok, out.resid_mass, out.flags,
                               _stream()))
+    return out
+
+
+@dataclass
+class Distilled:
+    loss: torch.Tensor            # float32 [rows]
+    accept: torch.Tensor          # float32 [rows]
+    stats: torch.Tensor           # float64 [rows, 4]: what distill_grad takes
+    grad: torch.Tensor | None     # [rows, V] in the logits' dtype
+
+
+def _distill_inputs(logits: torch.Tensor, rec: Compressed, weight: torch.Tensor | None):
+    """(dtype code, stride of a row, rows) of the logits; the record and the weights have to be theirs."""
+    dt, ld, rows = r = _logits_2d(logits)
+    if rec.idx.shape[0] != rows or (weight is not None and (weight.numel() != rows or weight.dtype != torch.float32 or not weight.is_contiguous())):
+        raise PicoSpecError(EINVAL)
+    return r
+
+
+def distill(logits: torch.Tensor, V: int, temperature: float, rec: Compressed, tail: int = 0, weight: torch.Tensor | None = None,
+            grad: bool = False) -> Distilled:
+    """picospec_distill of [rows, >=V] drafter logits on the target's records: loss and expected acceptance per row and, with `grad`,
+    weight * d loss / d logits in the same call.  training.distill_loss is the same for torch's autograd."""
+    dt, ld, rows = _distill_inputs(logits, rec, weight)
+    loss, accept, stats = _nat.empty(logits, "ffd", rows, rows, (rows, 4))
+    g = torch.empty((rows, V), dtype=logits.dtype, device=logits.device) if grad else None
+    _check(_nat.distill(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, loss, accept, stats, g, V, _stream()))
+    return Distilled(loss, accept, stats, g)
+
+
+def distill_grad(logits: torch.Tensor, V: int, temperature: float, rec: Compressed, stats: torch.Tensor, tail: int = 0,
+                 weight: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """picospec_distill_grad: weight * d loss / d logits [rows, V] from the stats of an earlier distill of the same logits and records."""
+    dt, ld, rows = _distill_inputs(logits, rec, weight)
+    out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device) if out is None else out
+    dt_g, ld_g, rows_g = _logits_2d(out)
+    if dt_g != dt or rows_g != rows or out.shape[1] < V or stats.numel() != 4 * rows or stats.dtype != torch.float64:
+        raise PicoSpecError(EINVAL)
+    _check(_nat.distill_grad(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, stats, out, ld_g, _stream()))
     return out
 
 

@@ -505,6 +505,44 @@ int picospec_sample_residual_ws(const void* tgt_logits, int dtype, int64_t ld, i
                                 q_mass, k, renorm, uniforms, out_tok, resid_mass, flags, workspace, workspace_bytes, true, stream);
 }
 
+// ---- the drafter's side
+
+namespace {
+
+int check_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
+                  const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const double* stats, const void* grad, int64_t ld_grad)
+{
+    if (int rc = check_logits(logits, dtype, ld, n_rows, V, temperature)) return rc;
+    if (k < 1 || k > V || (tail != 0 && tail != 1)) return PICOSPEC_EINVAL;
+    if (k > kMaxK) return PICOSPEC_EUNSUPPORTED;
+    if (n_rows > 0 && (!idx || !prob || !count)) return PICOSPEC_EINVAL;
+    if ((uintptr_t)stats & 15u) return PICOSPEC_EINVAL;
+    if (grad && (ld_grad < V || (uintptr_t)grad % (dtype == PICOSPEC_F32 ? 4 : 2))) return PICOSPEC_EINVAL;
+    return PICOSPEC_OK;
+}
+
+}  // namespace
+
+int picospec_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
+                     const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,
+                     float* loss, float* accept, double* stats, void* grad, int64_t ld_grad, void* stream)
+{
+    if (int rc = check_distill(logits, dtype, ld, n_rows, V, temperature, idx, prob, count, k, tail, stats, grad, ld_grad)) return rc;
+    if (n_rows > 0 && !loss) return PICOSPEC_EINVAL;
+    return hip_status(launch_distill(logits, dtype, ld, n_rows, V, temperature, idx, prob, count, k, tail, loss, accept, stats, weight,
+                                     grad, ld_grad, (hipStream_t)stream));
+}
+
+int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
+                          const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,
+                          const double* stats, void* grad, int64_t ld_grad, void* stream)
+{
+    if (int rc = check_distill(logits, dtype, ld, n_rows, V, temperature, idx, prob, count, k, tail, stats, grad, ld_grad)) return rc;
+    if (n_rows > 0 && (!stats || !grad)) return PICOSPEC_EINVAL;
+    return hip_status(launch_distill_grad(logits, dtype, ld, n_rows, V, temperature, idx, prob, count, k, tail, stats, weight,
+                                          grad, ld_grad, (hipStream_t)stream));
+}
+
 size_t picospec_workspace_bytes(int which_call, int dtype, int32_t rows, int32_t V, int32_t k)
 {
     if (rows < 0 || V < 1 || V > kMaxV) return 0;

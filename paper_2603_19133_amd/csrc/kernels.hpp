@@ -411,4 +411,14 @@ hipError_t launch_pack_uplink(int B, int n_draft, const int32_t* seq_off, const 
 hipError_t launch_unpack_uplink(const void* wire, int64_t wire_bytes, int B, int n_max, int32_t* seq_off,
                                 int32_t* draft_tok, float* q_scalar, uint32_t* status, hipStream_t stream);
 
+// ---- distillation on records (csrc/distill.hip): one workgroup of kDistillThreads per row; with the gradient in the same call a thread keeps
+// kDistillHeld vectors of its row in registers from the sum to the gradient
+constexpr int kDistillThreads = 1024, kDistillHeld = 0;
+hipError_t launch_distill(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature,
+                          const int32_t* idx, const float* prob, const int32_t* count, int k, int tail,
+                          float* loss, float* accept, double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream);
+hipError_t launch_distill_grad(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature,
+                               const int32_t* idx, const float* prob, const int32_t* count, int k, int tail,
+                               const double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream);
+
 }  // namespace picospec

@@ -224,6 +224,25 @@ PyObject* n_unpack_uplink(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
+PyObject* n_distill(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return enter(v, n, [](Args& a) {
+        auto z = a.ptr(); auto dt = a.i32(); auto ld = a.i64(); auto rows = a.i32(), V = a.i32(); auto T = a.f32();
+        auto idx = a.ptr<int32_t>(); auto prob = a.ptr<float>(); auto count = a.ptr<int32_t>(); auto k = a.i32(), tail = a.i32();
+        auto weight = a.ptr<float>(); auto loss = a.ptr<float>(); auto accept = a.ptr<float>(); auto stats = a.ptr<double>();
+        auto grad = a.ptr(); auto ldg = a.i64(); auto s = a.stream();
+        return [=] { return picospec_distill(z, dt, ld, rows, V, T, idx, prob, count, k, tail, weight, loss, accept, stats, grad, ldg, s); };
+    });
+}
+
+PyObject* n_distill_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return enter(v, n, [](Args& a) {
+        auto z = a.ptr(); auto dt = a.i32(); auto ld = a.i64(); auto rows = a.i32(), V = a.i32(); auto T = a.f32();
+        auto idx = a.ptr<int32_t>(); auto prob = a.ptr<float>(); auto count = a.ptr<int32_t>(); auto k = a.i32(), tail = a.i32();
+        auto weight = a.ptr<float>(); auto stats = a.ptr<double>(); auto grad = a.ptr(); auto ldg = a.i64(); auto s = a.stream();
+        return [=] { return picospec_distill_grad(z, dt, ld, rows, V, T, idx, prob, count, k, tail, weight, stats, grad, ldg, s); };
+    });
+}
+
 // rows2d(tensor) -> (dtype code, stride of a row, rows), or an error code of the library: a 2-d device tensor whose rows are
 // contiguous (the strides of a tensor without rows mean nothing)
 PyObject* n_rows2d(PyObject*, PyObject* o) {
@@ -280,7 +299,7 @@ PyObject* n_scratch(PyObject*, PyObject* const* v, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// empty(like, codes, size, ...) -> one tensor per letter of `codes` (i int32, l int64, f float32, b uint8) on the device of
+// empty(like, codes, size, ...) -> one tensor per letter of `codes` (i int32, l int64, f float32, d float64, b uint8) on the device of
 // `like`; a size is an int (1-d) or a tuple of two.  Outputs of up to kShared bytes share one allocation, each from a 512-byte boundary of it
 // on, as slices of a tensor do: an allocation costs 0.45 to 0.85 us, a slice 0.15 (the eight outputs of an unpacked downlink message of 32
 // records of 256: 2.1 us, each from torch.empty 6.8).  All of it lives as long as any of them, so larger ones, next to which an allocation is cheap to make and
@@ -301,7 +320,7 @@ PyObject* n_empty(PyObject*, PyObject* const* v, Py_ssize_t n) {
         dims[i][1] = nd[i] == 2 ? PyLong_AsLongLong(PyTuple_GET_ITEM(s, 1)) : 1;
         if (PyErr_Occurred()) return nullptr;
         if (dims[i][0] < 0 || dims[i][1] < 0 || __builtin_mul_overflow(dims[i][0], dims[i][1], &bytes[i]) || bytes[i] > (int64_t(1) << 56)) { PyErr_SetString(PyExc_RuntimeError, "empty: a size is out of range"); return nullptr; }
-        bytes[i] *= codes[i] == 'l' ? 8 : codes[i] == 'b' ? 1 : 4;
+        bytes[i] *= codes[i] == 'l' || codes[i] == 'd' ? 8 : codes[i] == 'b' ? 1 : 4;
         if (bytes[i] <= kShared) shared += (bytes[i] + 511) / 512 * 512;
     }
     THPObjectPtr out(PyTuple_New(len));
@@ -309,7 +328,7 @@ PyObject* n_empty(PyObject*, PyObject* const* v, Py_ssize_t n) {
     at::Tensor block;
     int64_t at_byte = 0;
     for (Py_ssize_t i = 0; i < len; ++i) {
-        const at::ScalarType type = codes[i] == 'i' ? at::kInt : codes[i] == 'l' ? at::kLong : codes[i] == 'b' ? at::kByte : at::kFloat;
+        const at::ScalarType type = codes[i] == 'i' ? at::kInt : codes[i] == 'l' ? at::kLong : codes[i] == 'b' ? at::kByte : codes[i] == 'd' ? at::kDouble : at::kFloat;
         at::Tensor piece;
         if (bytes[i] > kShared) {
             piece = at::empty(at::IntArrayRef(dims[i], nd[i]), like(v[0], type));
@@ -334,7 +353,7 @@ PyMethodDef methods[] = {
     FAST("round", n_round), FAST("verify_sample", n_verify_sample), FAST("verify_sample_static", n_verify_sample_static),
     FAST("sample_residual", n_sample_residual<picospec_sample_residual>), FAST("sample_residual_ws", n_sample_residual<picospec_sample_residual_ws>), FAST("row_stats", n_row_stats), FAST("compress_rejected", n_compress_rejected),
     FAST("resample_sparse", n_resample_sparse), FAST("pack_downlink", n_pack_downlink), FAST("unpack_downlink", n_unpack_downlink),
-    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
+    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
     {"rows2d", (PyCFunction)n_rows2d, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
