@@ -18,6 +18,7 @@
  *
  * and beside the round, for the drafter:
  *
+ *   picospec_sample          one token per row of logits with temperature, top-k, top-p and min-p
  *   picospec_distill / picospec_distill_grad
  *                            its divergence from the target's Top-K records and the gradient
  *
@@ -423,6 +424,28 @@ int picospec_unpack_uplink(const void* wire, int64_t wire_bytes, int32_t B, int3
 /*
  * ---- Beside the round: the drafter ---------------------------------------------------------------
  *
+ * One token per row of logits with the usual filters, from given uniform numbers: the first token of a request, decoding without a
+ * draft, roll-outs, a drafter that keeps no record.  For a row z (NaN counts as -inf, +inf as the largest finite number):
+ * w = exp((z - max z) / T); the row is ordered by (logit descending, id ascending); the first top_k of it are kept; of these the shortest
+ * prefix whose mass reaches top_p of theirs; of these the ones with w >= min_p; the token is the first id, ascending, at which the kept
+ * mass up to and with it exceeds u times all of it.
+ *   temperature  >= 0; 0: the largest logit, of equal ones the lowest id (T and top_k count as 1)
+ *   top_k        <= 0: no limit      top_p  <= 0 or >= 1: all      min_p  <= 0: all; at most 1
+ *   temperature_rows, top_k_rows, top_p_rows, min_p_rows [n_rows], each nullable: a setting per row instead.  What the host would refuse counts
+ *                as greedy (temperature), 1 (min_p above it) or none (NaN)
+ *   uniforms     [n_rows] in [0,1)                                                                            in
+ *   tok [n_rows] int32, prob [n_rows] fp32 = the token's share of the kept mass, count [n_rows] int32 = how many ids are kept,
+ *   lse [n_rows] fp32 = max z / T + ln(kept mass)                                                             out
+ * A row without a logit above -inf: tok -1, prob 0, count 0, lse -inf.  Masses are summed in 64 bits, in the order of a fixed rule: a call
+ * gives the same bits every time.
+ */
+int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                    float temperature, int32_t top_k, float top_p, float min_p,
+                    const float* temperature_rows, const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows,
+                    const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Distillation on the target's Top-K records (what picospec_compress makes of the target's rows): for each of n_rows rows of
  * the drafter's logits, q = softmax(z / T), the Kullback-Leibler divergence of q from the record (id_j, p_j), j < count:
  *   tail 0   loss = sum_j ph_j (ln ph_j - ln q_j),  ph_j = p_j / sum p

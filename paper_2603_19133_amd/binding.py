@@ -35,7 +35,7 @@ WIRE_BAD_HEADER, WIRE_BAD_BATCH, WIRE_CLAMPED, WIRE_TRUNCATED = 1, 2, 4, 8
 EXPORTS = ("picospec_round", "picospec_verify_sample", "picospec_verify_sample_static", "picospec_static_scratch_bytes", "picospec_compress", "picospec_sample_draft", "picospec_verify", "picospec_verify_range", "picospec_sample_residual", "picospec_sample_residual_ws",
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
-           "picospec_distill", "picospec_distill_grad",
+           "picospec_sample", "picospec_distill", "picospec_distill_grad",
            "picospec_downlink_bytes_max", "picospec_uplink_bytes", "picospec_max_load_byte", "picospec_check_device", "picospec_probe_clock",
            "picospec_workspace_bytes", "picospec_scratch_bytes", "picospec_one_launch_bytes", "picospec_limit", "picospec_strerror", "picospec_version")
 
@@ -80,6 +80,7 @@ lib.picospec_pack_downlink.argtypes = [_i32, _p, _p, _p, _p, _p, _p, _i32, C.c_i
 lib.picospec_unpack_downlink.argtypes = [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p]
 lib.picospec_pack_uplink.argtypes = [_i32, _i32, _p, _p, _p, C.c_int, _p, _i64, _p, _p]
 lib.picospec_unpack_uplink.argtypes = [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p]
+lib.picospec_sample.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _i32, _f, _f, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p]
 lib.picospec_distill.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _p, _p, _i64, _p]
 lib.picospec_distill_grad.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _i64, _p]
 lib.picospec_downlink_bytes_max.argtypes = [_i32, _i32, C.c_int]
@@ -105,7 +106,7 @@ lib.picospec_strerror.restype = C.c_char_p
 for _n in ("picospec_compress", "picospec_sample_draft", "picospec_verify", "picospec_sample_residual", "picospec_sample_residual_ws",
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse", "picospec_version",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
-           "picospec_verify_range", "picospec_round", "picospec_distill", "picospec_distill_grad"):
+           "picospec_verify_range", "picospec_round", "picospec_sample", "picospec_distill", "picospec_distill_grad"):
     getattr(lib, _n).restype = C.c_int
 
 
@@ -379,6 +380,39 @@ def resample_sparse(draft_logits: torch.Tensor, V: int, temperature: float, seq_
     _check(_nat.resample_sparse(draft_logits, dt, ld, V, temperature, B, n_draft, seq_off, n_accept, draft_max, draft_sum,
                               p.idx, p.prob, p.count, p.mass, p.k, renorm, uniforms, out.out_tok, out.resid_mass, out.flags,
                               _stream()))
+    return out
+
+
+@dataclass
+class Sampled:
+    tok: torch.Tensor     # int32 [rows]
+    prob: torch.Tensor    # float32 [rows]: the token's share of the kept mass
+    count: torch.Tensor   # int32 [rows]: ids kept
+    lse: torch.Tensor     # float32 [rows]: log of the kept mass
+
+
+def _setting(v, rows: int, dtype: torch.dtype):
+    """(value, tensor): a number for all rows, or a tensor with one for each."""
+    if not isinstance(v, torch.Tensor):
+        return v, None
+    if v.dtype != dtype or v.dim() != 1 or v.numel() != rows or not v.is_contiguous() or not v.is_cuda:
+        raise PicoSpecError(EINVAL)
+    return 0, v
+
+
+def sample(logits: torch.Tensor, V: int, uniforms: torch.Tensor, temperature=1.0, top_k=0, top_p=0.0, min_p=0.0,
+           out: Sampled | None = None) -> Sampled:
+    """picospec_sample: one token per row of [rows, >=V] device logits.  Every setting is a number for all rows or a device tensor with one per
+    row (float32, top_k int32)."""
+    dt, ld, rows = _logits_2d(logits)
+    if uniforms.numel() != rows or uniforms.dtype != torch.float32 or not uniforms.is_contiguous():
+        raise PicoSpecError(EINVAL)
+    T, T_rows = _setting(temperature, rows, torch.float32)
+    k, k_rows = _setting(top_k, rows, torch.int32)
+    p, p_rows = _setting(top_p, rows, torch.float32)
+    m, m_rows = _setting(min_p, rows, torch.float32)
+    out = out or Sampled(*_nat.empty(logits, "ifif", rows, rows, rows, rows))
+    _check(_nat.sample(logits, dt, ld, rows, V, T, k, p, m, T_rows, k_rows, p_rows, m_rows, uniforms, out.tok, out.prob, out.count, out.lse, None, _stream()))
     return out
 
 

@@ -507,6 +507,22 @@ int picospec_sample_residual_ws(const void* tgt_logits, int dtype, int64_t ld, i
 
 // ---- the drafter's side
 
+int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                    float temperature, int32_t top_k, float top_p, float min_p,
+                    const float* temperature_rows, const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows,
+                    const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse,
+                    void* workspace, size_t workspace_bytes, void* stream)
+{
+    // (0: greedy; settings that come per row are not looked at here)
+    if (int rc = check_logits(logits, dtype, ld, n_rows, V, temperature_rows || temperature == 0.f ? 1.f : temperature)) return rc;
+    if ((!top_p_rows && std::isnan(top_p)) || (!min_p_rows && !(min_p <= 1.f))) return PICOSPEC_EINVAL;
+    if (n_rows > 0 && (!uniforms || !tok || !prob || !count || !lse)) return PICOSPEC_EINVAL;
+    if ((uintptr_t)workspace & 15u) return PICOSPEC_EWORKSPACE;
+    (void)workspace_bytes;
+    return hip_status(launch_sample(logits, dtype, ld, n_rows, V, temperature, top_k, top_p, min_p, temperature_rows, top_k_rows, top_p_rows, min_p_rows,
+                                    uniforms, tok, prob, count, lse, (hipStream_t)stream));
+}
+
 namespace {
 
 int check_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,

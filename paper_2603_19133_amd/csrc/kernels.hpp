@@ -411,6 +411,11 @@ hipError_t launch_pack_uplink(int B, int n_draft, const int32_t* seq_off, const 
 hipError_t launch_unpack_uplink(const void* wire, int64_t wire_bytes, int B, int n_max, int32_t* seq_off,
                                 int32_t* draft_tok, float* q_scalar, uint32_t* status, hipStream_t stream);
 
+// ---- one token per row from the filtered distribution (csrc/sample.hip); *_rows: a setting per row, null where one serves all
+hipError_t launch_sample(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature, int top_k, float top_p, float min_p,
+                         const float* temperature_rows, const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows,
+                         const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse, hipStream_t stream);
+
 // ---- distillation on records (csrc/distill.hip): one workgroup of kDistillThreads per row; with the gradient in the same call a thread keeps
 // kDistillHeld vectors of its row in registers from the sum to the gradient
 constexpr int kDistillThreads = 1024, kDistillHeld = 0;

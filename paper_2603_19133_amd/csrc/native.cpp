@@ -224,6 +224,16 @@ PyObject* n_unpack_uplink(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
+PyObject* n_sample(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return enter(v, n, [](Args& a) {
+        auto z = a.ptr(); auto dt = a.i32(); auto ld = a.i64(); auto rows = a.i32(), V = a.i32(); auto T = a.f32(); auto k = a.i32(); auto p = a.f32(), mp = a.f32();
+        auto Tr = a.ptr<float>(); auto kr = a.ptr<int32_t>(); auto pr = a.ptr<float>(); auto mr = a.ptr<float>(); auto u = a.ptr<float>();
+        auto tok = a.ptr<int32_t>(); auto prob = a.ptr<float>(); auto count = a.ptr<int32_t>(); auto lse = a.ptr<float>();
+        auto ws = a.buffer(); auto s = a.stream();
+        return [=] { return picospec_sample(z, dt, ld, rows, V, T, k, p, mp, Tr, kr, pr, mr, u, tok, prob, count, lse, ws.p, ws.bytes, s); };
+    });
+}
+
 PyObject* n_distill(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return enter(v, n, [](Args& a) {
         auto z = a.ptr(); auto dt = a.i32(); auto ld = a.i64(); auto rows = a.i32(), V = a.i32(); auto T = a.f32();
@@ -353,7 +363,7 @@ PyMethodDef methods[] = {
     FAST("round", n_round), FAST("verify_sample", n_verify_sample), FAST("verify_sample_static", n_verify_sample_static),
     FAST("sample_residual", n_sample_residual<picospec_sample_residual>), FAST("sample_residual_ws", n_sample_residual<picospec_sample_residual_ws>), FAST("row_stats", n_row_stats), FAST("compress_rejected", n_compress_rejected),
     FAST("resample_sparse", n_resample_sparse), FAST("pack_downlink", n_pack_downlink), FAST("unpack_downlink", n_unpack_downlink),
-    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
+    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("sample", n_sample), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
     {"rows2d", (PyCFunction)n_rows2d, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

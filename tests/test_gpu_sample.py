@@ -1,0 +1,214 @@
+"""picospec_sample against the definition in 64 bits: tokens and counts equal, probabilities and log masses within their rounding.
+
+A weight is off by at most 1.1e-12 (the polynomial) + 60 * 2^-52 (the exponent's rounding), so masses, and what is compared with them, by 2e-12:
+a token or an end of a prefix differs from the definition only where a border lies within that of a step of the sum, one draw in a
+million.  prob: 4e-12 and half a step of fp32; lse: the same of its value and 4e-12."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+FAR = 4e-12
+
+
+@pytest.fixture(scope="module")
+def ps():
+    from paper_2603_19133_amd import binding
+    return binding
+
+
+def reference(z, T, top_k, top_p, min_p, u):
+    """One row: (tok, prob, count, lse)."""
+    z = z.astype(np.float64).copy()
+    z[np.isnan(z)] = -np.inf
+    z = np.minimum(z, float(np.finfo(np.float32).max))
+    if z.max() == -np.inf:
+        return -1, 0.0, 0, -np.inf
+    T, top_p, min_p = (float(np.float32(v)) for v in (T, top_p, min_p))
+    if T == 0:
+        T, top_k = 1.0, 1
+    order = np.argsort(-z, kind="stable")
+    order = order[z[order] > -np.inf]
+    if top_k > 0:
+        order = order[:top_k]
+    w = np.exp((z[order] - z.max()) / T)
+    if 0 < top_p < 1:
+        mass = np.cumsum(w)
+        n = 1 + int(np.searchsorted(mass, top_p * mass[-1], side="left"))
+        order, w = order[:n], w[:n]
+    if min_p > 0:
+        order, w = order[w >= min_p], w[w >= min_p]
+    byid = np.argsort(order)
+    mass = np.cumsum(w[byid])
+    at = min(int(np.searchsorted(mass, float(np.float32(u)) * mass[-1], side="right")), len(order) - 1)
+    return int(order[byid][at]), w[byid][at] / mass[-1], len(order), z.max() / T + math.log(mass[-1])
+
+
+def compare(got, z, T, top_k, top_p, min_p, u):
+    torch.cuda.synchronize()
+    tok, prob, count, lse = (t.cpu().numpy() for t in (got.tok, got.prob, got.count, got.lse))
+    z, u = z.float().cpu().numpy(), u.cpu().numpy()
+    rows = len(tok)
+    col = lambda v: v.cpu().numpy() if isinstance(v, torch.Tensor) else np.full(rows, v)
+    T, top_k, top_p, min_p = col(T), col(top_k), col(top_p), col(min_p)
+    for r in range(rows):
+        want = reference(z[r], T[r], int(top_k[r]), top_p[r], min_p[r], u[r])
+        where = (r, float(T[r]), int(top_k[r]), float(top_p[r]), float(min_p[r]), float(u[r]))
+        assert (int(tok[r]), int(count[r])) == (want[0], want[2]), (where, int(tok[r]), int(count[r]), want)
+        half = float(np.finfo(np.float32).eps) / 2
+        assert abs(float(prob[r]) - want[1]) <= want[1] * (half + FAR) + 1e-44, (where, float(prob[r]), want)
+        with np.errstate(over="ignore"):                          # (a log mass beyond fp32's range rounds to infinity)
+            rounded = np.float32(want[3])
+        assert lse[r] == rounded or abs(float(lse[r]) - want[3]) <= abs(want[3]) * half * (1 + 2.0 ** -20) + FAR, (where, float(lse[r]), want)
+
+
+def rows_of(n, V, dtype, kind, seed, pad=0, shift=0):
+    """[n, V] device logits, a view off any boundary."""
+    rng = np.random.default_rng(seed)
+    if kind == "normal":
+        z = rng.normal(size=(n, V)) * 3
+    elif kind == "flat":
+        z = rng.normal(size=(n, V)) * 0.5 - 1.2 * np.log(np.floor(rng.random((n, V)) * V) + 1.0)
+    elif kind == "trend":                                          # (frequent tokens at low ids)
+        z = rng.normal(size=(n, V)) - 1.1 * np.log(np.arange(V) + 1.0)
+    elif kind == "grid":                                           # (few values: many ties)
+        z = np.round(rng.normal(size=(n, V)) * 2) / 2
+    elif kind == "const":
+        z = np.full((n, V), -2.5)
+    flat = torch.zeros(n * (V + pad) + shift, dtype=dtype, device="cuda")
+    out = flat[shift:].view(n, V + pad)[:, :V]
+    out.copy_(torch.from_numpy(z).to(dtype))
+    return out, torch.from_numpy(rng.random(n).astype(np.float32)).cuda()
+
+
+SETTINGS = [dict(), dict(T=0.0), dict(T=0.7, top_k=1), dict(T=0.8, top_k=50, top_p=0.95), dict(top_p=0.9), dict(T=0.6, top_p=0.5, min_p=0.01),
+            dict(T=1.2, min_p=0.1), dict(top_k=700), dict(top_k=700, min_p=0.02), dict(T=1.5, top_k=300, top_p=0.8, min_p=0.05), dict(top_p=1.0, min_p=1.0),
+            dict(top_k=5000, top_p=0.99), dict(T=100.0, top_p=0.3), dict(T=0.01), dict(top_p=1e-6)]
+
+
+@pytest.mark.parametrize("setting", SETTINGS, ids=lambda s: ",".join(f"{k}={v}" for k, v in s.items()) or "plain")
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,kind,pad,shift", [
+    (3, 1, "normal", 0, 0), (4, 2, "grid", 1, 1), (5, 9, "normal", 0, 3), (6, 1023, "grid", 2, 1), (4, 4096, "normal", 0, 0), (5, 5003, "flat", 1, 5),
+    (3, 32000, "normal", 0, 0), (4, 50001, "flat", 2, 1), (2, 50001, "grid", 0, 0), (2, 40000, "trend", 0, 0), (2, 33333, "const", 3, 0),
+    (2, 152064, "flat", 0, 0), (2, 151936, "normal", 5, 0),
+], ids=str)
+def test_against_the_definition(gpu, ps, rows, V, kind, pad, shift, dtype, setting):
+    print(f"[case] sample rows={rows} V={V} {kind} pad={pad} shift={shift} {dtype} {setting}", flush=True)
+    z, u = rows_of(rows, V, dtype, kind, rows * 100003 + V, pad, shift)
+    s = dict(dict(T=1.0, top_k=0, top_p=0.0, min_p=0.0), **setting)
+    got = ps.sample(z, V, u, temperature=s["T"], top_k=s["top_k"], top_p=s["top_p"], min_p=s["min_p"])
+    compare(got, z, s["T"], s["top_k"], s["top_p"], s["min_p"], u)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(24, 20001), (96, 33000), (300, 8200)])
+def test_settings_per_row(gpu, ps, rows, V, dtype):
+    """Every row with its own settings, greedy ones among them, and the ones that count as something else."""
+    print(f"[case] sample per row {rows} x {V} {dtype}", flush=True)
+    rng = np.random.default_rng(rows)
+    z, u = rows_of(rows, V, dtype, "flat", rows)
+    d = lambda a, t: torch.from_numpy(np.asarray(a).astype(t)).cuda()
+    T = d(rng.choice([0.0, 0.6, 0.9, 1.3], rows), np.float32)
+    k = d(rng.choice([0, -4, 1, 50, 900, 4097], rows), np.int32)
+    p = d(rng.choice([0.0, -1.0, 0.5, 0.9, 1.0, 2.0], rows), np.float32)
+    m = d(rng.choice([0.0, -1.0, 0.05, 1.0], rows), np.float32)
+    compare(ps.sample(z, V, u, temperature=T, top_k=k, top_p=p, min_p=m), z, T, k, p, m, u)
+    got = ps.sample(z, V, u, temperature=torch.full_like(T, math.nan), top_k=k, top_p=torch.full_like(p, math.nan), min_p=torch.full_like(m, 7.0))
+    compare(got, z, 0.0, 1, 0.0, 1.0, u)
+
+
+@pytest.mark.parametrize("setting", [dict(), dict(top_k=40), dict(top_p=0.9), dict(min_p=0.05), dict(top_k=3000, top_p=0.97)], ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [37, 9001, 70001])
+def test_masks_and_odd_values(gpu, ps, V, dtype, setting):
+    """Rows masked with -inf and with the type's lowest value, one that is masked whole, NaN and +inf, one id, all ids equal to the lowest value."""
+    print(f"[case] sample masks V={V} {dtype} {setting}", flush=True)
+    z, u = rows_of(12, V, dtype, "normal", V, 1, 1)
+    rng = np.random.default_rng(V)
+    off = torch.from_numpy(rng.random((12, V)) < 0.875).cuda()
+    low = torch.finfo(dtype).min
+    z[0] = torch.where(off[0], torch.full_like(z[0], -math.inf), z[0])
+    z[1] = torch.where(off[1], torch.full_like(z[1], low), z[1])
+    z[2] = -math.inf
+    z[3] = math.nan
+    z[4, V // 2] = math.nan
+    z[5, V // 3] = math.inf
+    z[6, V // 3], z[6, V - 1] = math.inf, math.inf
+    z[7] = -math.inf
+    z[7, V - 1] = -3.0
+    z[8] = low
+    z[9] = 0.0
+    z[9, ::2] = -0.0                                               # (they tie)
+    z[10] *= 1000.0
+    z[11] = torch.where(off[11], torch.full_like(z[11], math.nan), z[11])
+    s = dict(dict(top_k=0, top_p=0.0, min_p=0.0), **setting)
+    compare(ps.sample(z, V, u, temperature=0.9, **s), z, 0.9, s["top_k"], s["top_p"], s["min_p"], u)
+
+
+@pytest.mark.parametrize("top_p", [0.0, 0.9])
+def test_the_ends_of_the_uniforms(gpu, ps, top_p):
+    """u = 0 draws the first kept id, the largest u below 1 the last; outside [0, 1): the first and the last."""
+    print("[case] sample ends", flush=True)
+    z, _ = rows_of(6, 30011, torch.float32, "normal", 4)
+    z[:] = z[0]
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, -0.5, math.nan, 1.0, 3.0], device="cuda")
+    got = ps.sample(z, 30011, u, top_p=top_p)
+    compare(ps.sample(z[:2], 30011, u[:2], top_p=top_p), z[:2], 1.0, 0, top_p, 0.0, u[:2])
+    tok = got.tok.cpu().tolist()
+    assert tok[2] == tok[0] and tok[3] == tok[0] and tok[4] == tok[5] and tok[4] >= tok[1]
+
+
+def test_draws_follow_the_distribution(gpu, ps):
+    """4096 draws of one row of 50 ids, at evenly spaced uniforms: frequencies are the probabilities to one and a half draws."""
+    print("[case] sample frequencies", flush=True)
+    z, _ = rows_of(1, 50, torch.float32, "normal", 8)
+    n = 4096
+    u = torch.from_numpy(((np.arange(n) + 0.5) / n).astype(np.float32)).cuda()
+    got = ps.sample(z.expand(n, 50).contiguous(), 50, u, temperature=1.5)
+    torch.cuda.synchronize()
+    p = np.exp(z[0].double().cpu().numpy() / 1.5)
+    p /= p.sum()
+    seen = np.bincount(got.tok.cpu().numpy(), minlength=50) / n
+    assert np.abs(seen - p).max() <= 1.5 / n                        # (both ends of an id's share fall between two uniforms)
+
+
+def test_same_bits_streams_and_graph(gpu, ps):
+    print("[case] sample stream and graph", flush=True)
+    for rows, V, s in ((3, 20001, dict(top_k=40, top_p=0.9)), (5, 70001, dict(top_p=0.9)), (2, 33001, dict())):
+        z, u = rows_of(rows, V, torch.bfloat16, "flat", 3)
+        want = ps.sample(z, V, u, **s)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = ps.sample(z, V, u, **s)
+        side.synchronize()
+        same = lambda a, b: all(torch.equal(x, y) for x, y in ((a.tok, b.tok), (a.prob, b.prob), (a.count, b.count), (a.lse, b.lse)))
+        assert same(got, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cap = ps.sample(z, V, u, **s)
+        for i in range(3):
+            z.copy_(torch.randn_like(z) * (1 + i))
+            u.copy_(torch.rand_like(u))
+            graph.replay()
+            torch.cuda.synchronize()
+            now = ps.sample(z, V, u, **s)
+            torch.cuda.synchronize()
+            assert same(cap, now)
+
+
+def test_refusals_of_the_binding(gpu, ps):
+    z, u = rows_of(4, 100, torch.float32, "normal", 1)
+    f = lambda *v: torch.tensor(v, device="cuda")
+    for call in (lambda: ps.sample(z, 100, u[:3]), lambda: ps.sample(z, 100, u.double()), lambda: ps.sample(z, 101, u), lambda: ps.sample(z[:, ::2], 50, u),
+                 lambda: ps.sample(z.half(), 100, u), lambda: ps.sample(z, 100, u, temperature=-1.0), lambda: ps.sample(z, 100, u, min_p=2.0),
+                 lambda: ps.sample(z, 100, u, temperature=f(1.0, 1.0, 1.0)), lambda: ps.sample(z, 100, u, top_k=f(1.0, 1.0, 1.0, 1.0)),
+                 lambda: ps.sample(z, 100, u, top_p=u.cpu())):
+        with pytest.raises(ps.PicoSpecError):
+            call()
+    torch.cuda.synchronize()
