@@ -97,7 +97,7 @@ enum {
 
 enum { PICOSPEC_CALL_COMPRESS = 0, PICOSPEC_CALL_SAMPLE_DRAFT = 1, PICOSPEC_CALL_VERIFY = 2, PICOSPEC_CALL_SAMPLE_RESIDUAL = 3,
        PICOSPEC_CALL_COMPRESS_REJECTED = 4, PICOSPEC_CALL_RESAMPLE_SPARSE = 5, PICOSPEC_CALL_ROUND = 6,
-       PICOSPEC_CALL_VERIFY_SAMPLE = 7, PICOSPEC_CALL_ROW_STATS = 8 };
+       PICOSPEC_CALL_VERIFY_SAMPLE = 7, PICOSPEC_CALL_ROW_STATS = 8, PICOSPEC_CALL_SAMPLE = 9 };
 enum { PICOSPEC_LIMIT_MAX_K = 0, PICOSPEC_LIMIT_MAX_V = 1 };
 
 /*
@@ -436,8 +436,10 @@ int picospec_unpack_uplink(const void* wire, int64_t wire_bytes, int32_t B, int3
  *   uniforms     [n_rows] in [0,1)                                                                            in
  *   tok [n_rows] int32, prob [n_rows] fp32 = the token's share of the kept mass, count [n_rows] int32 = how many ids are kept,
  *   lse [n_rows] fp32 = max z / T + ln(kept mass)                                                             out
- * A row without a logit above -inf: tok -1, prob 0, count 0, lse -inf.  Masses are summed in 64 bits, in the order of a fixed rule: a call
- * gives the same bits every time.
+ *   workspace    (optional): picospec_workspace_bytes(PICOSPEC_CALL_SAMPLE, dtype, n_rows, V, 0) bytes of scratch, in which a call of few rows spreads
+ *                every row over several workgroups; NULL or a smaller one: one workgroup per row
+ * A row without a logit above -inf: tok -1, prob 0, count 0, lse -inf.  Masses are summed in 64 bits, in an order that the sizes and the
+ * row decide: a call gives the same bits every time.
  */
 int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
                     float temperature, int32_t top_k, float top_p, float min_p,

@@ -27,7 +27,7 @@ F32, BF16 = 0, 1
 OK, EINVAL, EWORKSPACE, EDTYPE, EHIP, EUNSUPPORTED, ESCRATCH = 0, -1, -2, -3, -4, -5, -6
 FLAG_TOKEN_NOT_IN_SUPPORT, FLAG_NONFINITE, FLAG_RESIDUAL_EMPTY, FLAG_BAD_INPUT = 1, 2, 4, 8
 CALL_COMPRESS, CALL_SAMPLE_DRAFT, CALL_VERIFY, CALL_SAMPLE_RESIDUAL = 0, 1, 2, 3
-CALL_COMPRESS_REJECTED, CALL_RESAMPLE_SPARSE, CALL_ROUND, CALL_VERIFY_SAMPLE, CALL_ROW_STATS = 4, 5, 6, 7, 8
+CALL_COMPRESS_REJECTED, CALL_RESAMPLE_SPARSE, CALL_ROUND, CALL_VERIFY_SAMPLE, CALL_ROW_STATS, CALL_SAMPLE = 4, 5, 6, 7, 8, 9
 LIMIT_MAX_K, LIMIT_MAX_V = 0, 1
 WIRE_FP32, WIRE_FP16, WIRE_BF16 = 0, 1, 2
 WIRE_BAD_HEADER, WIRE_BAD_BATCH, WIRE_CLAMPED, WIRE_TRUNCATED = 1, 2, 4, 8
@@ -412,7 +412,8 @@ def sample(logits: torch.Tensor, V: int, uniforms: torch.Tensor, temperature=1.0
     p, p_rows = _setting(top_p, rows, torch.float32)
     m, m_rows = _setting(min_p, rows, torch.float32)
     out = out or Sampled(*_nat.empty(logits, "ifif", rows, rows, rows, rows))
-    _check(_nat.sample(logits, dt, ld, rows, V, T, k, p, m, T_rows, k_rows, p_rows, m_rows, uniforms, out.tok, out.prob, out.count, out.lse, None, _stream()))
+    _check(_nat.sample(logits, dt, ld, rows, V, T, k, p, m, T_rows, k_rows, p_rows, m_rows, uniforms, out.tok, out.prob, out.count, out.lse,
+                       _nat.scratch(logits, CALL_SAMPLE, dt, rows, 0, V, 0), _stream()))
     return out
 
 

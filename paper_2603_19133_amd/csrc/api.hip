@@ -518,9 +518,8 @@ int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, i
     if ((!top_p_rows && std::isnan(top_p)) || (!min_p_rows && !(min_p <= 1.f))) return PICOSPEC_EINVAL;
     if (n_rows > 0 && (!uniforms || !tok || !prob || !count || !lse)) return PICOSPEC_EINVAL;
     if ((uintptr_t)workspace & 15u) return PICOSPEC_EWORKSPACE;
-    (void)workspace_bytes;
     return hip_status(launch_sample(logits, dtype, ld, n_rows, V, temperature, top_k, top_p, min_p, temperature_rows, top_k_rows, top_p_rows, min_p_rows,
-                                    uniforms, tok, prob, count, lse, (hipStream_t)stream));
+                                    uniforms, tok, prob, count, lse, workspace, workspace_bytes, (hipStream_t)stream));
 }
 
 namespace {
@@ -573,6 +572,7 @@ size_t picospec_workspace_bytes(int which_call, int dtype, int32_t rows, int32_t
             const size_t table = round_seg_table_bytes(dtype, rows, V), split = split_scratch_bytes(dtype, rows, V, k);
             return split ? (table + 15) / 16 * 16 + split : table;
         }
+        case PICOSPEC_CALL_SAMPLE: return sample_scratch_bytes(dtype, rows, V);
         default:
             return 0;                           // every other kernel keeps its intermediate state in LDS
     }
@@ -595,6 +595,7 @@ size_t picospec_scratch_bytes(int which_call, int dtype, int32_t n_draft, int32_
             if (!round_split_serves(dtype, n_draft, rows, V, k)) return 0;
             return (round_seg_table_bytes(dtype, rows, V) + 15) / 16 * 16 + split_scratch_bytes(dtype, n_draft, V, k);
         }
+        case PICOSPEC_CALL_SAMPLE: return sample_scratch_bytes(dtype, n_draft, V);
         default: return 0;
     }
 }

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 
@@ -411,10 +412,34 @@ hipError_t launch_pack_uplink(int B, int n_draft, const int32_t* seq_off, const 
 hipError_t launch_unpack_uplink(const void* wire, int64_t wire_bytes, int B, int n_max, int32_t* seq_off,
                                 int32_t* draft_tok, float* q_scalar, uint32_t* status, hipStream_t stream);
 
-// ---- one token per row from the filtered distribution (csrc/sample.hip); *_rows: a setting per row, null where one serves all
+// ---- one token per row from the filtered distribution (csrc/sample.hip); *_rows: a setting per row, null where one serves all.
+// A call of few rows spreads every row over several workgroups, in scratch on a 16-byte boundary: as many as the chip holds at once (two on each of its
+// 256 CUs), each with a segment for every wave at least.
+constexpr int kSampleThreads = 512, kSampleList = 7168, kSampleSlots = 512, kSampleMostParts = 64;
+inline int sample_parts(int dtype, int64_t rows, int V) {
+    if (rows < 1 || V < 1) return 1;
+    const int waves = kSampleThreads / 64, most = (stats_segments(row_vecs_max(dtype == 1, V)) + waves - 1) / waves;
+    const int64_t fit = kSampleSlots / rows;
+    return (int)std::min<int64_t>(std::min(std::max<int64_t>(fit, 1), (int64_t)kSampleMostParts), most);
+}
+// a row's share of it: the arrival word, three words a part, one for the row and two sums a part, the segments' masses, the parts' histograms, the parts' lists
+struct SampleScratch { size_t seg_at, hist_at, list_at, row_bytes; int list_cap; };
+__host__ __device__ inline SampleScratch sample_scratch(bool bf16, int V, int parts) {
+    SampleScratch l;
+    l.seg_at = kArrivalStride + ((size_t)parts * 6 + 2 + 31) / 32 * 256;
+    l.hist_at = l.seg_at + ((size_t)stats_segments(row_vecs_max(bf16, V)) + 31) / 32 * 256;
+    l.list_at = l.hist_at + (size_t)parts * 2048 * 8;
+    l.list_cap = kSampleList * 2 / parts + 512 < kSampleList ? kSampleList * 2 / parts + 512 : kSampleList;
+    l.row_bytes = l.list_at + ((size_t)parts * l.list_cap * 8 + 255) / 256 * 256;
+    return l;
+}
+inline size_t sample_scratch_bytes(int dtype, int64_t rows, int V) {
+    const int parts = sample_parts(dtype, rows, V);
+    return parts > 1 ? (size_t)rows * sample_scratch(dtype == 1, V, parts).row_bytes : 0;
+}
 hipError_t launch_sample(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature, int top_k, float top_p, float min_p,
                          const float* temperature_rows, const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows,
-                         const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse, hipStream_t stream);
+                         const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse, void* scratch, size_t scratch_bytes, hipStream_t stream);
 
 // ---- distillation on records (csrc/distill.hip): one workgroup of kDistillThreads per row; with the gradient in the same call a thread keeps
 // kDistillHeld vectors of its row in registers from the sum to the gradient

@@ -16,12 +16,13 @@ namespace picospec {
 
 namespace {
 
-constexpr int kST = 512;                          // threads: one row
+constexpr int kST = kSampleThreads;
 constexpr int kSW = kST / kWave;
 constexpr int kSegs = kMaxV / 1024 + 2;           // segments of the longest row (fp32, off the boundary)
-constexpr int kBins = 2048;                       // of a histogram: four a thread
-constexpr int kBinsPer = kBins / kST;
 constexpr int kSegsPer = (kSegs + kST - 1) / kST;
+constexpr int kBins = 2048;                       // of a histogram over the row
+constexpr int kListBins = 1024;                   // ... over a list
+constexpr int kPeek = 8192;                       // elements that are looked at before the row is streamed
 constexpr double kLog2e = 1.4426950408889634;
 constexpr float kFloatMax = 3.4028234663852886e38f;
 
@@ -30,6 +31,7 @@ struct SampleArgs {
     float T; int top_k; float top_p, min_p;
     const float* T_rows; const int32_t* k_rows; const float *p_rows, *minp_rows; const float* u;
     int32_t* tok; float* prob; int32_t* count; float* lse;
+    char* scratch; int parts;                     // workgroups of a row; scratch of sample_scratch(...) where there are several
 };
 
 // 2^(d c), d = z - ref in fp64 (exact unless the two lie 2^29 apart).  The exponent is split at the nearest integer by adding 1.5 * 2^52, whose sum's low word
@@ -66,13 +68,22 @@ struct Cut {
 
 struct RowShared {
     double seg[kSegs];                            // kept mass of the segments
-    unsigned long long mass[kBins];
-    uint32_t count[kBins];
+    union {
+        unsigned long long list[kSampleList];     // composites: (logit descending, id ascending) == descending
+        unsigned long long hist[2][kBins];        // (how many, in 2^40; the sum of their places in the bin, in 2^-20); a copy for odd and one for even lanes
+        struct { unsigned long long mass[kBins]; uint32_t count[kBins]; } row;
+    };
+    unsigned long long mass[kListBins];
+    uint32_t count[kListBins];
     double red[2 * kSW];
     unsigned long long redu[kSW + 2];
-    int at, last;
+    unsigned long long entry, ends[2][kSW];
+    int at, last, n;
     float f[kSW + 1];
+    uint32_t votes[2][kSW];
+    int part_at[kWave];                           // ends of the parts' lists
 };
+static_assert(sizeof(RowShared) <= 80 * 1024, "two workgroups per CU");
 
 template <bool BF16>
 struct RowStream {
@@ -97,23 +108,23 @@ struct RowStream {
         }
     }
     // the values of vector q, -inf outside the row, and the id of the first of them
-    __device__ __forceinline__ void values(const uint4& raw, int q, float (&v)[Vec<BF16>::N]) const {
+    __device__ __forceinline__ void values(const uint4& raw, int q, int s, float (&v)[Vec<BF16>::N]) const {       // (of segment s)
         unpack<BF16>(raw, v);
-        if (q == 0 || q >= nq - 1) {
+        if (s == 0 || s >= n_seg - 1) {
             const unsigned vm = vec_valid_mask<BF16>(rv, q);
 #pragma unroll
             for (int e = 0; e < Vec<BF16>::N; ++e) v[e] = (vm >> e) & 1u ? v[e] : kNegInf;
         }
     }
     __device__ __forceinline__ int first_id(int q) const { return q * Vec<BF16>::N - rv.o; }
-    // f(s, raw) for every segment, a wave each, the next one's loads in flight
+    // f(s, raw) for every segment of workgroup `part` of `parts`, a wave each, the next one's loads in flight
     template <class F>
-    __device__ __forceinline__ void each(const F& f) const {
+    __device__ __forceinline__ void each(const F& f, int part = 0, int parts = 1) const {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         uint4 cur[kSplitStatsNV], next[kSplitStatsNV];
-        load(wave, cur);
-        for (int s = wave; s < n_seg; s += kSW) {
-            load(s + kSW, next);
+        load(part * kSW + wave, cur);
+        for (int s = part * kSW + wave; s < n_seg; s += parts * kSW) {
+            load(s + parts * kSW, next);
             f(s, cur);
 #pragma unroll
             for (int j = 0; j < kSplitStatsNV; ++j) cur[j] = next[j];
@@ -128,12 +139,13 @@ struct RowStream {
             for (int j = 0; j < kSplitStatsNV; ++j) {
                 const int q = stats_group_first(s, j) + lane;
                 float v[Vec<BF16>::N];
-                values(raw[j], q, v);
+                values(raw[j], q, s, v);
 #pragma unroll
                 for (int e = 0; e < Vec<BF16>::N; ++e) {
                     const float z = cleaned(v[e]);
                     if (z > kNegInf) f(z, first_id(q) + e, s);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         });
     }
@@ -216,7 +228,7 @@ __device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w
     const int q = s * (64 * kSplitStatsNV) + tid;
     const bool have = s >= 0 && tid < 64 * kSplitStatsNV;
     float v[N];
-    rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, v);
+    rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, s, v);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         const float z = cleaned(v[e]);
@@ -244,19 +256,20 @@ __device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w
 // ---------------------------------------------------------------- the careful way: any row, by passes over its keys
 
 // The bin, descending, in which `above` + the sums up to and with it reach the target; `above` becomes what lies in front of it.  -1: none does.
-template <typename T>
+template <int BINS, typename T>
 __device__ __forceinline__ int crossing(const T* bins, unsigned long long& above, double target, RowShared& sh, unsigned long long* total = nullptr)
 {
+    constexpr int PER = BINS / kST;
     const int tid = threadIdx.x;
-    unsigned long long mine[kBinsPer], sum = 0;
+    unsigned long long mine[PER], sum = 0;
 #pragma unroll
-    for (int i = 0; i < kBinsPer; ++i) { mine[i] = bins[tid * kBinsPer + i]; sum += mine[i]; }
+    for (int i = 0; i < PER; ++i) { mine[i] = bins[tid * PER + i]; sum += mine[i]; }
     if (tid == 0) sh.at = -1;
     unsigned long long all, b = above + block_scan_excl(sum, sh.redu, all);
     if (total) { *total = all; target *= (double)all; }
 #pragma unroll
-    for (int i = 0; i < kBinsPer; ++i) {
-        if ((double)b < target && (double)(b + mine[i]) >= target) { sh.at = tid * kBinsPer + i; sh.redu[kSW] = b; }
+    for (int i = 0; i < PER; ++i) {
+        if ((double)b < target && (double)(b + mine[i]) >= target) { sh.at = tid * PER + i; sh.redu[kSW] = b; }
         b += mine[i];
     }
     __syncthreads();
@@ -267,9 +280,10 @@ __device__ __forceinline__ int crossing(const T* bins, unsigned long long& above
 }
 
 template <bool BF16>
-__device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float T, int k, float p, float min_p, int V,
+__device__ __attribute__((noinline)) void sample_careful(const void* logits, int64_t ld, int64_t row, float T, int k, float p, float min_p, int V,
                                                RowShared& sh, Weights& w, Cut& cut, int& kept, float& M)
 {
+    const RowStream<BF16> rs(logits, ld, row, V);
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     float mx = kNegInf, mn = __builtin_huge_valf();
     unsigned n = 0;
@@ -291,7 +305,7 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
     unsigned long long ties = 0;
     bool has_cut = false;
     auto clear = [&] {
-        for (int i = tid; i < kBins; i += kST) { sh.mass[i] = 0; sh.count[i] = 0; }
+        for (int i = tid; i < kBins; i += kST) { sh.row.mass[i] = 0; sh.row.count[i] = 0; }
         __syncthreads();
     };
     auto fixed = [&](float z) { return (unsigned long long)(ldexp(w.weight(z), shift) + 0.5); };
@@ -304,10 +318,10 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
             clear();
             rs.each_value([&](float z, int, int) {
                 const uint32_t key = key_of_bits(__float_as_uint(z));
-                if (key >= lo && key <= hi) atomicAdd(&sh.count[(hi - key) >> sft], 1u);
+                if (key >= lo && key <= hi) atomicAdd(&sh.row.count[(hi - key) >> sft], 1u);
             });
             __syncthreads();
-            const int bin = max(0, crossing(sh.count, above, (double)k, sh));
+            const int bin = max(0, crossing<kBins>(sh.row.count, above, (double)k, sh));
             hi -= (uint32_t)bin << sft;
             if (sft == 0) break;
             const uint32_t next = hi - ((1u << sft) - 1u);
@@ -331,21 +345,21 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
             rs.each_value([&](float z, int, int) {
                 const uint32_t key = key_of_bits(__float_as_uint(z));
                 if (key >= lo && key <= hi && !(top && key == k_key)) {
-                    atomicAdd(&sh.mass[(hi - key) >> sft], fixed(z));
-                    atomicAdd(&sh.count[(hi - key) >> sft], 1u);
+                    atomicAdd(&sh.row.mass[(hi - key) >> sft], fixed(z));
+                    atomicAdd(&sh.row.count[(hi - key) >> sft], 1u);
                 }
             });
             if (top && tid == 0 && k_key >= lo && k_key <= hi) {                 // (of the ties at the end of the first top_k, those that are among them)
-                atomicAdd(&sh.mass[(hi - k_key) >> sft], k_one * k_ties);
-                atomicAdd(&sh.count[(hi - k_key) >> sft], (unsigned)k_ties);
+                atomicAdd(&sh.row.mass[(hi - k_key) >> sft], k_one * k_ties);
+                atomicAdd(&sh.row.count[(hi - k_key) >> sft], (unsigned)k_ties);
             }
             __syncthreads();
-            const int bin = max(0, crossing(sh.mass, above, target, sh, first ? &total : nullptr));
+            const int bin = max(0, crossing<kBins>(sh.row.mass, above, target, sh, first ? &total : nullptr));
             if (first) target *= (double)total;
             hi -= (uint32_t)bin << sft;
             if (sft == 0) {
                 // The integers' roundings, equal for equal logits, name the value; how many of its elements are kept is decided in fp64.
-                const unsigned long long have = sh.count[bin];
+                const unsigned long long have = sh.row.count[bin];
                 const float z_t = __uint_as_float(bits_of_key(hi)), z_k = top ? __uint_as_float(bits_of_key(k_key)) : kNegInf;
                 double over = 0.0, all = 0.0;
                 rs.each_value([&](float z, int, int) {
@@ -372,10 +386,10 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
         cut.t = __uint_as_float(bits_of_key(t_key));
         static_assert(kSegs <= kBins, "a count for every segment");
         clear();
-        rs.each_value([&](float z, int, int s) { if (z == cut.t) atomicAdd(&sh.count[s], 1u); });
+        rs.each_value([&](float z, int, int s) { if (z == cut.t) atomicAdd(&sh.row.count[s], 1u); });
         __syncthreads();
         unsigned long long above = 0;
-        const int s = crossing(sh.count, above, (double)ties, sh);
+        const int s = crossing<kBins>(sh.row.count, above, (double)ties, sh);
         if (tid == 0) sh.at = INT32_MAX;
         __syncthreads();
         if (s >= 0) {
@@ -383,7 +397,7 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
             const int q = s * (64 * kSplitStatsNV) + tid;
             const bool have = tid < 64 * kSplitStatsNV;
             float v[N];
-            rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, v);
+            rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, s, v);
             unsigned long long mine = 0, all;
 #pragma unroll
             for (int e = 0; e < N; ++e) mine += have && cleaned(v[e]) == cut.t;
@@ -404,7 +418,7 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
         for (int j = 0; j < kSplitStatsNV; ++j) {
             const int q = stats_group_first(s, j) + lane;
             float v[Vec<BF16>::N];
-            rs.values(raw[j], q, v);
+            rs.values(raw[j], q, s, v);
 #pragma unroll
             for (int e = 0; e < Vec<BF16>::N; ++e) {
                 const float z = cleaned(v[e]);
@@ -412,6 +426,7 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
                 sum += keep ? w.weight(z) : 0.0;
                 mine += keep;
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         sum = wave_sum(sum);
         if (lane == 0) sh.seg[s] = sum;
@@ -421,25 +436,631 @@ __device__ __forceinline__ void sample_careful(const RowStream<BF16>& rs, float 
     kept = (int)n_kept;
 }
 
+// ---------------------------------------------------------------- the quick ways
+//
+// kPeek elements of the row, taken evenly from it, say beforehand how the row can be served in one pass over it, or in two:
+//   sum      nothing is cut off: the segments' masses, against the largest element of the peek.
+//   list     what may be kept is short: the elements at or above a threshold go to a list in LDS.  top-k: the value of rank optimistic_rank(..) of
+//            the peek.  min-p alone: what min-p leaves against the peek's largest, which is no larger than the row's.  top-p alone: about kTopPList elements, with the mass
+//            of the whole row beside, where the peek has its mass there.
+//   histogram  top-p alone on rows whose mass is spread: a first pass counts by logit (2048 bins of 1/64 nat below the peek's largest, with the mean place
+//            of a bin's elements, of whose mass it gives 10^-5), which names the bin, or the few, in which the prefix ends; a second one sums the segments'
+//            masses above them and lists what lies in them.  (Counts, not masses: LDS adds a wave's 64 integers in 10 to 20 cycles, 64 floats in 195.)
+//            Elements that are likely behind the prefix are left out of the counts; a prefix that ends among them after all takes a third pass.
+// Whatever the peek promised is checked against the row (lists that are short or overflow, a prefix that does not end in its bins, +inf): such
+// rows, and records beyond the list, take the careful way.
+enum Way : int { kCareful, kSum, kList, kHist };
+constexpr int kTopPList = 2048;
+constexpr double kHistFar = 3e-5;                 // relative error allowed for the histogram's sums (checked in fp64 behind it)
+constexpr float kHistPerNat = 64.f;
+
+// ref: the peek's largest; least: what goes to the list; total: the row's mass as well; far: the bins that are counted
+struct Plan { Way way; float ref, least; bool total; float far; };
+
 template <bool BF16>
+__device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, int k, float p, float min_p, RowShared& sh)
+{
+    constexpr int N = Vec<BF16>::N, PER = kPeek / (kST * N);                    // vectors a thread
+    constexpr int BLOCKS = PER * kSW;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int n_blocks = (rs.nq + kWave - 1) / kWave;
+    float v[PER][N];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        // (rows of fewer blocks than that: each once)
+        const int i = j * kSW + wave, blk = n_blocks <= BLOCKS ? i : (int)((int64_t)i * n_blocks / BLOCKS), q = blk * kWave + lane;
+        rs.values(rs.vec(q), q, 0, v[j]);
+    }
+    float mx = kNegInf;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            v[j][e] = fmaxf(v[j][e], kNegInf);                                  // (NaN)
+            mx = fmaxf(mx, v[j][e]);
+        }
+    const float ref = block_max(mx, sh);
+    Plan pl{kCareful, ref, kNegInf, false, (float)(kBins - 1)};
+    if (!(ref > kNegInf) || !(ref <= kFloatMax)) return pl;
+    const bool cut_p = p > 0.f && p < 1.f, all = V <= kSampleList;
+    if (k <= 0 && !cut_p && !(min_p > 0.f)) { pl.way = kSum; return pl; }
+    if (all) { pl.way = kList; pl.total = k <= 0 && cut_p; return pl; }
+    if (k <= 0 && !cut_p) {                                                     // min-p alone
+        pl.way = kList;
+        pl.least = float_below(float_below((float)((double)ref + (double)T * log((double)fminf(min_p, 1.f)))));
+        return pl;
+    }
+    const int want = k > 0 ? k : kTopPList;
+    const int rank = want <= kSampleList ? optimistic_rank(want, V, min(kPeek, V), kSampleList) : 0;
+    if (rank == 0) {
+        if (k <= 0) pl.way = kHist;
+        return pl;
+    }
+    // the peek's element of that rank, or one a little behind: a threshold with `rank` to 1.25 `rank` elements at or above it
+    uint32_t lo = key_of_bits(__float_as_uint(kNegInf)), hi = key_of_bits(__float_as_uint(ref));
+    if (rank <= kST) lo = key_of_bits(__float_as_uint(-block_max(-mx, sh)));    // (every thread has one at or above the least of their largest)
+    for (int i = 0; lo < hi; ++i) {                                             // (count at or above lo >= rank, above hi: none; 32 halvings at most)
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        uint32_t n = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+#pragma unroll
+            for (int e = 0; e < N; ++e) n += (uint32_t)__builtin_popcountll(__ballot(key_of_bits(__float_as_uint(v[j][e])) >= mid));
+        if (lane == 0) sh.votes[i & 1][wave] = n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int w = 0; w < kSW; ++w) n += sh.votes[i & 1][w];
+        if (n >= (uint32_t)rank) {
+            lo = mid;
+            if (n <= (uint32_t)(rank + rank / 4)) break;
+        } else {
+            hi = mid - 1;
+        }
+    }
+    __syncthreads();
+    pl.least = __uint_as_float(bits_of_key(lo));
+    pl.way = kList;
+    if (k > 0) return pl;
+    pl.total = true;
+    const float c = (float)(kLog2e / (double)T);
+    float above = 0.f, total = 0.f;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float x = exp_stream(v[j][e], ref, c);
+            total += x;
+            above += v[j][e] >= pl.least ? x : 0.f;
+        }
+    double a_all, t_all;
+    block_scan_excl((double)above, sh.red, a_all);
+    block_scan_excl((double)total, sh.red, t_all);
+    // (without the peek's largest: one that is by chance among the row's few that hold much of it says nothing of the rest)
+    if (a_all - 1.0 >= ((double)p + 0.3 * (1.0 - (double)p)) * (t_all - 1.0)) return pl;
+    pl.way = kHist;
+    // bins behind which the peek has less than 1 / 1.15 of what top-p leaves out
+    float near = 0.f, far = (float)(kBins - 1);
+    for (int i = 0; i < 7; ++i) {
+        const float mid = 0.5f * (near + far);
+        float behind = 0.f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+#pragma unroll
+            for (int e = 0; e < N; ++e) behind += (ref - v[j][e]) * (kHistPerNat / T) > mid ? exp_stream(v[j][e], ref, c) : 0.f;
+        double all_behind;
+        block_scan_excl((double)behind, sh.red, all_behind);
+        if (all_behind * 1.15 <= (1.0 - (double)p) * (t_all - 1.0)) far = mid;
+        else near = mid;
+    }
+    pl.far = far;
+    return pl;
+}
+
+// Appends the elements of a segment whose bit is set (bit j * N + e) to the list.  sh.n counts on behind the list's end.
+template <bool BF16>
+__device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, const uint4 (&raw)[kSplitStatsNV], unsigned mask, RowShared& sh)
+{
+    constexpr int N = Vec<BF16>::N;
+    if (!__ballot(mask != 0u)) return;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int mine = __builtin_popcount(mask), incl = wave_scan_incl(mine), total = read_lane(incl, kWave - 1);
+    int base = 0;
+    if (lane == 0) base = atomicAdd(&sh.n, total);
+    int at = read_lane(base, 0) + incl - mine;
+#pragma unroll
+    for (int j = 0; j < kSplitStatsNV; ++j) {
+        uint4 again = raw[j];                                                   // (unpacked a second time: the values are not held for it)
+        asm volatile("" : "+v"(again.x), "+v"(again.y), "+v"(again.z), "+v"(again.w));
+        float v[N];
+        unpack<BF16>(again, v);
+        const int x = rs.first_id(stats_group_first(s, j) + lane);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if ((mask >> (j * N + e)) & 1u) {
+                if (at < kSampleList) sh.list[at] = composite_of(__float_as_uint(v[e]), (uint32_t)(x + e));
+                ++at;
+            }
+    }
+}
+
+__device__ __forceinline__ unsigned long long pack2(uint32_t a, uint32_t b) { return (unsigned long long)a | (unsigned long long)b << 32; }
+
+__device__ __forceinline__ float composite_value(unsigned long long c) { return __uint_as_float(bits_of_key((uint32_t)(c >> 32))); }
+__device__ __forceinline__ int composite_id(unsigned long long c) { return (int)(0xFFFFFFFFu - (uint32_t)c); }
+
+// one pass of a workgroup over its part of the row
+template <bool BF16, Way WAY, bool TOTAL>
+__device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, int parts, const Plan& pl, const Weights& w, float T, RowShared& sh,
+                                           float& M, int& n_finite, double& total, double& above_ref)
+{
+    constexpr int N = Vec<BF16>::N;
+    const int lane = threadIdx.x & (kWave - 1);
+    const float c = (float)w.c, per = kHistPerNat / T;
+    float mx = kNegInf;
+    int n = 0;
+    double sum_all = 0.0, sum_over = 0.0;
+    rs.each([&](int s, const uint4 (&raw)[kSplitStatsNV]) {
+        unsigned mask = 0u;
+        double sum = 0.0;
+        float mass = 0.f, over = 0.f;
+#pragma unroll
+        for (int j = 0; j < kSplitStatsNV; ++j) {
+            float v[N];
+            rs.values(raw[j], stats_group_first(s, j) + lane, s, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                mx = fmaxf(mx, v[e]);
+                if constexpr (WAY == kSum || TOTAL) sum += w.weight(v[e]);
+                if constexpr (WAY == kSum) n += v[e] > kNegInf;
+                if constexpr (WAY == kList) mask |= (v[e] >= pl.least && v[e] > kNegInf) ? 1u << (j * N + e) : 0u;
+                if constexpr (WAY == kHist) {
+                    const float z = fmaxf(v[e], kNegInf), x = fminf(fmaxf((pl.ref - z) * per, 0.f), (float)(kBins - 1));
+                    const float one = exp_stream(z, pl.ref, c);
+                    mass += one;
+                    over += fmaxf(one, 1.f);                                    // (what lies above the reference is counted as lying at it)
+                    if (x <= pl.far) {
+                        const unsigned bin = (unsigned)x;
+                        atomicAdd(&sh.hist[lane & 1][bin], pack2((unsigned)((x - (float)bin) * 0x1p20f), 1u << 8));
+                    }
+                }
+                if ((WAY == kSum || TOTAL) && (e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_sched_barrier(0);                                  // (a vector's exponentials side by side, not the segment's: registers)
+        }
+        if constexpr (WAY == kList) append<BF16>(rs, s, raw, mask, sh);
+        if constexpr (WAY == kSum) {
+            sum = wave_sum(sum);
+            if (lane == 0) sh.seg[s] = sum;
+        }
+        if constexpr (TOTAL) sum_all += sum;
+        if constexpr (WAY == kHist) { sum_all += (double)mass; sum_over += (double)(over - (float)(N * kSplitStatsNV)); }
+    }, part, parts);
+    M = block_max(mx, sh);
+    n_finite = 0;
+    total = 0.0;
+    if constexpr (WAY == kSum) { unsigned long long t; block_scan_excl((unsigned long long)n, sh.redu, t); n_finite = (int)t; }
+    if constexpr (TOTAL || WAY == kHist) block_scan_excl(sum_all, sh.red, total);
+    if constexpr (WAY == kHist) block_scan_excl(sum_over, sh.red, above_ref);
+    __syncthreads();
+}
+
+// The entry of the list's first n, from composite `from` on, with which the sum over the entries at or above it reaches the target: counts, or masses of 2^-kListShift.
+// 0: none.
+constexpr int kListShift = 49;
+static_assert(kSampleList <= 1 << 13, "sums of masses stay below 2^62");
+__device__ __forceinline__ unsigned long long list_mass(unsigned long long comp, const Weights& w)
+{
+    return (unsigned long long)(ldexp(w.weight(composite_value(comp)), kListShift) + 0.5);
+}
+
+template <bool MASS>
+__device__ __forceinline__ unsigned long long select(int n, unsigned long long from, double target, const Weights& w, RowShared& sh)
+{
+    const int tid = threadIdx.x;
+    unsigned long long lo = ~0ull, hi = 0ull, above = 0;
+    for (int i = tid; i < n; i += kST) {
+        const unsigned long long c = sh.list[i];
+        if (c >= from) { lo = min(lo, c); hi = max(hi, c); }
+    }
+    lo = wave_min_u64(lo);
+    hi = wave_max_u64(hi);
+    if ((tid & (kWave - 1)) == 0) { sh.ends[0][tid / kWave] = lo; sh.ends[1][tid / kWave] = hi; }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSW; ++i) { lo = min(lo, sh.ends[0][i]); hi = max(hi, sh.ends[1][i]); }
+    if (lo > hi) return 0ull;
+    for (;;) {
+        const unsigned long long span = hi - lo;
+        const int sft = span ? max(0, 64 - 10 - __builtin_clzll(span)) : 0;
+        for (int i = tid; i < kListBins; i += kST) { sh.mass[i] = 0; sh.count[i] = 0; }
+        __syncthreads();
+        for (int i = tid; i < n; i += kST) {
+            const unsigned long long c = sh.list[i];
+            if (c >= lo && c <= hi) {
+                const int bin = (int)((hi - c) >> sft);
+                atomicAdd(&sh.count[bin], 1u);
+                if constexpr (MASS) atomicAdd(&sh.mass[bin], list_mass(c, w));
+            }
+        }
+        __syncthreads();
+        int bin;
+        if constexpr (MASS) bin = crossing<kListBins>(sh.mass, above, target, sh);
+        else bin = crossing<kListBins>(sh.count, above, target, sh);
+        if (bin < 0) return 0ull;
+        hi -= (unsigned long long)bin << sft;
+        if (sft == 0) return hi;
+        const unsigned long long next = hi - ((1ull << sft) - 1ull);
+        lo = next > hi || next < lo ? lo : next;
+        if (sh.count[bin] == 1u) {
+            for (int i = tid; i < n; i += kST) {
+                const unsigned long long c = sh.list[i];
+                if (c >= lo && c <= hi) sh.entry = c;
+            }
+            __syncthreads();
+            return sh.entry;
+        }
+        __syncthreads();
+    }
+}
+
+// sum of the masses of the list's entries at or above `from`
+__device__ __forceinline__ unsigned long long list_sum(int n, unsigned long long from, const Weights& w, RowShared& sh)
+{
+    unsigned long long mine = 0, all;
+    for (int i = threadIdx.x; i < n; i += kST) { const unsigned long long c = sh.list[i]; if (c >= from) mine += list_mass(c, w); }
+    block_scan_excl(mine, sh.redu, all);
+    return all;
+}
+
+// Adds the masses of the kept entries to their segments' (as integers of 2^-kListShift: exact, whatever the order) and counts them.
+template <bool BF16>
+__device__ __forceinline__ int list_to_segments(const RowStream<BF16>& rs, int n, const Cut& cut, const Weights& w, bool add, RowShared& sh)
+{
+    unsigned long long* const extra = sh.mass;                                  // (segments in blocks of kListBins: one, but for fp32 rows of a million)
+    unsigned long long mine = 0, all;
+    for (int first = 0; first < rs.n_seg; first += kListBins) {
+        for (int i = threadIdx.x; i < kListBins; i += kST) extra[i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += kST) {
+            const unsigned long long c = sh.list[i];
+            const int x = composite_id(c), s = (rs.rv.o + x) / (64 * kSplitStatsNV * Vec<BF16>::N) - first;
+            if (s >= 0 && s < kListBins && cut.keeps(composite_value(c), x, w)) { ++mine; atomicAdd(&extra[s], list_mass(c, w)); }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < kListBins && first + i < rs.n_seg; i += kST) {
+            const double m = ldexp((double)extra[i], -kListShift);
+            sh.seg[first + i] = add ? sh.seg[first + i] + m : m;
+        }
+        __syncthreads();
+    }
+    block_scan_excl(mine, sh.redu, all);
+    return (int)all;
+}
+
+// what hand-over between the workgroups of a row, and between the two launches of a histogram, goes through
+template <bool BF16>
+struct RowScratch {
+    unsigned long long *word, *head, *seg, *hist, *lists;
+    double2* totals;
+    int cap;
+    __device__ __forceinline__ RowScratch(const SampleArgs& a, int64_t row) {
+        const SampleScratch l = sample_scratch(BF16, a.V, a.parts);
+        char* const base = a.scratch + row * (int64_t)l.row_bytes;
+        word = (unsigned long long*)base;
+        head = (unsigned long long*)(base + kArrivalStride);
+        totals = (double2*)(base + kArrivalStride + 16 * (2 * a.parts + 1));
+        seg = (unsigned long long*)(base + l.seg_at);
+        hist = (unsigned long long*)(base + l.hist_at);
+        lists = (unsigned long long*)(base + l.list_at);
+        cap = l.list_cap;
+    }
+};
+
+// The parts' shares together in the last of a row's workgroups to arrive: segments, lists, and M, count and total.  False in the others.
+template <bool BF16>
+__device__ __forceinline__ bool gather(const RowStream<BF16>& rs, const RowScratch<BF16>& rx, int part, int parts, bool segs, bool lists,
+                                       float& M, int& count, double& total, RowShared& sh)
+{
+    const int tid = threadIdx.x;
+    const int n = lists ? sh.n : 0;
+    if (segs)
+        for (int i = tid; i < rs.n_seg; i += kST)
+            if (i / kSW % parts == part) put_shared(&rx.seg[i], (unsigned long long)__double_as_longlong(sh.seg[i]));
+    for (int i = tid; i < min(n, rx.cap); i += kST) put_shared(&rx.lists[(int64_t)part * rx.cap + i], sh.list[i]);
+    if (tid == 0) {
+        put_shared(&rx.head[part * 3], pack2((uint32_t)n, __float_as_uint(M)));
+        put_shared(&rx.head[part * 3 + 1], (unsigned long long)(unsigned)count);
+        put_shared(&rx.head[part * 3 + 2], (unsigned long long)__double_as_longlong(total));
+    }
+    if (!arrive_last(rx.word, (unsigned)parts, tid == 0)) return false;
+    // (loads that pass by the L2 take a microsecond: all heads at once, then everything else at once)
+    static_assert(kSampleMostParts <= kWave, "a lane for each part");
+    {
+        const int lane = tid & (kWave - 1);
+        const bool mine = lane < parts;
+        const unsigned long long h0 = mine ? get_shared(&rx.head[lane * 3]) : pack2(0u, __float_as_uint(kNegInf));
+        const unsigned long long h1 = mine ? get_shared(&rx.head[lane * 3 + 1]) : 0ull, h2 = mine ? get_shared(&rx.head[lane * 3 + 2]) : 0ull;
+        const int m = (int)(uint32_t)h0, incl = wave_scan_incl(m);
+        M = wave_max(__uint_as_float((uint32_t)(h0 >> 32)));
+        count = read_lane(wave_scan_incl((int)h1), kWave - 1);
+        total = wave_sum(__longlong_as_double((long long)h2));
+        const bool over = __ballot(m > rx.cap) != 0ull;                         // (a part's list overflowed: so does the row's)
+        const int all = read_lane(incl, kWave - 1);
+        if (tid < kWave) { sh.part_at[tid] = incl; if (tid == 0) sh.n = over ? kSampleList + 1 : all; }
+        __syncthreads();
+        if (!over) {
+            const int listed = min(all, kSampleList);
+            for (int e0 = 0; e0 < listed; e0 += 4 * kST) {
+                unsigned long long got[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int e = e0 + i * kST + tid;
+                    if (e < listed) {
+                        int pt = 0;
+                        while (sh.part_at[pt] <= e) ++pt;
+                        got[i] = get_shared(&rx.lists[(int64_t)pt * rx.cap + (e - (pt ? sh.part_at[pt - 1] : 0))]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { const int e = e0 + i * kST + tid; if (e < listed) sh.list[e] = got[i]; }
+            }
+        }
+    }
+    if (segs)
+        for (int i = tid; i < rs.n_seg; i += kST) sh.seg[i] = __longlong_as_double((long long)get_shared(&rx.seg[i]));
+    __syncthreads();
+    return true;
+}
+
+// What the counts say: the bins in which the prefix ends, [from, to) down from the reference; by_min_p: min-p cuts above them.  1: found; 0: the prefix ends
+// behind what was counted; -1: nothing that the second pass could use.
+struct Bracket { bool by_min_p; float from, to; };
+__device__ __forceinline__ int bracket(float p, double total, double above_ref, float far, RowShared& sh, Bracket& br)
+{
+    constexpr int PER = kBins / kST;
+    const int tid = threadIdx.x;
+    double mine[PER], sum = 0.0, all;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const unsigned long long h = sh.hist[0][tid * PER + i] + sh.hist[1][tid * PER + i];
+        const double n = (double)(h >> 40), place = (double)(h & ((1ull << 40) - 1)) * 0x1p-20;
+        mine[i] = n > 0.0 ? n * exp2_split(((double)(tid * PER + i) + place / n) * (-kLog2e / (double)kHistPerNat)) : 0.0;
+        if (i == 0 && tid == 0) mine[0] += above_ref;
+        sum += mine[i];
+    }
+    if (tid == 0) { sh.at = INT32_MAX; sh.last = INT32_MAX; }
+    double b = block_scan_excl(sum, sh.red, all);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        b += mine[i];
+        if (b >= (double)p * total * (1.0 - kHistFar)) atomicMin(&sh.at, tid * PER + i);
+        if (b >= (double)p * total * (1.0 + kHistFar)) atomicMin(&sh.last, tid * PER + i);
+    }
+    __syncthreads();
+    const int first = sh.at, last = sh.last;
+    __syncthreads();
+    if (!(total < __builtin_huge_val())) return -1;
+    if ((float)(last + 1) > far || last == INT32_MAX) return far < (float)(kBins - 1) ? 0 : -1;    // (the last bin holds all that is far)
+    br = Bracket{false, (float)first, (float)(last + 1)};
+    return 1;
+}
+
+// The segments' masses of what lies above the bracket, and what lies in it to the list; MIN_P: of what min-p leaves, and no list.
+template <bool BF16, bool MIN_P>
+__device__ __forceinline__ void second_pass(const RowStream<BF16>& rs, int part, int parts, const Bracket& br, float ref, float per, const Weights& w, double a_min, RowShared& sh,
+                                            int& n_above, double& total)
+{
+    constexpr int N = Vec<BF16>::N;
+    const int lane = threadIdx.x & (kWave - 1);
+    const float from = br.from > 0.f ? br.from : kNegInf, to = br.to;
+    int n = 0;
+    double sum_all = 0.0;
+    rs.each([&](int s, const uint4 (&raw)[kSplitStatsNV]) {
+        unsigned mask = 0u;
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < kSplitStatsNV; ++j) {
+            float v[N];
+            rs.values(raw[j], stats_group_first(s, j) + lane, s, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const double x = w.weight(v[e]);
+                bool above;
+                if constexpr (MIN_P) {
+                    above = w.exponent(v[e]) >= a_min;
+                } else {
+                    // (the place of the first pass, but for its ends, which lie outside the bracket; what is not a number lies nowhere)
+                    const float at = (ref - v[e]) * per;
+                    above = at < from;
+                    mask |= at >= from && at < to ? 1u << (j * N + e) : 0u;
+                    sum_all += x;
+                }
+                sum += above ? x : 0.0;
+                n += above;
+                if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (!MIN_P) append<BF16>(rs, s, raw, mask, sh);
+        sum = wave_sum(sum);
+        if (lane == 0) sh.seg[s] = sum;
+    }, part, parts);
+    unsigned long long t;
+    block_scan_excl((unsigned long long)n, sh.redu, t);
+    n_above = (int)t;
+    block_scan_excl(sum_all, sh.red, total);
+    __syncthreads();
+}
+
+// PHASE 0: everything but the second pass of histograms whose rows have several workgroups; 1: those.
+template <bool BF16, int PHASE>
 __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
 {
     __shared__ RowShared sh;
-    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, parts = a.parts, part = blockIdx.x % parts;
+    const int64_t row = blockIdx.x / parts;
     const RowStream<BF16> rs(a.logits, a.ld, row, a.V);
     float T = a.T_rows ? a.T_rows[row] : a.T;
     int k = a.k_rows ? a.k_rows[row] : a.top_k;
     const float p = a.p_rows ? a.p_rows[row] : a.top_p, min_p = a.minp_rows ? a.minp_rows[row] : a.min_p;
     if (!(T > 0.f)) { T = 1.f; k = 1; }                                          // (greedy)
     T = fminf(T, kFloatMax);
+    const bool cut_p = p > 0.f && p < 1.f;
+    if (PHASE == 1 && (k > 0 || !cut_p)) return;
+    const float per = kHistPerNat / T;
+    const double a_min = min_p > 0.f ? log2((double)fminf(min_p, 1.f)) : -__builtin_huge_val();
+
     Weights w;
-    Cut cut;
-    int kept, tok = -1;
-    float M;
-    double total = 0.0;
-    sample_careful<BF16>(rs, T, k, p, min_p, a.V, sh, w, cut, kept, M);
+    Cut cut{kNegInf, -1, a_min};
+    Plan pl;
+    int kept = 0;
+    float M = kNegInf;
+    double total = 0.0, above_ref = 0.0;
+    bool done = false;
+    if (tid == 0) sh.n = 0;
+    if constexpr (PHASE == 0) {
+        if (parts > 1 && tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
+        pl = peek<BF16>(rs, a.V, T, k, p, min_p, sh);
+        w.set(pl.ref, T);
+        if (parts > 1 && cut_p && k <= 0 && part == 0 && tid == 0) {             // (for the second launch)
+            const RowScratch<BF16> rx(a, row);
+            rx.head[parts * 3] = pack2((uint32_t)pl.way, __float_as_uint(pl.ref));
+        }
+        __syncthreads();
+    } else {
+        const unsigned long long h = RowScratch<BF16>(a, row).head[parts * 3];
+        pl = Plan{(Way)(int)(uint32_t)h, __uint_as_float((uint32_t)(h >> 32)), kNegInf, false};
+        if (pl.way != kHist) return;
+        if (tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
+        __syncthreads();
+    }
+    if (pl.way == kCareful && part != 0) return;
+    bool alone = parts == 1;
+    if (pl.way == kSum || pl.way == kList) {
+        if constexpr (PHASE == 0) {
+            if (pl.way == kSum) first_pass<BF16, kSum, false>(rs, part, parts, pl, w, T, sh, M, kept, total, above_ref);
+            else if (pl.total) first_pass<BF16, kList, true>(rs, part, parts, pl, w, T, sh, M, kept, total, above_ref);
+            else first_pass<BF16, kList, false>(rs, part, parts, pl, w, T, sh, M, kept, total, above_ref);
+            if (parts > 1 && !gather<BF16>(rs, RowScratch<BF16>(a, row), part, parts, pl.way == kSum, pl.way == kList, M, kept, total, sh)) return;
+            const bool near = fabs(((double)M - (double)pl.ref) * w.c) < 500.0;   // (+inf: not)
+            if (pl.way == kSum) {
+                done = near;
+            } else if (near && sh.n <= kSampleList) {
+                const int n = sh.n;
+                const double scale = exp2(((double)pl.ref - (double)M) * w.c);   // (the total was summed against the peek's largest)
+                w.set(M, T);
+                unsigned long long last = 0;
+                done = k <= 0 || n >= k || !(pl.least > kNegInf);
+                if (done && k > 0 && k < n) last = select<false>(n, 0ull, (double)k, w, sh);
+                if (done && cut_p) {
+                    const unsigned long long listed = list_sum(n, last, w, sh);
+                    const double target = k > 0 ? (double)p * (double)listed : ldexp((double)p * total * scale, kListShift);
+                    done = target <= (double)listed;
+                    if (done) last = max(last, select<true>(n, last, target, w, sh));
+                }
+                if (done) {
+                    if (last) { cut.t = composite_value(last); cut.id = composite_id(last); }
+                    kept = list_to_segments<BF16>(rs, n, cut, w, false, sh);
+                }
+            }
+            if (!done && near && pl.total) { pl.way = kHist; alone = true; }     // (the peek took a spread row for a peaked one)
+        }
+    }
+    if (pl.way == kHist) {
+        const int at = alone ? 0 : part, of = alone ? 1 : parts;
+        bool good = true;
+        if constexpr (PHASE == 0) {
+            w.set(pl.ref, T);
+            __syncthreads();
+            if (!alone) pl.far = (float)(kBins - 1);                             // (there is no third pass)
+            for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
+            __syncthreads();
+            first_pass<BF16, kHist, false>(rs, at, of, pl, w, T, sh, M, kept, total, above_ref);
+            if (!alone) {                                                      // (the second launch goes on)
+                const RowScratch<BF16> rx(a, row);
+                for (int i = tid; i < kBins; i += kST) rx.hist[(int64_t)part * kBins + i] = sh.hist[0][i] + sh.hist[1][i];
+                if (tid == 0) {
+                    rx.head[part * 3] = pack2(0u, __float_as_uint(M));
+                    rx.totals[part] = make_double2(total, above_ref);
+                }
+                return;
+            }
+        } else {
+            const RowScratch<BF16> rx(a, row);
+            unsigned long long sums[kBins / kST] = {};
+            for (int j = 0; j < parts; ++j)
+#pragma unroll
+                for (int i = 0; i < kBins / kST; ++i) sums[i] += rx.hist[(int64_t)j * kBins + i * kST + tid];
+#pragma unroll
+            for (int i = 0; i < kBins / kST; ++i) { sh.hist[0][i * kST + tid] = sums[i]; sh.hist[1][i * kST + tid] = 0ull; }
+            const int lane = tid & (kWave - 1);
+            M = wave_max(lane < parts ? __uint_as_float((uint32_t)(rx.head[lane * 3] >> 32)) : kNegInf);
+            const double2 t = lane < parts ? rx.totals[lane] : make_double2(0.0, 0.0);
+            total = wave_sum(t.x);
+            above_ref = wave_sum(t.y);
+            pl.far = (float)(kBins - 1);
+            __syncthreads();
+        }
+        Bracket br;
+        int found = M <= kFloatMax ? bracket(p, total, above_ref, pl.far, sh, br) : -1;
+        if constexpr (PHASE == 0) {
+            if (found == 0) {
+                pl.far = (float)(kBins - 1);
+                for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
+                __syncthreads();
+                first_pass<BF16, kHist, false>(rs, 0, 1, pl, w, T, sh, M, kept, total, above_ref);
+                found = bracket(p, total, above_ref, pl.far, sh, br);
+            }
+        }
+        good = found > 0;
+        if (good && a_min > -__builtin_huge_val()) {
+            // (min-p against where top-p ends: clearly above, clearly not, or the careful way)
+            const double x = ((double)pl.ref - ((double)M + a_min / kLog2e * (double)T)) * (double)per;
+            br.by_min_p = x < (double)br.from - 1.0;
+            good = br.by_min_p || x > (double)br.to + 1.0;
+        }
+        if (!good && at != 0) return;                                            // (all parts see the same)
+        if (good) {
+            w.set(M, T);
+            if (tid == 0) sh.n = 0;
+            __syncthreads();
+            if (br.by_min_p) second_pass<BF16, true>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
+            else second_pass<BF16, false>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
+            if (!alone && !gather<BF16>(rs, RowScratch<BF16>(a, row), part, parts, true, true, M, kept, total, sh)) return;
+            if (br.by_min_p) {
+                done = true;
+            } else if (sh.n <= kSampleList) {
+                const int n = sh.n;
+                double above = 0.0, mine = 0.0;
+                for (int i = tid * kSegsPer; i < min((tid + 1) * kSegsPer, rs.n_seg); ++i) mine += sh.seg[i];
+                block_scan_excl(mine, sh.red, above);
+                const double target = ldexp((double)p * total - above, kListShift);
+                const unsigned long long listed = list_sum(n, 0ull, w, sh);
+                done = target > 0.0 && target <= (double)listed;
+                if (done) {
+                    const unsigned long long last = select<true>(n, 0ull, target, w, sh);
+                    cut = Cut{composite_value(last), composite_id(last), -__builtin_huge_val()};
+                    kept += list_to_segments<BF16>(rs, n, cut, w, true, sh);
+                }
+            }
+        }
+    }
+    if (!done) {
+        __syncthreads();
+        Weights w2;                                                              // (what a call takes by reference lives in memory)
+        Cut cut2;
+        int kept2;
+        float M2;
+        sample_careful<BF16>(a.logits, a.ld, row, T, k, p, min_p, a.V, sh, w2, cut2, kept2, M2);
+        w = w2;
+        cut = cut2;
+        kept = kept2;
+        M = M2;
+    }
+    int tok = -1;
+    total = 0.0;
     if (M > kNegInf) draw<BF16>(rs, w, cut, a.u[row], sh, tok, total);
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
         a.tok[row] = tok;
         a.prob[row] = tok < 0 ? 0.f : (float)(w.weight(cleaned(logit_at<BF16>(a.logits, a.ld, row, tok))) / total);
         a.count[row] = kept;
@@ -447,17 +1068,27 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     }
 }
 
+template <bool BF16>
+hipError_t launch(const SampleArgs& a, int64_t rows, bool hist, hipStream_t stream)
+{
+    hipLaunchKernelGGL((sample_kernel<BF16, 0>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
+    if (a.parts > 1 && hist) hipLaunchKernelGGL((sample_kernel<BF16, 1>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_sample(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature, int top_k, float top_p, float min_p,
                          const float* temperature_rows, const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows,
-                         const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse, hipStream_t stream)
+                         const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse, void* scratch, size_t scratch_bytes, hipStream_t stream)
 {
     if (n_rows == 0) return hipSuccess;
-    const SampleArgs a{logits, ld, V, temperature, top_k, top_p, min_p, temperature_rows, top_k_rows, top_p_rows, min_p_rows, uniforms, tok, prob, count, lse};
-    if (dtype == 1) hipLaunchKernelGGL((sample_kernel<true>), dim3((unsigned)n_rows), dim3(kST), 0, stream, a);
-    else hipLaunchKernelGGL((sample_kernel<false>), dim3((unsigned)n_rows), dim3(kST), 0, stream, a);
-    return hipGetLastError();
+    const int parts = scratch && scratch_bytes >= sample_scratch_bytes(dtype, n_rows, V) ? sample_parts(dtype, n_rows, V) : 1;
+    const SampleArgs a{logits, ld, V, temperature, top_k, top_p, min_p, temperature_rows, top_k_rows, top_p_rows, min_p_rows, uniforms, tok, prob, count, lse,
+                       (char*)scratch, parts};
+    const bool greedy = !temperature_rows && temperature == 0.f;
+    const bool hist = !greedy && (top_p_rows || (top_p > 0.f && top_p < 1.f)) && (top_k_rows || top_k <= 0);   // (may a row take two passes?)
+    return dtype == 1 ? launch<true>(a, n_rows, hist, stream) : launch<false>(a, n_rows, hist, stream);
 }
 
 }  // namespace picospec
