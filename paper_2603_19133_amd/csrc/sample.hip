@@ -51,7 +51,8 @@ struct Weights {
         p = fma(p, f, 0x1.c6b08defc25fdp-5);
         p = fma(p, f, 0x1.ebfbdff7c5a79p-3);
         p = fma(p, f, 0x1.62e42fef7a78bp-1);
-        return ldexp(fma(p, f, 1.0), (int)__double2loint(t));
+        p = fma(p, f, 1.0);
+        return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));     // (from 2^-1000 to 2^1000: no subnormal)
     }
 };
 
@@ -279,6 +280,36 @@ __device__ __forceinline__ int crossing(const T* bins, unsigned long long& above
     return at;
 }
 
+// The id of the `ties`-th element that equals t, from how many the segments have of it (kBins counts, cleared behind the row).
+template <bool BF16>
+__device__ __forceinline__ int id_of_tie(const RowStream<BF16>& rs, const uint32_t* per_segment, float t, unsigned long long ties, RowShared& sh)
+{
+    constexpr int N = Vec<BF16>::N;
+    static_assert(kSegs <= kBins, "a count for every segment");
+    const int tid = threadIdx.x;
+    unsigned long long above = 0;
+    const int s = crossing<kBins>(per_segment, above, (double)ties, sh);
+    if (tid == 0) sh.at = INT32_MAX;
+    __syncthreads();
+    if (s >= 0) {
+        const int q = s * (64 * kSplitStatsNV) + tid;
+        const bool have = tid < 64 * kSplitStatsNV;
+        float v[N];
+        rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, s, v);
+        unsigned long long mine = 0, all;
+#pragma unroll
+        for (int e = 0; e < N; ++e) mine += have && cleaned(v[e]) == t;
+        unsigned long long b = above + block_scan_excl(mine, sh.redu, all);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (have && cleaned(v[e]) == t && ++b == ties) sh.at = rs.first_id(q) + e;
+    }
+    __syncthreads();
+    const int id = sh.at;
+    __syncthreads();
+    return id;
+}
+
 template <bool BF16>
 __device__ __attribute__((noinline)) void sample_careful(const void* logits, int64_t ld, int64_t row, float T, int k, float p, float min_p, int V,
                                                RowShared& sh, Weights& w, Cut& cut, int& kept, float& M)
@@ -388,27 +419,7 @@ __device__ __attribute__((noinline)) void sample_careful(const void* logits, int
         clear();
         rs.each_value([&](float z, int, int s) { if (z == cut.t) atomicAdd(&sh.row.count[s], 1u); });
         __syncthreads();
-        unsigned long long above = 0;
-        const int s = crossing<kBins>(sh.row.count, above, (double)ties, sh);
-        if (tid == 0) sh.at = INT32_MAX;
-        __syncthreads();
-        if (s >= 0) {
-            constexpr int N = Vec<BF16>::N;
-            const int q = s * (64 * kSplitStatsNV) + tid;
-            const bool have = tid < 64 * kSplitStatsNV;
-            float v[N];
-            rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, s, v);
-            unsigned long long mine = 0, all;
-#pragma unroll
-            for (int e = 0; e < N; ++e) mine += have && cleaned(v[e]) == cut.t;
-            unsigned long long b = above + block_scan_excl(mine, sh.redu, all);
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (have && cleaned(v[e]) == cut.t && ++b == ties) sh.at = rs.first_id(q) + e;
-        }
-        __syncthreads();
-        cut.id = sh.at;
-        __syncthreads();
+        cut.id = id_of_tie<BF16>(rs, sh.row.count, cut.t, ties, sh);
     }
     // the segments' kept masses
     unsigned mine = 0;
@@ -539,6 +550,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
     // (without the peek's largest: one that is by chance among the row's few that hold much of it says nothing of the rest)
     if (a_all - 1.0 >= ((double)p + 0.3 * (1.0 - (double)p)) * (t_all - 1.0)) return pl;
     pl.way = kHist;
+    if constexpr (BF16) return pl;                                               // (count_values, or several workgroups: neither leaves any out)
     // bins behind which the peek has less than 1 / 1.15 of what top-p leaves out
     float near = 0.f, far = (float)(kBins - 1);
     for (int i = 0; i < 7; ++i) {
@@ -559,7 +571,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
 
 // Appends the elements of a segment whose bit is set (bit j * N + e) to the list.  sh.n counts on behind the list's end.
 template <bool BF16>
-__device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, const uint4 (&raw)[kSplitStatsNV], unsigned mask, RowShared& sh)
+__device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, const uint4 (&raw)[kSplitStatsNV], unsigned mask, RowShared& sh, int cap = kSampleList)
 {
     constexpr int N = Vec<BF16>::N;
     if (!__ballot(mask != 0u)) return;
@@ -578,7 +590,7 @@ __device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, const u
 #pragma unroll
         for (int e = 0; e < N; ++e)
             if ((mask >> (j * N + e)) & 1u) {
-                if (at < kSampleList) sh.list[at] = composite_of(__float_as_uint(v[e]), (uint32_t)(x + e));
+                if (at < cap) sh.list[at] = composite_of(__float_as_uint(v[e]), (uint32_t)(x + e));
                 ++at;
             }
     }
@@ -598,7 +610,7 @@ __device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, 
     const int lane = threadIdx.x & (kWave - 1);
     const float c = (float)w.c, per = kHistPerNat / T;
     float mx = kNegInf;
-    int n = 0;
+    int n = 0;                                                                   // (of the wave)
     double sum_all = 0.0, sum_over = 0.0;
     rs.each([&](int s, const uint4 (&raw)[kSplitStatsNV]) {
         unsigned mask = 0u;
@@ -612,7 +624,7 @@ __device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, 
             for (int e = 0; e < N; ++e) {
                 mx = fmaxf(mx, v[e]);
                 if constexpr (WAY == kSum || TOTAL) sum += w.weight(v[e]);
-                if constexpr (WAY == kSum) n += v[e] > kNegInf;
+                if constexpr (WAY == kSum) n += __builtin_popcountll(__ballot(v[e] >= -kFloatMax));
                 if constexpr (WAY == kList) mask |= (v[e] >= pl.least && v[e] > kNegInf) ? 1u << (j * N + e) : 0u;
                 if constexpr (WAY == kHist) {
                     const float z = fmaxf(v[e], kNegInf), x = fminf(fmaxf((pl.ref - z) * per, 0.f), (float)(kBins - 1));
@@ -639,7 +651,7 @@ __device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, 
     M = block_max(mx, sh);
     n_finite = 0;
     total = 0.0;
-    if constexpr (WAY == kSum) { unsigned long long t; block_scan_excl((unsigned long long)n, sh.redu, t); n_finite = (int)t; }
+    if constexpr (WAY == kSum) { unsigned long long t; block_scan_excl((unsigned long long)(lane == 0 ? n : 0), sh.redu, t); n_finite = (int)t; }
     if constexpr (TOTAL || WAY == kHist) block_scan_excl(sum_all, sh.red, total);
     if constexpr (WAY == kHist) block_scan_excl(sum_over, sh.red, above_ref);
     __syncthreads();
@@ -892,6 +904,159 @@ __device__ __forceinline__ void second_pass(const RowStream<BF16>& rs, int part,
     __syncthreads();
 }
 
+// bf16 rows of one workgroup, top-p alone: the values themselves are counted.  A window of 14 octaves of magnitude, up to the one that holds the peek's largest
+// and what lies 50 T below it, has 1792 values of either sign; what is smaller lies between the two signs' and goes to the list; what lies below
+// weighs less than e^-50 and is passed over.  Counts times weights are the row's exact masses, so the prefix's end is known after one pass without an exponential
+// per element, and the second one looks weights up: 160 -> 75 us for 512 rows of 152,064 (the two passes of the histogram with fp64 weights).
+constexpr int kWindow = 14 * 128, kValues = 2 * kWindow + 1, kValuesPer = (kValues + kST - 1) / kST;
+constexpr int kSmallList = kSampleList - kValues;                               // (the counts, two copies, and then the weights, lie behind the list)
+__device__ __forceinline__ int window_base(float ref, float T)
+{
+    const float x = fmaxf(fabsf(ref), fabsf(ref - 50.f * T));
+    const int e = (int)(__float_as_uint(x) >> 23);
+    return e <= 252 ? max(e - 13, 1) << 7 : -1;                                 // -1: no such window
+}
+// where a value lies in the order: 0 .. 2 kWindow; kWindow: the small ones; outside: not in the window
+__device__ __forceinline__ int value_bin(float z, int base, bool& counted)
+{
+    const int bits = (int)__float_as_uint(z), d = min(max((int)(((unsigned)bits >> 16) & 0x7FFFu) - (base - 1), 0), kWindow + 1);
+    const int sign = ~(bits >> 31);
+    counted = d <= kWindow;
+    return kWindow + ((d ^ sign) - sign);
+}
+__device__ __forceinline__ float value_of_bin(int bin, int base)
+{
+    const int d = bin - kWindow;
+    return __uint_as_float((unsigned)(d < 0 ? (base - 1 - d) << 16 : ((base - 1 + d) << 16) | 0x80000000));
+}
+
+__device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Plan& pl, float T, float p, double a_min, Weights& w, Cut& cut, int& kept, float& M, RowShared& sh)
+{
+    constexpr int N = 8;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), base = window_base(pl.ref, T);
+    if (base < 0) return false;
+    double* const weight = reinterpret_cast<double*>(&sh.list[kSmallList]);
+    uint32_t* const counts = reinterpret_cast<uint32_t*>(weight);
+    for (int i = tid; i < 2 * kValues; i += kST) counts[i] = 0u;
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    uint32_t* const mine = counts + (lane & 1) * kValues;
+    float mx = kNegInf;
+    rs.each([&](int s, const uint4 (&raw)[kSplitStatsNV]) {
+        unsigned mask = 0u;
+#pragma unroll
+        for (int j = 0; j < kSplitStatsNV; ++j) {
+            float v[N];
+            rs.values(raw[j], stats_group_first(s, j) + lane, s, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                bool counted;
+                const int bin = value_bin(v[e], base, counted);
+                mx = fmaxf(mx, v[e]);
+                mask |= bin == kWindow ? 1u << (j * N + e) : 0u;
+                if (counted) atomicAdd(&mine[bin], 1u);
+            }
+        }
+        append<true>(rs, s, raw, mask, sh, kSmallList);
+    });
+    M = block_max(mx, sh);
+    const int n_small = sh.n;
+    if (!(M > kNegInf) || n_small > kSmallList || (M > 0.f && (int)(__float_as_uint(M) >> 16) >= base + kWindow)) return false;
+    w.set(M, T);
+    const double small = ldexp((double)list_sum(n_small, 0ull, w, sh), -kListShift);
+    // masses in order; the first bin with which they reach the target
+    uint32_t n[kValuesPer];
+    double one[kValuesPer], sum = 0.0, total;
+#pragma unroll
+    for (int i = 0; i < kValuesPer; ++i) {
+        const int bin = tid * kValuesPer + i;
+        n[i] = bin < kValues ? counts[bin] + counts[kValues + bin] : 0u;
+        one[i] = n[i] && bin != kWindow ? w.weight(value_of_bin(bin, base)) : 0.0;
+        sum += bin == kWindow ? small : (double)n[i] * one[i];
+    }
+    if (tid == 0) sh.at = INT32_MAX;
+    double b = block_scan_excl(sum, sh.red, total), b_hit = 0.0;
+    const double target = (double)p * total;
+    int hit = INT32_MAX, n_hit = 0;
+#pragma unroll
+    for (int i = 0; i < kValuesPer; ++i) {
+        const int bin = tid * kValuesPer + i;
+        const double next = b + (bin == kWindow ? small : (double)n[i] * one[i]);
+        if (n[i] && next >= target && hit == INT32_MAX) { hit = bin; b_hit = b; n_hit = (int)n[i]; atomicMin(&sh.at, bin); }
+        b = next;
+    }
+    __syncthreads();
+    const int last = sh.at;
+    if (last == INT32_MAX) return false;                                         // (uniform)
+    if (hit == last) { sh.red[kSW] = b_hit; sh.last = n_hit; }
+    __syncthreads();
+    const double rest = target - sh.red[kSW];
+    const float t = value_of_bin(last, base);
+    const double w_t = w.weight(t);
+    int ties = 0;
+    cut = Cut{t, INT32_MAX, a_min};
+    if (last != kWindow) {
+        const double need = ceil(rest / w_t);
+        ties = need >= (double)sh.last ? sh.last : need < 1.0 ? 1 : (int)need;
+        if (w.exponent(t) < a_min) ties = 0;
+    }
+    __syncthreads();
+    if (last == kWindow) {
+        const unsigned long long c = select<true>(n_small, 0ull, ldexp(rest, kListShift), w, sh);
+        if (!c) return false;
+        cut.t = composite_value(c);
+        cut.id = composite_id(c);
+    }
+    unsigned long long mine_kept = 0, all_kept;
+#pragma unroll
+    for (int i = 0; i < kValuesPer; ++i) {
+        const int bin = tid * kValuesPer + i;
+        const bool keep = bin < last && bin != kWindow && n[i] && w.exponent(value_of_bin(bin, base)) >= a_min;
+        if (keep) mine_kept += n[i];
+        if (bin < kValues) weight[bin] = keep ? one[i] : 0.0;                    // (the counts are in registers: list_sum and the scan lie between)
+    }
+    uint32_t* const tied = reinterpret_cast<uint32_t*>(sh.mass);                 // per segment
+    static_assert(sizeof(sh.mass) >= kBins * sizeof(uint32_t), "counts for id_of_tie");
+    for (int i = tid; i < kBins; i += kST) tied[i] = 0u;
+    block_scan_excl(mine_kept, sh.redu, all_kept);
+    kept = (int)all_kept + ties;
+    rs.each([&](int s, const uint4 (&raw)[kSplitStatsNV]) {
+        double seg = 0.0;
+        int eq = 0;
+#pragma unroll
+        for (int j = 0; j < kSplitStatsNV; ++j) {
+            float v[N];
+            rs.values(raw[j], stats_group_first(s, j) + lane, s, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                bool counted;
+                const int bin = value_bin(v[e], base, counted);
+                if (counted && bin < last) seg += weight[bin];
+                eq += __builtin_popcountll(__ballot(bin == last));
+            }
+        }
+        seg = wave_sum(seg);
+        if (lane == 0) { sh.seg[s] = seg; tied[s] = (uint32_t)eq; }
+    });
+    __syncthreads();
+    if (ties > 0) {
+        // the first `ties` of them by id
+        unsigned long long c[kSegsPer], own = 0, all;
+#pragma unroll
+        for (int i = 0; i < kSegsPer; ++i) { const int s = tid * kSegsPer + i; c[i] = s < rs.n_seg ? tied[s] : 0u; own += c[i]; }
+        unsigned long long before = block_scan_excl(own, sh.redu, all);
+#pragma unroll
+        for (int i = 0; i < kSegsPer; ++i) {
+            const int s = tid * kSegsPer + i;
+            if (s < rs.n_seg && before < (unsigned long long)ties) sh.seg[s] += w_t * (double)min(c[i], (unsigned long long)ties - before);
+            before += c[i];
+        }
+        cut.id = id_of_tie<true>(rs, tied, t, (unsigned long long)ties, sh);
+    }
+    if (n_small > 0 && last >= kWindow) kept += list_to_segments<true>(rs, n_small, cut, w, true, sh);
+    return true;
+}
+
 // PHASE 0: everything but the second pass of histograms whose rows have several workgroups; 1: those.
 template <bool BF16, int PHASE>
 __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
@@ -966,9 +1131,13 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
             if (!done && near && pl.total) { pl.way = kHist; alone = true; }     // (the peek took a spread row for a peaked one)
         }
     }
-    if (pl.way == kHist) {
+    constexpr bool COUNTS = PHASE == 0 && BF16;                                  // (then the histogram's second pass is the second launch's)
+    if constexpr (COUNTS) {
+        __syncthreads();
+        if (pl.way == kHist && alone) done = count_values(rs, pl, T, p, a_min, w, cut, kept, M, sh);
+    }
+    if (pl.way == kHist && !(COUNTS && alone)) {
         const int at = alone ? 0 : part, of = alone ? 1 : parts;
-        bool good = true;
         if constexpr (PHASE == 0) {
             w.set(pl.ref, T);
             __syncthreads();
@@ -976,7 +1145,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
             for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
             __syncthreads();
             first_pass<BF16, kHist, false>(rs, at, of, pl, w, T, sh, M, kept, total, above_ref);
-            if (!alone) {                                                      // (the second launch goes on)
+            if (COUNTS || !alone) {                                            // (the second launch goes on)
                 const RowScratch<BF16> rx(a, row);
                 for (int i = tid; i < kBins; i += kST) rx.hist[(int64_t)part * kBins + i] = sh.hist[0][i] + sh.hist[1][i];
                 if (tid == 0) {
@@ -1001,46 +1170,48 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
             pl.far = (float)(kBins - 1);
             __syncthreads();
         }
-        Bracket br;
-        int found = M <= kFloatMax ? bracket(p, total, above_ref, pl.far, sh, br) : -1;
-        if constexpr (PHASE == 0) {
-            if (found == 0) {
-                pl.far = (float)(kBins - 1);
-                for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
-                __syncthreads();
-                first_pass<BF16, kHist, false>(rs, 0, 1, pl, w, T, sh, M, kept, total, above_ref);
-                found = bracket(p, total, above_ref, pl.far, sh, br);
+        if constexpr (!COUNTS) {
+            Bracket br;
+            int found = M <= kFloatMax ? bracket(p, total, above_ref, pl.far, sh, br) : -1;
+            if constexpr (PHASE == 0) {
+                if (found == 0) {
+                    pl.far = (float)(kBins - 1);
+                    for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
+                    __syncthreads();
+                    first_pass<BF16, kHist, false>(rs, 0, 1, pl, w, T, sh, M, kept, total, above_ref);
+                    found = bracket(p, total, above_ref, pl.far, sh, br);
+                }
             }
-        }
-        good = found > 0;
-        if (good && a_min > -__builtin_huge_val()) {
-            // (min-p against where top-p ends: clearly above, clearly not, or the careful way)
-            const double x = ((double)pl.ref - ((double)M + a_min / kLog2e * (double)T)) * (double)per;
-            br.by_min_p = x < (double)br.from - 1.0;
-            good = br.by_min_p || x > (double)br.to + 1.0;
-        }
-        if (!good && at != 0) return;                                            // (all parts see the same)
-        if (good) {
-            w.set(M, T);
-            if (tid == 0) sh.n = 0;
-            __syncthreads();
-            if (br.by_min_p) second_pass<BF16, true>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
-            else second_pass<BF16, false>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
-            if (!alone && !gather<BF16>(rs, RowScratch<BF16>(a, row), part, parts, true, true, M, kept, total, sh)) return;
-            if (br.by_min_p) {
-                done = true;
-            } else if (sh.n <= kSampleList) {
-                const int n = sh.n;
-                double above = 0.0, mine = 0.0;
-                for (int i = tid * kSegsPer; i < min((tid + 1) * kSegsPer, rs.n_seg); ++i) mine += sh.seg[i];
-                block_scan_excl(mine, sh.red, above);
-                const double target = ldexp((double)p * total - above, kListShift);
-                const unsigned long long listed = list_sum(n, 0ull, w, sh);
-                done = target > 0.0 && target <= (double)listed;
-                if (done) {
-                    const unsigned long long last = select<true>(n, 0ull, target, w, sh);
-                    cut = Cut{composite_value(last), composite_id(last), -__builtin_huge_val()};
-                    kept += list_to_segments<BF16>(rs, n, cut, w, true, sh);
+            bool good = found > 0;
+            if (good && a_min > -__builtin_huge_val()) {
+                // (min-p against where top-p ends: clearly above, clearly not, or the careful way)
+                const double x = ((double)pl.ref - ((double)M + a_min / kLog2e * (double)T)) * (double)per;
+                br.by_min_p = x < (double)br.from - 1.0;
+                good = br.by_min_p || x > (double)br.to + 1.0;
+            }
+            if (!good && at != 0) return;                                            // (all parts see the same)
+            if (good) {
+                w.set(M, T);
+                if (tid == 0) sh.n = 0;
+                __syncthreads();
+                if (br.by_min_p) second_pass<BF16, true>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
+                else second_pass<BF16, false>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
+                if (!alone && !gather<BF16>(rs, RowScratch<BF16>(a, row), part, parts, true, true, M, kept, total, sh)) return;
+                if (br.by_min_p) {
+                    done = true;
+                } else if (sh.n <= kSampleList) {
+                    const int n = sh.n;
+                    double above = 0.0, mine = 0.0;
+                    for (int i = tid * kSegsPer; i < min((tid + 1) * kSegsPer, rs.n_seg); ++i) mine += sh.seg[i];
+                    block_scan_excl(mine, sh.red, above);
+                    const double target = ldexp((double)p * total - above, kListShift);
+                    const unsigned long long listed = list_sum(n, 0ull, w, sh);
+                    done = target > 0.0 && target <= (double)listed;
+                    if (done) {
+                        const unsigned long long last = select<true>(n, 0ull, target, w, sh);
+                        cut = Cut{composite_value(last), composite_id(last), -__builtin_huge_val()};
+                        kept += list_to_segments<BF16>(rs, n, cut, w, true, sh);
+                    }
                 }
             }
         }
