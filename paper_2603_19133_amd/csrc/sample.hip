@@ -469,7 +469,7 @@ constexpr float kHistPerNat = 64.f;
 struct Plan { Way way; float ref, least; bool total; float far; };
 
 template <bool BF16>
-__device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, int k, float p, float min_p, RowShared& sh)
+__device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, int k, float p, float min_p, bool alone, RowShared& sh)
 {
     constexpr int N = Vec<BF16>::N, PER = kPeek / (kST * N);                    // vectors a thread
     constexpr int BLOCKS = PER * kSW;
@@ -501,6 +501,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
         pl.least = float_below(float_below((float)((double)ref + (double)T * log((double)fminf(min_p, 1.f)))));
         return pl;
     }
+    if (BF16 && alone && k <= 0) { pl.way = kHist; return pl; }                  // (values are counted whether the mass is spread or not)
     const int want = k > 0 ? k : kTopPList;
     const int rank = want <= kSampleList ? optimistic_rank(want, V, min(kPeek, V), kSampleList) : 0;
     if (rank == 0) {
@@ -571,7 +572,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
 
 // Appends the elements of a segment whose bit is set (bit j * N + e) to the list.  sh.n counts on behind the list's end.
 template <bool BF16>
-__device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, const uint4 (&raw)[kSplitStatsNV], unsigned mask, RowShared& sh, int cap = kSampleList)
+__device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, unsigned mask, RowShared& sh, int cap = kSampleList)
 {
     constexpr int N = Vec<BF16>::N;
     if (!__ballot(mask != 0u)) return;
@@ -580,19 +581,11 @@ __device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, const u
     int base = 0;
     if (lane == 0) base = atomicAdd(&sh.n, total);
     int at = read_lane(base, 0) + incl - mine;
-#pragma unroll
-    for (int j = 0; j < kSplitStatsNV; ++j) {
-        uint4 again = raw[j];                                                   // (unpacked a second time: the values are not held for it)
-        asm volatile("" : "+v"(again.x), "+v"(again.y), "+v"(again.z), "+v"(again.w));
-        float v[N];
-        unpack<BF16>(again, v);
-        const int x = rs.first_id(stats_group_first(s, j) + lane);
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if ((mask >> (j * N + e)) & 1u) {
-                if (at < cap) sh.list[at] = composite_of(__float_as_uint(v[e]), (uint32_t)(x + e));
-                ++at;
-            }
+    // (few lanes have any, and they read theirs again, from the caches: 36 instructions for a segment's 340 with a test for every element in registers)
+    for (unsigned left = mask; left; left &= left - 1u, ++at) {
+        const int bit = __builtin_ctz(left), v = (stats_group_first(s, bit / N) + lane) * N + bit % N;      // (element of the row's vectors: inside the row, or its bit were not set)
+        const uint32_t bits = BF16 ? (uint32_t)reinterpret_cast<const uint16_t*>(rs.rv.base)[v] << 16 : reinterpret_cast<const uint32_t*>(rs.rv.base)[v];
+        if (at < cap) sh.list[at] = composite_of(bits, (uint32_t)(v - rs.rv.o));
     }
 }
 
@@ -640,7 +633,7 @@ __device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, 
             }
             __builtin_amdgcn_sched_barrier(0);                                  // (a vector's exponentials side by side, not the segment's: registers)
         }
-        if constexpr (WAY == kList) append<BF16>(rs, s, raw, mask, sh);
+        if constexpr (WAY == kList) append<BF16>(rs, s, mask, sh);
         if constexpr (WAY == kSum) {
             sum = wave_sum(sum);
             if (lane == 0) sh.seg[s] = sum;
@@ -893,7 +886,7 @@ __device__ __forceinline__ void second_pass(const RowStream<BF16>& rs, int part,
                 if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if constexpr (!MIN_P) append<BF16>(rs, s, raw, mask, sh);
+        if constexpr (!MIN_P) append<BF16>(rs, s, mask, sh);
         sum = wave_sum(sum);
         if (lane == 0) sh.seg[s] = sum;
     }, part, parts);
@@ -904,35 +897,54 @@ __device__ __forceinline__ void second_pass(const RowStream<BF16>& rs, int part,
     __syncthreads();
 }
 
-// bf16 rows of one workgroup, top-p alone: the values themselves are counted.  A window of 14 octaves of magnitude, up to the one that holds the peek's largest
-// and what lies 50 T below it, has 1792 values of either sign; what is smaller lies between the two signs' and goes to the list; what lies below
-// weighs less than e^-50 and is passed over.  Counts times weights are the row's exact masses, so the prefix's end is known after one pass without an exponential
-// per element, and the second one looks weights up: 160 -> 75 us for 512 rows of 152,064 (the two passes of the histogram with fp64 weights).
-constexpr int kWindow = 14 * 128, kValues = 2 * kWindow + 1, kValuesPer = (kValues + kST - 1) / kST;
+// bf16 rows of one workgroup, top-p alone: the values themselves are counted.  A window of 16 octaves of magnitude less eight values, up to the end of the one that
+// holds the peek's largest and what lies 50 T below it, has kWindow values of either sign; what is smaller lies between the two signs' and goes to the list; what lies
+// below weighs less than e^-50 and is passed over.  Counts times weights are the row's exact masses, so the prefix's end is known after one pass without an
+// exponential, and the second one looks weights up.  Elements are taken two at a time, as 16-bit integers.
+constexpr int kWindow = 16 * 128 - 8, kValues = 2 * kWindow + 1, kValuesPer = (kValues + kST - 1) / kST;
+static_assert(kValuesPer == 8, "all but a few of the threads' places hold a value");
 constexpr int kSmallList = kSampleList - kValues;                               // (the counts, two copies, and then the weights, lie behind the list)
+typedef short short2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+
+// 16-bit magnitude in front of the window's first: -1: no such window
 __device__ __forceinline__ int window_base(float ref, float T)
 {
     const float x = fmaxf(fabsf(ref), fabsf(ref - 50.f * T));
     const int e = (int)(__float_as_uint(x) >> 23);
-    return e <= 252 ? max(e - 13, 1) << 7 : -1;                                 // -1: no such window
+    return e <= 252 ? max(((e + 1) << 7) - kWindow, 128) - 1 : -1;
 }
-// where a value lies in the order: 0 .. 2 kWindow; kWindow: the small ones; outside: not in the window
-__device__ __forceinline__ int value_bin(float z, int base, bool& counted)
+// Where values lie in the order: -kWindow .. kWindow from the largest down, 0: the small ones; kWindow + 1 of either sign: outside
+__device__ __forceinline__ void value_places(const RowStream<true>& rs, const uint4& raw, int q, int s, int base, short2_t (&at)[4])
 {
-    const int bits = (int)__float_as_uint(z), d = min(max((int)(((unsigned)bits >> 16) & 0x7FFFu) - (base - 1), 0), kWindow + 1);
-    const int sign = ~(bits >> 31);
-    counted = d <= kWindow;
-    return kWindow + ((d ^ sign) - sign);
+    uint32_t word[4] = {raw.x, raw.y, raw.z, raw.w};
+    if (s == 0 || s >= rs.n_seg - 1) {                                           // (outside the row: -inf)
+        const unsigned vm = vec_valid_mask<true>(rs.rv, q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!((vm >> (2 * i)) & 1u)) word[i] = (word[i] & 0xFFFF0000u) | 0xFF80u;
+            if (!((vm >> (2 * i + 1)) & 1u)) word[i] = (word[i] & 0xFFFFu) | 0xFF800000u;
+        }
+    }
+    const ushort2_t base2 = {(unsigned short)base, (unsigned short)base}, far = {kWindow + 1, kWindow + 1};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t mag = word[i] & 0x7FFF7FFFu;
+        ushort2_t d, w;
+        __builtin_memcpy(&d, &mag, 4);
+        __builtin_memcpy(&w, &word[i], 4);
+        d = __builtin_elementwise_min(__builtin_elementwise_sub_sat(d, base2), far);
+        const short2_t positive = ~((short2_t)w >> 15);                          // -1 or 0
+        at[i] = ((short2_t)d ^ positive) - positive;
+    }
 }
-__device__ __forceinline__ float value_of_bin(int bin, int base)
+__device__ __forceinline__ float value_at(int place, int base)
 {
-    const int d = bin - kWindow;
-    return __uint_as_float((unsigned)(d < 0 ? (base - 1 - d) << 16 : ((base - 1 + d) << 16) | 0x80000000));
+    return __uint_as_float(place < 0 ? (unsigned)(base - place) << 16 : ((unsigned)(base + place) << 16) | 0x80000000u);
 }
 
 __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Plan& pl, float T, float p, double a_min, Weights& w, Cut& cut, int& kept, float& M, RowShared& sh)
 {
-    constexpr int N = 8;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), base = window_base(pl.ref, T);
     if (base < 0) return false;
     double* const weight = reinterpret_cast<double*>(&sh.list[kSmallList]);
@@ -941,27 +953,40 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
     if (tid == 0) sh.n = 0;
     __syncthreads();
     uint32_t* const mine = counts + (lane & 1) * kValues;
-    float mx = kNegInf;
+    short2_t first = {kWindow + 1, kWindow + 1};
     rs.each([&](int s, const uint4 (&raw)[kSplitStatsNV]) {
         unsigned mask = 0u;
 #pragma unroll
         for (int j = 0; j < kSplitStatsNV; ++j) {
-            float v[N];
-            rs.values(raw[j], stats_group_first(s, j) + lane, s, v);
+            short2_t at[4];
+            value_places(rs, raw[j], stats_group_first(s, j) + lane, s, base, at);
+            ushort2_t least = {0xFFFF, 0xFFFF};                                  // (of the magnitudes: 0 where one is small)
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                bool counted;
-                const int bin = value_bin(v[e], base, counted);
-                mx = fmaxf(mx, v[e]);
-                mask |= bin == kWindow ? 1u << (j * N + e) : 0u;
-                if (counted) atomicAdd(&mine[bin], 1u);
+            for (int i = 0; i < 4; ++i) {
+                first = __builtin_elementwise_min(first, at[i]);
+                least = __builtin_elementwise_min(least, (ushort2_t)__builtin_elementwise_abs(at[i]));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int place = at[i][h];
+                    if ((unsigned)(place + kWindow) <= (unsigned)(2 * kWindow)) atomicAdd(&mine[kWindow + place], 1u);
+                }
+            }
+            if (__ballot(least[0] == 0 || least[1] == 0)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mask |= at[e / 2][e % 2] == 0 ? 1u << (j * 8 + e) : 0u;
             }
         }
-        append<true>(rs, s, raw, mask, sh, kSmallList);
+        append<true>(rs, s, mask, sh, kSmallList);
     });
-    M = block_max(mx, sh);
+    const int n_first = (int)-block_max(-(float)min((int)first[0], (int)first[1]), sh);
     const int n_small = sh.n;
-    if (!(M > kNegInf) || n_small > kSmallList || (M > 0.f && (int)(__float_as_uint(M) >> 16) >= base + kWindow)) return false;
+    if (n_first < -kWindow || n_first > kWindow || n_small > kSmallList) return false;
+    M = value_at(n_first, base);
+    if (n_first == 0) {
+        float mx = kNegInf;
+        for (int i = tid; i < n_small; i += kST) mx = fmaxf(mx, composite_value(sh.list[i]));
+        M = block_max(mx, sh);
+    }
     w.set(M, T);
     const double small = ldexp((double)list_sum(n_small, 0ull, w, sh), -kListShift);
     // masses in order; the first bin with which they reach the target
@@ -971,7 +996,7 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
     for (int i = 0; i < kValuesPer; ++i) {
         const int bin = tid * kValuesPer + i;
         n[i] = bin < kValues ? counts[bin] + counts[kValues + bin] : 0u;
-        one[i] = n[i] && bin != kWindow ? w.weight(value_of_bin(bin, base)) : 0.0;
+        one[i] = n[i] && bin != kWindow ? w.weight(value_at(bin - kWindow, base)) : 0.0;
         sum += bin == kWindow ? small : (double)n[i] * one[i];
     }
     if (tid == 0) sh.at = INT32_MAX;
@@ -991,7 +1016,7 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
     if (hit == last) { sh.red[kSW] = b_hit; sh.last = n_hit; }
     __syncthreads();
     const double rest = target - sh.red[kSW];
-    const float t = value_of_bin(last, base);
+    const float t = value_at(last - kWindow, base);
     const double w_t = w.weight(t);
     int ties = 0;
     cut = Cut{t, INT32_MAX, a_min};
@@ -1011,7 +1036,7 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
 #pragma unroll
     for (int i = 0; i < kValuesPer; ++i) {
         const int bin = tid * kValuesPer + i;
-        const bool keep = bin < last && bin != kWindow && n[i] && w.exponent(value_of_bin(bin, base)) >= a_min;
+        const bool keep = bin < last && bin != kWindow && n[i] && w.exponent(value_at(bin - kWindow, base)) >= a_min;
         if (keep) mine_kept += n[i];
         if (bin < kValues) weight[bin] = keep ? one[i] : 0.0;                    // (the counts are in registers: list_sum and the scan lie between)
     }
@@ -1025,14 +1050,13 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
         int eq = 0;
 #pragma unroll
         for (int j = 0; j < kSplitStatsNV; ++j) {
-            float v[N];
-            rs.values(raw[j], stats_group_first(s, j) + lane, s, v);
+            short2_t at[4];
+            value_places(rs, raw[j], stats_group_first(s, j) + lane, s, base, at);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                bool counted;
-                const int bin = value_bin(v[e], base, counted);
-                if (counted && bin < last) seg += weight[bin];
-                eq += __builtin_popcountll(__ballot(bin == last));
+            for (int e = 0; e < 8; ++e) {
+                const int place = at[e / 2][e % 2];
+                if (place < last - kWindow) seg += weight[kWindow + place];      // (none lies in front of the window: M would)
+                eq += __builtin_popcountll(__ballot(place == last - kWindow));
             }
         }
         seg = wave_sum(seg);
@@ -1085,7 +1109,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     if (tid == 0) sh.n = 0;
     if constexpr (PHASE == 0) {
         if (parts > 1 && tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
-        pl = peek<BF16>(rs, a.V, T, k, p, min_p, sh);
+        pl = peek<BF16>(rs, a.V, T, k, p, min_p, parts == 1, sh);
         w.set(pl.ref, T);
         if (parts > 1 && cut_p && k <= 0 && part == 0 && tid == 0) {             // (for the second launch)
             const RowScratch<BF16> rx(a, row);
