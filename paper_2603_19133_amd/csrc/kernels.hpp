@@ -422,11 +422,11 @@ inline int sample_parts(int dtype, int64_t rows, int V) {
     const int64_t fit = kSampleSlots / rows;
     return (int)std::min<int64_t>(std::min(std::max<int64_t>(fit, 1), (int64_t)kSampleMostParts), most);
 }
-// a row's share of it: the arrival word, three words a part, one for the row and two sums a part, the segments' masses, the parts' histograms, the parts' lists
+// a row's share of it: the arrival word, three words a part and three for the row, the segments' masses, the parts' histograms, the parts' lists
 struct SampleScratch { size_t seg_at, hist_at, list_at, row_bytes; int list_cap; };
 __host__ __device__ inline SampleScratch sample_scratch(bool bf16, int V, int parts) {
     SampleScratch l;
-    l.seg_at = kArrivalStride + ((size_t)parts * 6 + 2 + 31) / 32 * 256;
+    l.seg_at = kArrivalStride + ((size_t)parts * 3 + 3 + 31) / 32 * 256;
     l.hist_at = l.seg_at + ((size_t)stats_segments(row_vecs_max(bf16, V)) + 31) / 32 * 256;
     l.list_at = l.hist_at + (size_t)parts * 2048 * 8;
     l.list_cap = kSampleList * 2 / parts + 512 < kSampleList ? kSampleList * 2 / parts + 512 : kSampleList;

@@ -508,48 +508,53 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
         if (k <= 0) pl.way = kHist;
         return pl;
     }
-    // the peek's element of that rank, or one a little behind: a threshold with `rank` to 1.25 `rank` elements at or above it
-    uint32_t lo = key_of_bits(__float_as_uint(kNegInf)), hi = key_of_bits(__float_as_uint(ref));
-    if (rank <= kST) lo = key_of_bits(__float_as_uint(-block_max(-mx, sh)));    // (every thread has one at or above the least of their largest)
-    for (int i = 0; lo < hi; ++i) {                                             // (count at or above lo >= rank, above hi: none; 32 halvings at most)
-        const uint32_t mid = lo + (hi - lo) / 2 + 1;
-        uint32_t n = 0;
+    // the peek's element of a rank, or one a little behind: `rank` to 1.25 `rank` elements lie at or above it
+    const float least_max = -block_max(-mx, sh);                                // (every thread has one at or above the least of their largest)
+    auto of_rank = [&](int rank) {
+        uint32_t lo = key_of_bits(__float_as_uint(rank <= kST ? least_max : kNegInf)), hi = key_of_bits(__float_as_uint(ref));
+        for (int i = 0; lo < hi; ++i) {                                         // (count at or above lo >= rank, above hi: none; 32 halvings at most)
+            const uint32_t mid = lo + (hi - lo) / 2 + 1;
+            const float t = __uint_as_float(bits_of_key(mid));
+            uint32_t n = 0;
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
+            for (int j = 0; j < PER; ++j)
 #pragma unroll
-            for (int e = 0; e < N; ++e) n += (uint32_t)__builtin_popcountll(__ballot(key_of_bits(__float_as_uint(v[j][e])) >= mid));
-        if (lane == 0) sh.votes[i & 1][wave] = n;
-        __syncthreads();
-        n = 0;
+                for (int e = 0; e < N; ++e) n += (uint32_t)__builtin_popcountll(__ballot(v[j][e] >= t));
+            if (lane == 0) sh.votes[i & 1][wave] = n;
+            __syncthreads();
+            n = 0;
 #pragma unroll
-        for (int w = 0; w < kSW; ++w) n += sh.votes[i & 1][w];
-        if (n >= (uint32_t)rank) {
-            lo = mid;
-            if (n <= (uint32_t)(rank + rank / 4)) break;
-        } else {
-            hi = mid - 1;
+            for (int w = 0; w < kSW; ++w) n += sh.votes[i & 1][w];
+            if (n >= (uint32_t)rank) {
+                lo = mid;
+                if (n <= (uint32_t)(rank + rank / 4)) break;
+            } else {
+                hi = mid - 1;
+            }
         }
-    }
-    __syncthreads();
-    pl.least = __uint_as_float(bits_of_key(lo));
+        __syncthreads();
+        return __uint_as_float(bits_of_key(lo));
+    };
+    pl.least = of_rank(rank);
     pl.way = kList;
     if (k > 0) return pl;
     pl.total = true;
     const float c = (float)(kLog2e / (double)T);
+    // (without the peek's eight largest: what is by chance among the row's few that hold much of it says nothing of the rest)
+    const float few = of_rank(8);
     float above = 0.f, total = 0.f;
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float x = exp_stream(v[j][e], ref, c);
+            const float x = v[j][e] < few ? exp_stream(v[j][e], ref, c) : 0.f;
             total += x;
             above += v[j][e] >= pl.least ? x : 0.f;
         }
     double a_all, t_all;
     block_scan_excl((double)above, sh.red, a_all);
     block_scan_excl((double)total, sh.red, t_all);
-    // (without the peek's largest: one that is by chance among the row's few that hold much of it says nothing of the rest)
-    if (a_all - 1.0 >= ((double)p + 0.3 * (1.0 - (double)p)) * (t_all - 1.0)) return pl;
+    if (a_all >= ((double)p + 0.3 * (1.0 - (double)p)) * t_all) return pl;
     pl.way = kHist;
     if constexpr (BF16) return pl;                                               // (count_values, or several workgroups: neither leaves any out)
     // bins behind which the peek has less than 1 / 1.15 of what top-p leaves out
@@ -563,7 +568,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
             for (int e = 0; e < N; ++e) behind += (ref - v[j][e]) * (kHistPerNat / T) > mid ? exp_stream(v[j][e], ref, c) : 0.f;
         double all_behind;
         block_scan_excl((double)behind, sh.red, all_behind);
-        if (all_behind * 1.15 <= (1.0 - (double)p) * (t_all - 1.0)) far = mid;
+        if (all_behind * 1.15 <= (1.0 - (double)p) * t_all) far = mid;
         else near = mid;
     }
     pl.far = far;
@@ -747,14 +752,12 @@ __device__ __forceinline__ int list_to_segments(const RowStream<BF16>& rs, int n
 template <bool BF16>
 struct RowScratch {
     unsigned long long *word, *head, *seg, *hist, *lists;
-    double2* totals;
     int cap;
     __device__ __forceinline__ RowScratch(const SampleArgs& a, int64_t row) {
         const SampleScratch l = sample_scratch(BF16, a.V, a.parts);
         char* const base = a.scratch + row * (int64_t)l.row_bytes;
         word = (unsigned long long*)base;
         head = (unsigned long long*)(base + kArrivalStride);
-        totals = (double2*)(base + kArrivalStride + 16 * (2 * a.parts + 1));
         seg = (unsigned long long*)(base + l.seg_at);
         hist = (unsigned long long*)(base + l.hist_at);
         lists = (unsigned long long*)(base + l.list_at);
@@ -1081,6 +1084,63 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
     return true;
 }
 
+// A list of up to kST entries, an entry a thread: ordered by counting what lies in front of each (256 entries: a microsecond; a selection, whose histograms
+// are a dozen barriers each, takes two to three), then the kept ones by id in the same way.  False: the list does not reach the prefix's end.
+__device__ __forceinline__ bool finish_short(int n, int k, float p, double a_min, double row_total, bool whole_row, float u, const Weights& w, RowShared& sh,
+                                             int& tok, int& kept, double& total)
+{
+    const int tid = threadIdx.x;
+    unsigned long long c = tid < n ? sh.list[tid] : 0ull;
+    if (tid < 8) sh.list[n + tid] = 0ull;
+    if (tid == 0) { sh.at = INT32_MAX; sh.last = -1; }
+    __syncthreads();
+    static_assert(kST + 8 <= kSampleList && kST <= kListBins && kST <= kSegs, "the arrays that lend their room");
+    int rank = 0;
+    if ((tid & ~(kWave - 1)) < n) {
+        for (int j = 0; j < n; j += 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rank += sh.list[j + i] > c;
+        }
+        if (tid < n) sh.mass[rank] = c;
+    }
+    __syncthreads();
+    c = tid < n ? sh.mass[tid] : 0ull;
+    const bool in_k = tid < n && (k <= 0 || tid < k);
+    const float z = composite_value(c);
+    const int x = composite_id(c);
+    const double one = in_k ? w.weight(z) : 0.0;
+    double listed, before = block_scan_excl(one, sh.red, listed);
+    const double target = p > 0.f && p < 1.f ? (double)p * (whole_row ? row_total : listed) : (double)INFINITY;
+    if (whole_row && listed < target) return false;
+    if (!(in_k && before < target && w.exponent(z) >= a_min)) atomicMin(&sh.at, tid);
+    __syncthreads();
+    kept = min(sh.at, kST);
+    __syncthreads();
+    if (tid < kept) sh.count[tid] = (uint32_t)x;
+    else if (tid < kept + 8) sh.count[tid] = 0xFFFFFFFFu;
+    if (tid < 8 && kept + 8 > kST) sh.count[kST + tid] = 0xFFFFFFFFu;
+    if (tid == 0) sh.at = INT32_MAX;
+    __syncthreads();
+    rank = 0;
+    if ((tid & ~(kWave - 1)) < kept) {
+        for (int j = 0; j < kept; j += 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rank += sh.count[j + i] < (uint32_t)x;
+        }
+        if (tid < kept) { sh.mass[rank] = (unsigned long long)(uint32_t)x; sh.seg[rank] = one; }
+    }
+    __syncthreads();
+    const double mine = tid < kept ? sh.seg[tid] : 0.0;
+    before = block_scan_excl(mine, sh.red, total);
+    if (mine > 0.0) {
+        if (before + mine > (u >= 0.f ? (double)u : 0.0) * total) atomicMin(&sh.at, tid);
+        atomicMax(&sh.last, tid);
+    }
+    __syncthreads();
+    tok = (int)sh.mass[sh.at != INT32_MAX ? sh.at : sh.last];
+    return true;
+}
+
 // PHASE 0: everything but the second pass of histograms whose rows have several workgroups; 1: those.
 template <bool BF16, int PHASE>
 __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
@@ -1102,25 +1162,27 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     Weights w;
     Cut cut{kNegInf, -1, a_min};
     Plan pl;
+    Bracket br{false, 0.f, 0.f};
     int kept = 0;
     float M = kNegInf;
     double total = 0.0, above_ref = 0.0;
-    bool done = false;
+    bool done = false, drawn = false;
+    int tok = -1;
     if (tid == 0) sh.n = 0;
     if constexpr (PHASE == 0) {
         if (parts > 1 && tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
         pl = peek<BF16>(rs, a.V, T, k, p, min_p, parts == 1, sh);
         w.set(pl.ref, T);
-        if (parts > 1 && cut_p && k <= 0 && part == 0 && tid == 0) {             // (for the second launch)
-            const RowScratch<BF16> rx(a, row);
-            rx.head[parts * 3] = pack2((uint32_t)pl.way, __float_as_uint(pl.ref));
-        }
+        if (parts > 1 && cut_p && k <= 0 && pl.way != kHist && part == 0 && tid == 0) RowScratch<BF16>(a, row).head[parts * 3] = 0ull;   // (nothing for the second launch)
         __syncthreads();
     } else {
-        const unsigned long long h = RowScratch<BF16>(a, row).head[parts * 3];
-        pl = Plan{(Way)(int)(uint32_t)h, __uint_as_float((uint32_t)(h >> 32)), kNegInf, false};
-        if (pl.way != kHist) return;
-        if (tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
+        const RowScratch<BF16> rx(a, row);
+        const unsigned long long h = rx.head[parts * 3], ends = rx.head[parts * 3 + 1];
+        if ((uint32_t)h == 0u) return;
+        pl = Plan{kHist, __uint_as_float((uint32_t)(h >> 32)), kNegInf, false, 0.f};
+        br = Bracket{(uint32_t)h == 2u, __uint_as_float((uint32_t)ends), __uint_as_float((uint32_t)(ends >> 32))};
+        M = __uint_as_float((uint32_t)(rx.head[parts * 3 + 2] >> 32));
+        if (tid == 0) open_arrival(rx.word);
         __syncthreads();
     }
     if (pl.way == kCareful && part != 0) return;
@@ -1140,16 +1202,20 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                 w.set(M, T);
                 unsigned long long last = 0;
                 done = k <= 0 || n >= k || !(pl.least > kNegInf);
-                if (done && k > 0 && k < n) last = select<false>(n, 0ull, (double)k, w, sh);
-                if (done && cut_p) {
-                    const unsigned long long listed = list_sum(n, last, w, sh);
-                    const double target = k > 0 ? (double)p * (double)listed : ldexp((double)p * total * scale, kListShift);
-                    done = target <= (double)listed;
-                    if (done) last = max(last, select<true>(n, last, target, w, sh));
-                }
-                if (done) {
-                    if (last) { cut.t = composite_value(last); cut.id = composite_id(last); }
-                    kept = list_to_segments<BF16>(rs, n, cut, w, false, sh);
+                if (done && n <= kST) {
+                    done = drawn = finish_short(n, k, p, a_min, total * scale, pl.total, a.u[row], w, sh, tok, kept, total);
+                } else if (done) {
+                    if (k > 0 && k < n) last = select<false>(n, 0ull, (double)k, w, sh);
+                    if (cut_p) {
+                        const unsigned long long listed = list_sum(n, last, w, sh);
+                        const double target = k > 0 ? (double)p * (double)listed : ldexp((double)p * total * scale, kListShift);
+                        done = target <= (double)listed;
+                        if (done) last = max(last, select<true>(n, last, target, w, sh));
+                    }
+                    if (done) {
+                        if (last) { cut.t = composite_value(last); cut.id = composite_id(last); }
+                        kept = list_to_segments<BF16>(rs, n, cut, w, false, sh);
+                    }
                 }
             }
             if (!done && near && pl.total) { pl.way = kHist; alone = true; }     // (the peek took a spread row for a peaked one)
@@ -1162,6 +1228,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     }
     if (pl.way == kHist && !(COUNTS && alone)) {
         const int at = alone ? 0 : part, of = alone ? 1 : parts;
+        bool good = PHASE == 1;
         if constexpr (PHASE == 0) {
             w.set(pl.ref, T);
             __syncthreads();
@@ -1169,51 +1236,57 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
             for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
             __syncthreads();
             first_pass<BF16, kHist, false>(rs, at, of, pl, w, T, sh, M, kept, total, above_ref);
-            if (COUNTS || !alone) {                                            // (the second launch goes on)
+            bool last = true;
+            if (!alone) {
                 const RowScratch<BF16> rx(a, row);
-                for (int i = tid; i < kBins; i += kST) rx.hist[(int64_t)part * kBins + i] = sh.hist[0][i] + sh.hist[1][i];
+                for (int i = tid; i < kBins; i += kST) put_shared(&rx.hist[(int64_t)part * kBins + i], sh.hist[0][i] + sh.hist[1][i]);
                 if (tid == 0) {
-                    rx.head[part * 3] = pack2(0u, __float_as_uint(M));
-                    rx.totals[part] = make_double2(total, above_ref);
+                    put_shared(&rx.head[part * 3], pack2(0u, __float_as_uint(M)));
+                    put_shared(&rx.head[part * 3 + 1], (unsigned long long)__double_as_longlong(total));
+                    put_shared(&rx.head[part * 3 + 2], (unsigned long long)__double_as_longlong(above_ref));
                 }
-                return;
+                last = arrive_last(rx.word, (unsigned)parts, tid == 0);
+                if (!last) return;                                               // (the second launch goes on)
+                unsigned long long sums[kBins / kST] = {};
+#pragma unroll 4
+                for (int j = 0; j < parts; ++j)
+#pragma unroll
+                    for (int i = 0; i < kBins / kST; ++i) sums[i] += get_shared(&rx.hist[(int64_t)j * kBins + i * kST + tid]);
+                const int lane = tid & (kWave - 1), mine = min(lane, parts - 1);
+                const unsigned long long h0 = get_shared(&rx.head[mine * 3]), h1 = get_shared(&rx.head[mine * 3 + 1]), h2 = get_shared(&rx.head[mine * 3 + 2]);
+                M = wave_max(__uint_as_float((uint32_t)(h0 >> 32)));
+                total = wave_sum(lane < parts ? __longlong_as_double((long long)h1) : 0.0);
+                above_ref = wave_sum(lane < parts ? __longlong_as_double((long long)h2) : 0.0);
+#pragma unroll
+                for (int i = 0; i < kBins / kST; ++i) { sh.hist[0][i * kST + tid] = sums[i]; sh.hist[1][i * kST + tid] = 0ull; }
+                __syncthreads();
             }
-        } else {
-            const RowScratch<BF16> rx(a, row);
-            unsigned long long sums[kBins / kST] = {};
-            for (int j = 0; j < parts; ++j)
-#pragma unroll
-                for (int i = 0; i < kBins / kST; ++i) sums[i] += rx.hist[(int64_t)j * kBins + i * kST + tid];
-#pragma unroll
-            for (int i = 0; i < kBins / kST; ++i) { sh.hist[0][i * kST + tid] = sums[i]; sh.hist[1][i * kST + tid] = 0ull; }
-            const int lane = tid & (kWave - 1);
-            M = wave_max(lane < parts ? __uint_as_float((uint32_t)(rx.head[lane * 3] >> 32)) : kNegInf);
-            const double2 t = lane < parts ? rx.totals[lane] : make_double2(0.0, 0.0);
-            total = wave_sum(t.x);
-            above_ref = wave_sum(t.y);
-            pl.far = (float)(kBins - 1);
-            __syncthreads();
-        }
-        if constexpr (!COUNTS) {
-            Bracket br;
             int found = M <= kFloatMax ? bracket(p, total, above_ref, pl.far, sh, br) : -1;
-            if constexpr (PHASE == 0) {
-                if (found == 0) {
-                    pl.far = (float)(kBins - 1);
-                    for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
-                    __syncthreads();
-                    first_pass<BF16, kHist, false>(rs, 0, 1, pl, w, T, sh, M, kept, total, above_ref);
-                    found = bracket(p, total, above_ref, pl.far, sh, br);
-                }
+            if (!BF16 && found == 0) {
+                pl.far = (float)(kBins - 1);
+                for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
+                __syncthreads();
+                first_pass<BF16, kHist, false>(rs, 0, 1, pl, w, T, sh, M, kept, total, above_ref);
+                found = bracket(p, total, above_ref, pl.far, sh, br);
             }
-            bool good = found > 0;
+            good = found > 0;
             if (good && a_min > -__builtin_huge_val()) {
                 // (min-p against where top-p ends: clearly above, clearly not, or the careful way)
                 const double x = ((double)pl.ref - ((double)M + a_min / kLog2e * (double)T)) * (double)per;
                 br.by_min_p = x < (double)br.from - 1.0;
                 good = br.by_min_p || x > (double)br.to + 1.0;
             }
-            if (!good && at != 0) return;                                            // (all parts see the same)
+            if (!alone) {
+                if (tid == 0) {
+                    const RowScratch<BF16> rx(a, row);
+                    put_shared(&rx.head[parts * 3], pack2(good ? (br.by_min_p ? 2u : 1u) : 0u, __float_as_uint(pl.ref)));
+                    put_shared(&rx.head[parts * 3 + 1], pack2(__float_as_uint(br.from), __float_as_uint(br.to)));
+                    put_shared(&rx.head[parts * 3 + 2], pack2(0u, __float_as_uint(M)));
+                }
+                if (good) return;
+            }
+        }
+        if constexpr (!COUNTS) {
             if (good) {
                 w.set(M, T);
                 if (tid == 0) sh.n = 0;
@@ -1252,9 +1325,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
         kept = kept2;
         M = M2;
     }
-    int tok = -1;
-    total = 0.0;
-    if (M > kNegInf) draw<BF16>(rs, w, cut, a.u[row], sh, tok, total);
+    if (!drawn && M > kNegInf) draw<BF16>(rs, w, cut, a.u[row], sh, tok, total);
     if (tid == 0) {
         a.tok[row] = tok;
         a.prob[row] = tok < 0 ? 0.f : (float)(w.weight(cleaned(logit_at<BF16>(a.logits, a.ld, row, tok))) / total);
