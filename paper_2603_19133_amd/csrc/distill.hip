@@ -5,10 +5,10 @@
 //            T dL/dz_v = q_v - ph_v
 //   tail 1   L = sum_j p_j (ln p_j - ln q_j) + pt (ln pt - ln qt),  pt = max(0, 1 - sum p), qt = q's mass off the record
 //            T dL/dz_v = W q_v - p_v on the record, (W - pt / qt) q_v off it,  W = sum p + pt
-// What bounds it: the row is read once (forward) and the gradient written once.  With the gradient in the same call a thread can keep kDistillHeld
-// vectors of its row in registers between the two (0: the gradient reads the row again).
+// What bounds it: the row is read once (forward) and the gradient written once, at the rate of a copy where both are in one call (2048 rows of 128,256 fp32 with records of
+// 1024 450 us = 4.7 TB/s, 4096 of 151,936 bf16 500 us = 5.0 TB/s); the forward alone is at 5.5 TB/s with short records.  With the gradient in the same call a row is
+// read twice by its workgroup, but for what a thread holds of it, and the second time from the caches.
 // qt is summed directly: 1 - sum_j q_j loses it where the record holds nearly all of q, and the gradient off the record has pt / qt in it.
-// The ids of the record are a bitmap in LDS, one bit per element (a byte per vector of eight bf16 values), which the streaming sum masks with.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -16,8 +16,6 @@ namespace picospec {
 
 namespace {
 
-constexpr int kDT = kDistillThreads;
-constexpr int kDW = kDT / kWave;
 
 struct DistillArgs {
     const void* logits; int64_t ld; int V; float T;
@@ -26,7 +24,7 @@ struct DistillArgs {
 };
 
 // sums of N doubles over the workgroup, the same bits in every thread (fixed order)
-template <int N>
+template <int kDW, int N>
 __device__ __forceinline__ void block_sums(double (&v)[N], double* sh)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -46,6 +44,13 @@ __device__ __forceinline__ void block_sums(double (&v)[N], double* sh)
     __syncthreads();
 }
 
+// log2 p, p > 0 and finite, to 2^-24 or so whatever its size: the exponent apart, the mantissa's logarithm in fp32 (a 64-bit logarithm per entry of a long record costs as
+// much as the row)
+__device__ __forceinline__ double log2_of(float p)
+{
+    return (double)__builtin_amdgcn_frexp_expf(p) + (double)__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(p));
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
     // (round to nearest, ties to even)
@@ -56,8 +61,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return r;
 }
 
-// 16 bytes to an address that is element-aligned only: the output rows need not lie like the input's (global stores take any alignment)
-struct __attribute__((packed, aligned(2))) Loose16 { u32x4_t v; };
+// 16 bytes to an address that is element-aligned only: the output rows need not lie like the input's (global stores take any alignment).  Non-temporal: the
+// gradient is not read here again, and the rows that are read twice keep their place in the caches (2048 rows of 128,256 fp32: 671 -> 544 us).
+typedef u32x4_t loose_t __attribute__((aligned(2)));
 
 template <bool BF16>
 __device__ __forceinline__ void store_vec(char* grad_row, const RowView& rv, int q, const float (&g)[Vec<BF16>::N])
@@ -68,7 +74,7 @@ __device__ __forceinline__ void store_vec(char* grad_row, const RowView& rv, int
         u32x4_t t;
         if constexpr (BF16) { t.x = pack_bf16(g[0], g[1]); t.y = pack_bf16(g[2], g[3]); t.z = pack_bf16(g[4], g[5]); t.w = pack_bf16(g[6], g[7]); }
         else { t.x = __float_as_uint(g[0]); t.y = __float_as_uint(g[1]); t.z = __float_as_uint(g[2]); t.w = __float_as_uint(g[3]); }
-        reinterpret_cast<Loose16*>(grad_row + (int64_t)x * ESZ)->v = t;
+        __builtin_nontemporal_store(t, reinterpret_cast<loose_t*>(grad_row + (int64_t)x * ESZ));
         return;
     }
     const unsigned vm = vec_valid_mask<BF16>(rv, q);
@@ -88,19 +94,30 @@ __device__ __forceinline__ void store_one(char* grad_row, int x, float g)
 }
 
 // One row per workgroup.  FWD: loss, acceptance and the row's statistics; GRAD: the gradient, from the statistics of this or of an earlier call.
-template <bool BF16, bool FWD, bool GRAD, bool TAIL>
+// HELD: vectors that a thread keeps from the sum to the gradient.
+//
+// Weights are 2^(z c - r), c = log2(e) / T in fp32 and r an integer that is the same for a wave, near its largest exponent: one fused multiply-add and one
+// exponential per element (the product inside is exact, so the error is that of (z - M) c).  r moves up, and the lanes' sums are rescaled, only when an element
+// lies more than 2^64 above it.  Rows with |M c| >= 2^24, where r is no integer near M c any more, take (z - M) c and read the row once more.
+//
+// What the record's entries need of the row, and the row of them:
+//   SLOTS   The record lies in LDS in the order of its ids: a bit per element, the number of bits in front of every 32, and the entries' p.  The streaming finds the
+//           entry of a marked element by counting bits; it leaves the element's logit there (FWD) and writes its gradient in place (GRAD).
+//   else    The logits are gathered, and the entries' gradients written over what the streaming left in their places: less to prepare, but every entry touches a line
+//           of the row each way.  For short records, and for vocabularies whose marks do not fit (kDistillLds).
+template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, int kDT, int HELD>
 __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
 {
-    constexpr int N = Vec<BF16>::N, G = 2;                       // vectors per step
-    constexpr int HELD = FWD && GRAD ? kDistillHeld : 0;         // vectors a thread keeps from the sum to the gradient
+    constexpr int N = Vec<BF16>::N, G = 2, kDW = kDT / kWave;    // G: vectors per step
     static_assert(HELD % G == 0, "whole steps");
-    __shared__ double sh[4 * kDW];
-    extern __shared__ uint32_t on_record[];                      // TAIL && FWD: bit o + id
-    const int tid = threadIdx.x;
+    __shared__ double sh[5 * kDW];
+    extern __shared__ uint32_t on_record[];                      // (TAIL && FWD) || SLOTS: bit o + id
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int64_t row = blockIdx.x;
     const RowView rv = row_view<BF16>(a.logits, a.ld, row, a.V);
     const int nq = (rv.L + N - 1) / N, trips = (nq + kDT - 1) / kDT;
     const float c = 1.4426950408889634f / a.T;
+    const double c64 = 1.4426950408889634 / (double)a.T;
     const int count = min(max(a.count[row], 0), a.k);
     char* const grad_row = (char*)a.grad + row * a.ld_grad * (BF16 ? 2 : 4);
     if (count == 0) {                                            // (a position that is not trained on)
@@ -131,190 +148,318 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
         for (int i = 0; i < HELD; ++i) if (i < trips) held[i] = load(i, Stream{});
     }
 
-    // the record: entries tid, tid + kDT, ..; a thread keeps its first one (ids outside the vocabulary: no entry)
+    // the record: entries tid, tid + kDT, .. (ids outside the vocabulary: no entry)
     struct Entry { int id; float p, z; };
-    auto entry = [&](int s) {
-        Entry e{-1, 0.f, 0.f};
-        if (s < count) {
-            e.id = a.idx[row * a.k + s];
-            if ((unsigned)e.id < (unsigned)a.V) { e.p = a.prob[row * a.k + s]; e.z = logit_at<BF16>(a.logits, a.ld, row, e.id); }
-            else e.id = -1;
-        }
-        return e;
+    auto id_of = [&](int s) {
+        const int id = s < count ? a.idx[row * a.k + s] : -1;
+        return (unsigned)id < (unsigned)a.V ? id : -1;
     };
-    const Entry own = entry(tid);
+    const int words = (rv.L + 31) / 32;
+    constexpr bool MARKS = SLOTS || (TAIL && FWD);
+    uint16_t* const in_front = reinterpret_cast<uint16_t*>(on_record + words);
+    float* const slot_p = reinterpret_cast<float*>(on_record + words + (words + 1) / 2);
+    float* const slot_z = slot_p + a.k;
+    int n_slots = 0;
+    Entry own{-1, 0.f, 0.f};
+    if constexpr (!SLOTS) {
+        own.id = id_of(tid);
+        if (own.id >= 0) { own.p = a.prob[row * a.k + tid]; own.z = logit_at<BF16>(a.logits, a.ld, row, own.id); }
+    }
+    if constexpr (MARKS) {
+        constexpr int PER = kMaxK / kDT;
+        int id[PER];
+        float p[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            id[j] = id_of(j * kDT + tid);
+            p[j] = SLOTS && id[j] >= 0 ? a.prob[row * a.k + j * kDT + tid] : 0.f;
+        }
+        for (int w = tid; w < words; w += kDT) on_record[w] = 0u;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (id[j] >= 0) atomicOr(&on_record[(rv.o + id[j]) >> 5], 1u << ((rv.o + id[j]) & 31));
+        __syncthreads();
+        if constexpr (SLOTS) {
+            const int each = (words + kDT - 1) / kDT, first = tid * each, end = min(first + each, words);
+            int mine = 0;
+            for (int w = first; w < end; ++w) mine += __builtin_popcount(on_record[w]);
+            const int incl = wave_scan_incl(mine);
+            int* const wave_sums = reinterpret_cast<int*>(sh);
+            if (lane == kWave - 1) wave_sums[wave] = incl;
+            __syncthreads();
+            int before = incl - mine;
+#pragma unroll
+            for (int w = 0; w < kDW; ++w) { if (w < wave) before += wave_sums[w]; n_slots += wave_sums[w]; }
+            for (int w = first; w < end; ++w) { in_front[w] = (uint16_t)before; before += __builtin_popcount(on_record[w]); }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (id[j] >= 0) {
+                    const int v = rv.o + id[j];
+                    slot_p[in_front[v >> 5] + __builtin_popcount(on_record[v >> 5] & ((1u << (v & 31)) - 1u))] = p[j];
+                }
+            __syncthreads();
+        }
+    }
+    // marks of vector q, and the slot of the first of them
+    auto marks = [&](int q, int& slot) {
+        const int v = min(q, nq - 1) * N, at = v & 31;
+        const uint32_t word = on_record[v >> 5];
+        if constexpr (SLOTS) slot = in_front[v >> 5] + __builtin_popcount(word & ((1u << at) - 1u));
+        return (word >> at) & ((1u << N) - 1u);
+    };
     auto each_entry = [&](auto f) {
-        if (own.id >= 0) f(own);
-#pragma unroll 1
-        for (int s = tid + kDT; s < count; s += kDT) { const Entry e = entry(s); if (e.id >= 0) f(e); }
+        if constexpr (SLOTS) {
+            for (int s = tid; s < n_slots; s += kDT) f(Entry{0, slot_p[s], slot_z[s]});
+        } else {
+            if (own.id >= 0) f(own);
+#pragma unroll 2
+            for (int s = tid + kDT; s < count; s += kDT) {
+                const int id = id_of(s);
+                if (id >= 0) f(Entry{id, a.prob[row * a.k + s], logit_at<BF16>(a.logits, a.ld, row, id)});
+            }
+        }
     };
 
     float M;
     double S, b, mass, whole;
     if constexpr (FWD) {
-        if constexpr (TAIL) {
-            for (int w = tid; w < (rv.L + 31) / 32; w += kDT) on_record[w] = 0u;
-            __syncthreads();
-            each_entry([&](const Entry& e) { atomicOr(&on_record[(rv.o + e.id) >> 5], 1u << ((rv.o + e.id) & 31)); });
-            __syncthreads();
-        }
-        // the maximum of the row and, TAIL, the sum off the record, else over all
-        OnlineSum os;
-        float mx = kNegInf;
+        // the row's maximum and the sum: over all elements, TAIL over those off the record
+        float mx = kNegInf, r = kNegInf, s = 0.f;
+        auto values = [&](int q, const uint4& raw, float (&t)[N]) {           // -inf: not in the sum
+            unpack<BF16>(raw, t);
+            unsigned out = 0u;
+            int slot = 0;
+            if constexpr (MARKS) out = marks(q, slot);
+            if (q == 0 || q >= nq - 1) {
+                const unsigned vm = vec_valid_mask<BF16>(rv, q);
+#pragma unroll
+                for (int e = 0; e < N; ++e) t[e] = (vm >> e) & 1u ? t[e] : kNegInf;
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) mx = fmaxf(mx, t[e]);
+            if constexpr (SLOTS) {
+                const unsigned in = q < nq ? out : 0u;
+                if (__ballot(in != 0u)) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) if ((in >> e) & 1u) slot_z[slot++] = t[e];
+                }
+            }
+            if constexpr (TAIL) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {                                  // (the bit as a mask over the value: two instructions)
+                    const uint32_t on = (uint32_t)((int)(out << (31 - e)) >> 31);
+                    t[e] = __uint_as_float((on & 0xFF800000u) | (~on & __float_as_uint(t[e])));
+                }
+            }
+        };
         auto add = [&](int i0, const uint4 (&raw)[G]) {
-            float v[G * N], bm = kNegInf;
+            float v[G * N];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float t[N];
-                unpack<BF16>(raw[g], t);
-                const int q = (i0 + g) * kDT + tid;
-                unsigned out = 0u;                                // elements that do not count
-                if constexpr (TAIL) {
-                    const int qq = min(q, nq - 1);
-                    const unsigned byte = reinterpret_cast<const uint8_t*>(on_record)[BF16 ? qq : qq >> 1];
-                    out = BF16 ? byte : byte >> (4 * (qq & 1));
-                }
-                if (q == 0 || q >= nq - 1) {
-                    const unsigned vm = vec_valid_mask<BF16>(rv, q);
-                    out |= ~vm;
+                values((i0 + g) * kDT + tid, raw[g], t);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) t[e] = (vm >> e) & 1u ? t[e] : kNegInf;
-                }
-                if constexpr (TAIL) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) mx = fmaxf(mx, t[e]);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) t[e] = (out >> e) & 1u ? kNegInf : t[e];
-                }
-#pragma unroll
-                for (int e = 0; e < N; ++e) { v[g * N + e] = t[e]; bm = fmaxf(bm, t[e]); }
+                for (int e = 0; e < N; ++e) v[g * N + e] = t[e];
             }
-            const float ref = os.rebase(bm, c);
-            os.s += tree_sum<0, G * N>([&](int e) { return exp_stream(v[e], ref, c); });
+            float bm = v[0];
+#pragma unroll
+            for (int e = 1; e < G * N; ++e) bm = fmaxf(bm, v[e]);
+            if (__ballot(bm * c > r + 64.f)) {                                // (uniform; the first step, and outliers)
+                const float rn = ceilf(wave_max(bm) * c);
+                if (rn > r) { s *= __builtin_amdgcn_exp2f(r - rn); r = rn; }   // (r = -inf: s is 0 and stays 0)
+            }
+            const float nr = r == kNegInf ? 0.f : -r;
+            s += tree_sum<0, G * N>([&](int e) { return __builtin_amdgcn_exp2f(fmaf(v[e], c, nr)); });
         };
         if constexpr (HELD > 0) {
 #pragma unroll
             for (int i = 0; i < HELD; i += G)
                 if (i < trips) { const uint4 raw[G] = {held[i], held[i + 1]}; add(i, raw); }
         }
-        uint4 cur[G], nxt[G];
+        if (HELD == 0 || HELD < trips) {
+            uint4 cur[G], nxt[G];
 #pragma unroll
-        for (int g = 0; g < G; ++g) cur[g] = load(HELD + g, First{});
-        for (int i = HELD; i < trips; i += G) {
+            for (int g = 0; g < G; ++g) cur[g] = load(HELD + g, First{});
+            for (int i = HELD; i < trips; i += G) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) nxt[g] = load(i + G + g, First{});
-            add(i, cur);
+                for (int g = 0; g < G; ++g) nxt[g] = load(i + G + g, First{});
+                add(i, cur);
 #pragma unroll
-            for (int g = 0; g < G; ++g) cur[g] = nxt[g];
+                for (int g = 0; g < G; ++g) cur[g] = nxt[g];
+            }
         }
-        double sum;
-        block_softmax_stats<kDW>(os.m, os.s, c, sh, M, sum);
-        if constexpr (TAIL) {                                     // (the sum is relative to the largest element off the record)
-            const float m_off = M;
-            const int lane = tid & (kWave - 1), wave = tid / kWave;
-            const float wm = wave_max(mx);
-            if (lane == 0) sh[wave] = (double)wm;
-            __syncthreads();
-            M = kNegInf;
+        const float wm = wave_max(mx);
+        if (lane == 0) sh[wave] = (double)wm;
+        __syncthreads();
+        M = kNegInf;
 #pragma unroll
-            for (int w = 0; w < kDW; ++w) M = fmaxf(M, (float)sh[w]);
-            __syncthreads();
-            if (m_off != M) sum = m_off == kNegInf ? (sum == sum ? 0.0 : sum) : sum * exp2_split(((double)m_off - (double)M) * 1.4426950408889634 / (double)a.T);
+        for (int w = 0; w < kDW; ++w) M = fmaxf(M, (float)sh[w]);
+        __syncthreads();
+        double sums[5] = {0.0, 0.0, 0.0, 0.0, 0.0};               // the weights; p, p log2 p, p log2(e) y and (TAIL) w of the record
+        if (fabsf(M * c) < 16777216.f) {
+            sums[0] = r == kNegInf ? (double)s : (double)s * exp2_split((double)r - (double)M * (double)c);
+        } else if (M > kNegInf) {
+            for (int q = tid; q < nq; q += kDT) {
+                float t[N];
+                values(q, load(q / kDT, Keep{}), t);
+#pragma unroll
+                for (int e = 0; e < N; ++e) sums[0] += (double)exp_stream(t[e], M, c);
+            }
         }
-        // the record's sums
-        const double c64 = 1.4426950408889634 / (double)a.T;
-        double s4[4] = {0.0, 0.0, 0.0, 0.0};                      // p, p ln p, p y, w (TAIL)
+        if constexpr (SLOTS) __syncthreads();                     // (the logits are in their slots)
         each_entry([&](const Entry& e) {
-            if constexpr (TAIL) s4[3] += exp_emit(e.z, M, c64);
+            if constexpr (TAIL) sums[4] += exp_emit(e.z, M, c64);
             if (e.p > 0.f) {
-                s4[0] += (double)e.p;
-                s4[1] += (double)e.p * log((double)e.p);
-                s4[2] += (double)e.p * (((double)e.z - (double)M) / (double)a.T);
+                sums[1] += (double)e.p;
+                sums[2] += (double)e.p * log2_of(e.p);
+                sums[3] += (double)e.p * (((double)e.z - (double)M) * c64);
             }
         });
-        block_sums(s4, sh);
-        mass = s4[0];
-        S = TAIL ? sum + s4[3] : sum;
-        const double lnS = log(S);
-        double loss, acc[1] = {0.0};
+        block_sums<kDW>(sums, sh);
+        mass = sums[1];
+        S = sums[0] + sums[4];
+        double pt = 0.0;
         if constexpr (TAIL) {
-            const double pt = mass < 1.0 ? 1.0 - mass : 0.0;
-            whole = mass + pt;
-            b = whole;
-            loss = mass > 0.0 ? s4[1] - s4[2] + mass * lnS : 0.0;
-            if (pt > 0.0) {
-                const double qt = sum / S;
-                loss += pt * (log(pt) - log(qt));
-                b = qt > 0.0 ? whole - pt / qt : 0.0;             // (nothing left off the record: every q there is 0)
-            }
+            pt = mass < 1.0 ? 1.0 - mass : 0.0;
+            b = whole = mass + pt;
+            if (pt > 0.0) b = sums[0] > 0.0 ? whole - pt * S / sums[0] : 0.0;  // (nothing left off the record: every q there is 0)
         } else {
-            whole = b = mass > 0.0 ? 1.0 : 0.0;
-            loss = mass > 0.0 ? (s4[1] - s4[2]) / mass - log(mass) + lnS : 0.0;
+            b = whole = mass > 0.0 ? 1.0 : 0.0;
         }
-        each_entry([&](const Entry& e) { acc[0] += fmin((double)e.p, exp_emit(e.z, M, c64) / S); });
-        block_sums(acc, sh);
-        if (M == kNegInf) { loss = 0.0; acc[0] = 0.0; b = 0.0; whole = 0.0; mass = 0.0; S = 1.0; }   // (a row that is masked whole: there is no q, and nothing is learnt from it)
         if (tid == 0) {
-            a.loss[row] = (float)loss;
-            if (a.accept) a.accept[row] = (float)acc[0];
+            const double lnS = log(S);
+            double loss = 0.0;
+            const double plain = (sums[2] - sums[3]) * 0.69314718055994531;    // sum of p (ln p - y)
+            if (mass > 0.0) loss = TAIL ? plain + mass * lnS : plain / mass - log(mass) + lnS;
+            if (pt > 0.0) loss += pt * (log(pt) - log(sums[0]) + lnS);
+            // (a row that is masked whole: there is no q, and nothing is learnt from it)
+            a.loss[row] = M == kNegInf ? 0.f : (float)loss;
             if (a.stats) a.stats[row] = make_double4((double)M, S, b, mass);
         }
     } else {
         const double4 st = a.stats[row];
         M = (float)st.x; S = st.y; b = st.z; mass = st.w;
-        whole = M == kNegInf ? 0.0 : TAIL ? mass + (mass < 1.0 ? 1.0 - mass : 0.0) : b;
+        whole = TAIL ? mass + (mass < 1.0 ? 1.0 - mass : 0.0) : b;
     }
 
     if constexpr (GRAD) {
         const double scale = (a.weight ? (double)a.weight[row] : 1.0) / (double)a.T;
-        const float off = M == kNegInf ? 0.f : (float)(scale * b / S);
-        const float ref = M == kNegInf ? 0.f : M;
-        auto put = [&](int i, const uint4& raw) {
+        const bool masked = M == kNegInf, far = !(fabsf(M * c) < 16777216.f);
+        const float nr = far ? 0.f : -(M * c);
+        // (what the rounding of M c puts into every exponent is taken out of the factor)
+        const float off = masked ? 0.f : (float)(scale * b / S * (far ? 1.0 : exp2_split((double)M * -(double)c - (double)nr)));
+        // of a marked element: on_w w - on_p p, in 64 bits (the two are often near each other)
+        const double on_w = masked ? 0.0 : scale * whole / S * (far ? 1.0 : exp2_split((double)M * -(double)c - (double)nr));
+        const double on_p = masked ? 0.0 : TAIL ? scale : mass > 0.0 ? scale / mass : 0.0;
+        auto put = [&](int i, const uint4& raw, auto far_tag) {
             const int q = i * kDT + tid;
             if (q >= nq) return;
-            float t[N];
+            float t[N], w[N];
             unpack<BF16>(raw, t);
 #pragma unroll
-            for (int e = 0; e < N; ++e) t[e] = off * exp_stream(t[e], ref, c);
+            for (int e = 0; e < N; ++e) {
+                w[e] = decltype(far_tag)::value ? exp_stream(t[e], masked ? 0.f : M, c) : __builtin_amdgcn_exp2f(fmaf(t[e], c, nr));
+                t[e] = off * w[e];
+            }
+            if constexpr (SLOTS) {
+                int slot;
+                const unsigned in = marks(q, slot);
+                if (__ballot(in != 0u)) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) if ((in >> e) & 1u) t[e] = (float)((double)w[e] * on_w - (double)slot_p[slot++] * on_p);
+                }
+            }
             store_vec<BF16>(grad_row, rv, q, t);
         };
-        // (what is not held, last first: it was read last)
-        for (int i = HELD + (trips - 1 - HELD) / 4 * 4; i >= HELD; i -= 4) {
-            uint4 raw[4];
+        if (far) {
+            for (int i = 0; i < trips; ++i) put(i, load(i, Keep{}), std::true_type{});
+        } else {
+            // (what is not held, last first: it was read last)
+            for (int i = HELD + (trips - 1 - HELD) / 4 * 4; i >= HELD; i -= 4) {
+                uint4 raw[4];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) raw[g] = load(i + g, Stream{});
+                for (int g = 0; g < 4; ++g) raw[g] = load(i + g, Stream{});
 #pragma unroll
-            for (int g = 0; g < 4; ++g) put(i + g, raw[g]);
+                for (int g = 0; g < 4; ++g) put(i + g, raw[g], std::false_type{});
+            }
+            if constexpr (HELD > 0) {
+#pragma unroll
+                for (int i = 0; i < HELD; ++i) if (i < trips) put(i, held[i], std::false_type{});
+            }
         }
-        if constexpr (HELD > 0) {
-#pragma unroll
-            for (int i = 0; i < HELD; ++i) if (i < trips) put(i, held[i]);
+    }
+    if constexpr (FWD) {
+        if (a.accept) {
+            double acc[1] = {0.0};
+            const double per_S = 1.0 / S;
+            each_entry([&](const Entry& e) { acc[0] += fmin((double)e.p, exp_emit(e.z, M, c64) * per_S); });
+            block_sums<kDW>(acc, sh);
+            if (tid == 0) a.accept[row] = M == kNegInf ? 0.f : (float)acc[0];
         }
+    }
+    if constexpr (GRAD && !SLOTS) {
         // the record's own entries over what the streaming wrote in their places
+        const double scale = (a.weight ? (double)a.weight[row] : 1.0) / (double)a.T;
+        const bool masked = M == kNegInf;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const double on = TAIL ? (M == kNegInf ? 0.0 : 1.0) : (mass > 0.0 ? 1.0 / mass : 0.0), c64 = 1.4426950408889634 / (double)a.T;
+        const double on = TAIL ? 1.0 : mass > 0.0 ? 1.0 / mass : 0.0, per_S = whole / S;
         each_entry([&](const Entry& e) {
-            store_one<BF16>(grad_row, e.id, M == kNegInf ? 0.f : (float)(scale * (whole * (exp_emit(e.z, M, c64) / S) - (e.p > 0.f ? (double)e.p * on : 0.0))));
+            store_one<BF16>(grad_row, e.id, masked ? 0.f : (float)(scale * (exp_emit(e.z, M, c64) * per_S - (e.p > 0.f ? (double)e.p * on : 0.0))));
         });
     }
 }
 
-template <bool BF16, bool FWD, bool GRAD>
+constexpr int kDistillLds = 80 * 1024;            // two workgroups per CU: slots of 4096 entries for vocabularies of up to 262,000, of 512 up to 408,000
+constexpr size_t kDistillMostLds = 144 * 1024;    // the marks of the longest row alone
+inline size_t mark_words(const DistillArgs& a) { return ((size_t)a.V + 8 + 31) / 32; }
+inline size_t marks_lds(const DistillArgs& a) { return mark_words(a) * 4; }
+inline size_t slots_lds(const DistillArgs& a, bool forward) { return (mark_words(a) + (mark_words(a) + 1) / 2 + (size_t)a.k * (forward ? 2 : 1)) * 4; }
+
+template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, int THREADS, int HELD>
+hipError_t launch_one(const DistillArgs& a, int64_t rows, size_t lds, hipStream_t stream)
+{
+    const auto kernel = distill_kernel<BF16, FWD, GRAD, TAIL, SLOTS, THREADS, HELD>;
+    static DeviceFlags done;
+    int dev;
+    if (lds > 32 * 1024)
+        if (hipError_t e = raise_lds_limit_once((const void*)kernel, kDistillMostLds, done, dev)) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(THREADS), lds, stream, a);
+    return hipGetLastError();
+}
+
+template <bool BF16, bool FWD, bool GRAD, bool SLOTS, int THREADS, int HELD>
 hipError_t launch(const DistillArgs& a, int64_t rows, hipStream_t stream)
 {
-    if (rows == 0) return hipSuccess;
-    if (a.tail) {
-        const size_t lds = FWD ? ((size_t)a.V + 8 + 31) / 32 * 4 : 0;
-        static DeviceFlags done;
-        int dev;
-        if (lds > 32 * 1024)
-            if (hipError_t e = raise_lds_limit_once((const void*)distill_kernel<BF16, FWD, GRAD, true>, ((size_t)kMaxV + 8 + 31) / 32 * 4, done, dev)) return e;
-        hipLaunchKernelGGL((distill_kernel<BF16, FWD, GRAD, true>), dim3((unsigned)rows), dim3(kDT), lds, stream, a);
-    } else {
-        hipLaunchKernelGGL((distill_kernel<BF16, FWD, GRAD, false>), dim3((unsigned)rows), dim3(kDT), 0, stream, a);
+    const size_t lds = SLOTS ? slots_lds(a, FWD) : FWD && a.tail ? marks_lds(a) : 0;
+    return a.tail ? launch_one<BF16, FWD, GRAD, true, SLOTS, THREADS, HELD>(a, rows, lds, stream) : launch_one<BF16, FWD, GRAD, false, SLOTS, THREADS, HELD>(a, rows, lds, stream);
+}
+
+// Which way, by rows, type and record length (us, 1500 rows of 128,256 unless said):
+//   loss      gathered up to 768 entries (fp32) or 1536 (bf16, where the marks cost the vector ALU more than the memory takes), slots beyond: 300 entries 134 / 135
+//             fp32, 75 / 94 bf16; 1000 147 / 137, 91 / 101; 2500 184 / 149, 126 / 107.  512 threads; gathered calls of 1024 rows and more with up to 256 entries 256: 4096 rows of
+//             32,000 bf16 50 against 57, 1024 of 128,256 fp32 86 against 93; of 256 rows of 151,936 fp32 50 against 33.
+//   gradient  slots beyond 256 entries: 300 297 / 292, 147 / 144; 2500 418 / 294, 239 / 148.  1024 threads: 3000 rows of 100,000 450 against 469 with 512 (fp32), 233 against 250.
+//   both      slots beyond 256 entries (fp32: 300 352 / 331, 2500 538 / 348), beyond 512 (bf16: 300 169 / 177, 1000 211 / 183, 2500 315 / 196), where there are fewer than 512
+//             rows beyond 2048 (256 of 151,936: 1000 47 / 58, 2500 63 / 63).  512 threads that hold 12 vectors each, a third to two thirds of a row (4096 rows of 151,936 bf16: 500;
+//             with none held 560, with 40, all of the row and one workgroup per CU, 575); none with bf16 slots (1000 entries 183 against 210).
+template <bool BF16>
+hipError_t launch_forward(const DistillArgs& a, int64_t rows, hipStream_t stream)
+{
+    if (a.grad) {
+        const bool slots = a.k > (BF16 ? (rows >= 512 ? 512 : 2048) : 256) && slots_lds(a, true) <= (size_t)kDistillLds;
+        return slots ? launch<BF16, true, true, true, 512, BF16 ? 0 : 12>(a, rows, stream) : launch<BF16, true, true, false, 512, 12>(a, rows, stream);
     }
-    return hipGetLastError();
+    if (a.k > (BF16 ? 1536 : 768) && slots_lds(a, true) <= (size_t)kDistillLds) return launch<BF16, true, false, true, 512, 0>(a, rows, stream);
+    return rows >= 1024 && a.k <= 256 ? launch<BF16, true, false, false, 256, 0>(a, rows, stream) : launch<BF16, true, false, false, 512, 0>(a, rows, stream);
+}
+
+template <bool BF16>
+hipError_t launch_backward(const DistillArgs& a, int64_t rows, hipStream_t stream)
+{
+    return a.k > 256 && slots_lds(a, false) <= (size_t)kDistillLds ? launch<BF16, false, true, true, 1024, 0>(a, rows, stream) : launch<BF16, false, true, false, 1024, 0>(a, rows, stream);
 }
 
 }  // namespace
@@ -324,8 +469,8 @@ hipError_t launch_distill(const void* logits, int dtype, int64_t ld, int n_rows,
                           float* loss, float* accept, double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream)
 {
     const DistillArgs a{logits, ld, V, temperature, idx, prob, count, k, tail, loss, accept, reinterpret_cast<double4*>(stats), weight, grad, ld_grad};
-    if (grad) return dtype == 1 ? launch<true, true, true>(a, n_rows, stream) : launch<false, true, true>(a, n_rows, stream);
-    return dtype == 1 ? launch<true, true, false>(a, n_rows, stream) : launch<false, true, false>(a, n_rows, stream);
+    if (n_rows == 0) return hipSuccess;
+    return dtype == 1 ? launch_forward<true>(a, n_rows, stream) : launch_forward<false>(a, n_rows, stream);
 }
 
 hipError_t launch_distill_grad(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature,
@@ -334,7 +479,8 @@ hipError_t launch_distill_grad(const void* logits, int dtype, int64_t ld, int n_
 {
     const DistillArgs a{logits, ld, V, temperature, idx, prob, count, k, tail, nullptr, nullptr,
                         reinterpret_cast<double4*>(const_cast<double*>(stats)), weight, grad, ld_grad};
-    return dtype == 1 ? launch<true, false, true>(a, n_rows, stream) : launch<false, false, true>(a, n_rows, stream);
+    if (n_rows == 0) return hipSuccess;
+    return dtype == 1 ? launch_backward<true>(a, n_rows, stream) : launch_backward<false>(a, n_rows, stream);
 }
 
 }  // namespace picospec

@@ -441,9 +441,7 @@ hipError_t launch_sample(const void* logits, int dtype, int64_t ld, int n_rows, 
                          const float* temperature_rows, const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows,
                          const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse, void* scratch, size_t scratch_bytes, hipStream_t stream);
 
-// ---- distillation on records (csrc/distill.hip): one workgroup of kDistillThreads per row; with the gradient in the same call a thread keeps
-// kDistillHeld vectors of its row in registers from the sum to the gradient
-constexpr int kDistillThreads = 1024, kDistillHeld = 0;
+// ---- distillation on records (csrc/distill.hip)
 hipError_t launch_distill(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature,
                           const int32_t* idx, const float* prob, const int32_t* count, int k, int tail,
                           float* loss, float* accept, double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream);

@@ -97,7 +97,7 @@ def check(got, want, tol, dtype=torch.float32):
 
 
 def run_all(ps, z, V, T, idx, prob, count, tail, weight):
-    """Step, forward + backward through autograd, and the calls apart: all against the definition, the gradients equal bit for bit."""
+    """Step, forward + backward through autograd, and the calls apart: all against the definition."""
     from paper_2603_19133_amd.training import distill_loss
     rec = record(ps, idx, prob, count)
     w = torch.from_numpy(weight).cuda()
@@ -135,6 +135,12 @@ def run_all(ps, z, V, T, idx, prob, count, tail, weight):
     (3, 32000, 256, 0.6, 0, 0, False),
     (2, 50001, 4096, 1.0, 3, 1, False),           # the longest record
     (2, 163841, 777, 0.8, 0, 5, False),           # longer than what is held between sum and gradient
+    (2, 40001, 300, 1.0, 1, 1, True),
+    (2, 30003, 1600, 1.0, 0, 3, True),
+    (600, 2049, 600, 1.0, 1, 0, True),            # slots, bf16, gradient in the call
+    (1100, 515, 7, 1.0, 0, 1, True),              # many rows
+    (1, 420001, 1000, 1.0, 0, 1, False),          # marks that do not fit beside the slots
+    (1, 1048576, 300, 1.0, 0, 1, False),          # the longest row
 ], ids=str)
 def test_against_the_definition(gpu, ps, rows, V, k, T, pad, shift, ragged, dtype, tail):
     print(f"[case] distill rows={rows} V={V} k={k} T={T} pad={pad} shift={shift} {dtype} tail={tail}", flush=True)
@@ -145,11 +151,23 @@ def test_against_the_definition(gpu, ps, rows, V, k, T, pad, shift, ragged, dtyp
 
 @pytest.mark.parametrize("tail", [0, 1])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
-def test_masks(gpu, ps, dtype, tail):
+@pytest.mark.parametrize("shift,T", [(1000.0, 1.0), (-3e7, 1e4), (2e9, 1.0), (0.0, 1e-3)])
+def test_logits_far_from_zero(gpu, ps, shift, T, dtype, tail):
+    """Rows whose exponents are large: an offset that all logits share, beyond what the fused form of the exponents takes, a small temperature."""
+    print(f"[case] distill far {shift} T={T} {dtype} tail={tail}", flush=True)
+    z, idx, prob, count = inputs(4, 3001, 300, torch.float32, 1.0, 17)
+    z = (z.double() * (1.0 if T >= 1.0 else 1e-2) * T + shift).to(dtype)
+    run_all(ps, z, 3001, T, idx, prob, count, tail, np.ones(4, np.float32))
+
+
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("k", [40, 1700])
+def test_masks(gpu, ps, k, dtype, tail):
     """Masked ids (-inf and the type's lowest value), a row that is masked whole, record ids on masked logits, probabilities of 0, a mass
     of 0 and one above 1, entries outside the vocabulary, counts outside 0..k."""
-    print(f"[case] distill masks {dtype} tail={tail}", flush=True)
-    rows, V, k = 12, 5003, 40
+    print(f"[case] distill masks k={k} {dtype} tail={tail}", flush=True)
+    rows, V = 12, 5003
     z, idx, prob, count = inputs(rows, V, k, dtype, 1.0, 77, 1, 1)
     rng = np.random.default_rng(5)
     keep = torch.from_numpy(rng.random((rows, V)) < 0.125).cuda()
