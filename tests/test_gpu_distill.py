@@ -240,6 +240,13 @@ def test_one_gradient_for_all_rows_and_a_wider_tensor(gpu, ps):
     assert torch.equal(wide.grad[:, :1003], want) and not wide.grad[:, 1003:].any()
     with pytest.raises(RuntimeError):
         acc.sum().backward()
+    loss, _ = distill_loss(wide, rec, 1003, 1.0)
+    with pytest.raises(RuntimeError, match="once"):
+        torch.autograd.grad(loss.sum(), wide, create_graph=True)
+    loss, _ = distill_loss(wide, rec, 1003, 1.0)
+    rec.prob.mul_(0.5)                                         # (what the backward call reads may not change in between)
+    with pytest.raises(RuntimeError, match="modified"):
+        loss.sum().backward()
 
 
 def test_streams_and_graph(gpu, ps):
