@@ -5,7 +5,9 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
@@ -253,6 +255,96 @@ PyObject* n_distill_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
+// ---- the distillation loss on torch's tape, in native code: the engine runs the backward call in a thread of its own, which would have to wait for the
+// interpreter twice (forward and backward of a small batch, on the host: 37 us with a Python function, of which torch takes 25 for any operator)
+
+struct Refused { int code; };
+
+int logits_code(const at::Tensor& t, int64_t& ld) {        // dtype code or error of rows2d
+    if (t.dim() != 2 || !t.is_cuda()) throw Refused{PICOSPEC_EINVAL};
+    if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) throw Refused{PICOSPEC_EDTYPE};
+    if (t.size(0) != 0 && t.stride(1) != 1) throw Refused{PICOSPEC_EINVAL};
+    ld = t.size(0) ? t.stride(0) : t.size(1);
+    return t.scalar_type() == at::kFloat ? PICOSPEC_F32 : PICOSPEC_BF16;
+}
+
+struct DistillLoss : torch::autograd::Function<DistillLoss> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& z, const at::Tensor& idx, const at::Tensor& prob, const at::Tensor& count,
+                                                  int64_t k, int64_t V, double T, int64_t tail) {
+        int64_t ld;
+        const int dt = logits_code(z, ld);
+        const int64_t rows = z.size(0);
+        if (idx.dim() != 2 || idx.size(0) != rows) throw Refused{PICOSPEC_EINVAL};
+        const auto f32 = z.options().dtype(at::kFloat);
+        at::Tensor loss = at::empty({rows}, f32), accept = at::empty({rows}, f32), stats = at::empty({rows, 4}, z.options().dtype(at::kDouble));
+        const int rc = picospec_distill(z.data_ptr(), dt, ld, (int32_t)rows, (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
+                                        (int)tail, nullptr, loss.data_ptr<float>(), accept.data_ptr<float>(), stats.data_ptr<double>(), nullptr, 0, c10::hip::getCurrentHIPStream().stream());
+        if (rc != PICOSPEC_OK) throw Refused{rc};
+        ctx->save_for_backward({z, idx, prob, count, stats});
+        ctx->saved_data["k"] = k;
+        ctx->saved_data["V"] = V;
+        ctx->saved_data["T"] = T;
+        ctx->saved_data["tail"] = tail;
+        ctx->mark_non_differentiable({accept});
+        ctx->set_materialize_grads(false);
+        return {loss, accept};
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        torch::autograd::variable_list out(8);
+        if (!grads[0].defined()) return out;
+        TORCH_CHECK(!at::GradMode::is_enabled(), "distill_loss is differentiable once");           // (create_graph: the kernel is not on the tape)
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &z = saved[0], &idx = saved[1], &prob = saved[2], &count = saved[3], &stats = saved[4];
+        const int64_t k = ctx->saved_data["k"].toInt(), V = ctx->saved_data["V"].toInt(), tail = ctx->saved_data["tail"].toInt();
+        const double T = ctx->saved_data["T"].toDouble();
+        int64_t ld;
+        const int dt = logits_code(z, ld);
+        at::Tensor grad = at::empty(z.sizes(), z.options());
+        if (z.size(1) > V) grad.slice(1, V).zero_();                                                // (columns behind the vocabulary are not read)
+        const at::Tensor weight = grads[0].contiguous();                                            // (of a sum or mean over the rows: one value seen from every row)
+        const int rc = picospec_distill_grad(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
+                                             (int)tail, weight.data_ptr<float>(), stats.data_ptr<double>(), grad.data_ptr(), z.size(1), c10::hip::getCurrentHIPStream().stream());
+        TORCH_CHECK(rc == PICOSPEC_OK, "picospec error ", rc, ": ", picospec_strerror(rc));
+        out[0] = grad;
+        return out;
+    }
+};
+
+// distill_loss(logits, idx, prob, count, k, V, temperature, tail) -> (loss, accept), or an error code of the library
+PyObject* n_distill_loss(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    try {
+        Args a{v, n};
+        const at::Tensor* t[4];
+        for (auto& x : t) {
+            PyObject* o = a.next();
+            if (!THPVariable_Check(o)) throw BadArgument("a tensor is expected");
+            x = &THPVariable_Unpack(o);
+        }
+        const int64_t k = a.i64(), V = a.i64();
+        const double T = a.f32();
+        const int64_t tail = a.i64();
+        a.done();
+        if (V < 1 || V > INT32_MAX || k < 1 || k > INT32_MAX || (tail != 0 && tail != 1)) throw Refused{PICOSPEC_EINVAL};
+        auto out = DistillLoss::apply(*t[0], *t[1], *t[2], *t[3], k, V, T, tail);
+        THPObjectPtr pair(PyTuple_New(2));
+        if (!pair) return nullptr;
+        for (int i = 0; i < 2; ++i) {
+            PyObject* o = THPVariable_Wrap(out[i]);
+            if (!o) return nullptr;
+            PyTuple_SET_ITEM(pair.get(), i, o);
+        }
+        return pair.release();
+    } catch (const Refused& r) {
+        return PyLong_FromLong(r.code);
+    } catch (const BadArgument& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, e.what());
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
 // rows2d(tensor) -> (dtype code, stride of a row, rows), or an error code of the library: a 2-d device tensor whose rows are
 // contiguous (the strides of a tensor without rows mean nothing)
 PyObject* n_rows2d(PyObject*, PyObject* o) {
@@ -363,7 +455,7 @@ PyMethodDef methods[] = {
     FAST("round", n_round), FAST("verify_sample", n_verify_sample), FAST("verify_sample_static", n_verify_sample_static),
     FAST("sample_residual", n_sample_residual<picospec_sample_residual>), FAST("sample_residual_ws", n_sample_residual<picospec_sample_residual_ws>), FAST("row_stats", n_row_stats), FAST("compress_rejected", n_compress_rejected),
     FAST("resample_sparse", n_resample_sparse), FAST("pack_downlink", n_pack_downlink), FAST("unpack_downlink", n_unpack_downlink),
-    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("sample", n_sample), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
+    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("sample", n_sample), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("distill_loss", n_distill_loss), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
     {"rows2d", (PyCFunction)n_rows2d, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

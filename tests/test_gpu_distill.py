@@ -277,6 +277,7 @@ def test_streams_and_graph(gpu, ps):
 
 
 def test_refusals_of_the_binding(gpu, ps):
+    from paper_2603_19133_amd.training import distill_loss
     z, idx, prob, count = inputs(4, 100, 5, torch.float32, 1.0, 2)
     rec = record(ps, idx, prob, count)
     short = ps.Compressed(rec.idx[:3], rec.prob[:3], rec.count[:3], rec.mass, rec.lse, 5)
@@ -286,7 +287,9 @@ def test_refusals_of_the_binding(gpu, ps):
                  lambda: ps.distill(z, 100, 0.0, rec), lambda: ps.distill(z, 101, 1.0, rec),
                  lambda: ps.distill_grad(z, 100, 1.0, rec, f.stats, out=torch.empty(4, 100, dtype=torch.bfloat16, device="cuda")),
                  lambda: ps.distill_grad(z, 100, 1.0, rec, f.stats, out=torch.empty(4, 99, device="cuda")),
-                 lambda: ps.distill_grad(z, 100, 1.0, rec, f.stats[:2])):
+                 lambda: ps.distill_grad(z, 100, 1.0, rec, f.stats[:2]),
+                 lambda: distill_loss(z, short, 100, 1.0), lambda: distill_loss(z[:, ::2], rec, 50, 1.0), lambda: distill_loss(z.half(), rec, 100, 1.0),
+                 lambda: distill_loss(z, rec, 101, 1.0), lambda: distill_loss(z, rec, 100, 0.0), lambda: distill_loss(z, rec, 100, 1.0, tail=2)):
         with pytest.raises(ps.PicoSpecError):
             call()
     torch.cuda.synchronize()
