@@ -118,18 +118,24 @@ struct RowStream {
         }
     }
     __device__ __forceinline__ int first_id(int q) const { return q * Vec<BF16>::N - rv.o; }
-    // f(s, raw) for every segment of workgroup `part` of `parts`, a wave each, the next one's loads in flight
+    // f(s, raw) for every segment of workgroup `part` of `parts`, a wave each, the next one's loads in flight; `cur` holds the first one's vectors (first_of)
+    __device__ __forceinline__ void first_of(int part, uint4 (&cur)[kSplitStatsNV]) const { load(part * kSW + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave), cur); }
     template <class F>
-    __device__ __forceinline__ void each(const F& f, int part = 0, int parts = 1) const {
+    __device__ __forceinline__ void each_from(uint4 (&cur)[kSplitStatsNV], const F& f, int part, int parts) const {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        uint4 cur[kSplitStatsNV], next[kSplitStatsNV];
-        load(part * kSW + wave, cur);
+        uint4 next[kSplitStatsNV];
         for (int s = part * kSW + wave; s < n_seg; s += parts * kSW) {
             load(s + parts * kSW, next);
             f(s, cur);
 #pragma unroll
             for (int j = 0; j < kSplitStatsNV; ++j) cur[j] = next[j];
         }
+    }
+    template <class F>
+    __device__ __forceinline__ void each(const F& f, int part = 0, int parts = 1) const {
+        uint4 cur[kSplitStatsNV];
+        first_of(part, cur);
+        each_from(cur, f, part, parts);
     }
     // f(z, x) for every element z (cleaned) with id x above -inf
     template <class F>
@@ -189,7 +195,7 @@ __device__ __forceinline__ T block_scan_excl(T v, T* red, T& total)
 
 // The segments' kept masses are in sh.seg: their sum, the token and its probability.
 template <bool BF16>
-__device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w, const Cut& cut, float u, RowShared& sh, int& tok, double& total)
+__device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w, const Cut& cut, float u, RowShared& sh, int& tok, float& z_tok, double& total)
 {
     constexpr int N = Vec<BF16>::N;
     const int tid = threadIdx.x;
@@ -251,6 +257,10 @@ __device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w
     if (last >= 0) atomicMax(&sh.last, last);
     __syncthreads();
     tok = sh.at != INT32_MAX ? sh.at : sh.last;
+#pragma unroll
+    for (int e = 0; e < N; ++e) if (have && rs.first_id(q) + e == tok) sh.f[0] = cleaned(v[e]);
+    __syncthreads();
+    z_tok = sh.f[0];
     __syncthreads();
 }
 
@@ -575,7 +585,8 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
     return pl;
 }
 
-// Appends the elements of a segment whose bit is set (bit j * N + e) to the list.  sh.n counts on behind the list's end.
+// Appends the ids of the elements of a segment whose bit is set (bit j * N + e) to the list; sh.n counts on behind the list's end.  fill_list reads their logits
+// again, from the caches, all at once: with the values at hand here a segment takes 340 instructions, a test for every element in registers.
 template <bool BF16>
 __device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, unsigned mask, RowShared& sh, int cap = kSampleList)
 {
@@ -586,12 +597,23 @@ __device__ __forceinline__ void append(const RowStream<BF16>& rs, int s, unsigne
     int base = 0;
     if (lane == 0) base = atomicAdd(&sh.n, total);
     int at = read_lane(base, 0) + incl - mine;
-    // (few lanes have any, and they read theirs again, from the caches: 36 instructions for a segment's 340 with a test for every element in registers)
     for (unsigned left = mask; left; left &= left - 1u, ++at) {
-        const int bit = __builtin_ctz(left), v = (stats_group_first(s, bit / N) + lane) * N + bit % N;      // (element of the row's vectors: inside the row, or its bit were not set)
-        const uint32_t bits = BF16 ? (uint32_t)reinterpret_cast<const uint16_t*>(rs.rv.base)[v] << 16 : reinterpret_cast<const uint32_t*>(rs.rv.base)[v];
-        if (at < cap) sh.list[at] = composite_of(bits, (uint32_t)(v - rs.rv.o));
+        const int bit = __builtin_ctz(left);
+        if (at < cap) sh.list[at] = (unsigned)rs.first_id(stats_group_first(s, bit / N) + lane) + (unsigned)(bit % N);
     }
+}
+
+// The list's first n entries, ids so far, with their logits.  Called behind a barrier; ends with one.
+template <bool BF16>
+__device__ __forceinline__ void fill_list(const RowStream<BF16>& rs, int n, RowShared& sh)
+{
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kST) {
+        const int x = (int)sh.list[i], v = rs.rv.o + x;                        // (ids of elements inside the row)
+        const uint32_t bits = BF16 ? (uint32_t)reinterpret_cast<const uint16_t*>(rs.rv.base)[v] << 16 : reinterpret_cast<const uint32_t*>(rs.rv.base)[v];
+        sh.list[i] = composite_of(bits, (uint32_t)x);
+    }
+    __syncthreads();
 }
 
 __device__ __forceinline__ unsigned long long pack2(uint32_t a, uint32_t b) { return (unsigned long long)a | (unsigned long long)b << 32; }
@@ -601,7 +623,7 @@ __device__ __forceinline__ int composite_id(unsigned long long c) { return (int)
 
 // one pass of a workgroup over its part of the row
 template <bool BF16, Way WAY, bool TOTAL>
-__device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, int parts, const Plan& pl, const Weights& w, float T, RowShared& sh,
+__device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, uint4 (&ahead)[kSplitStatsNV], int part, int parts, const Plan& pl, const Weights& w, float T, RowShared& sh,
                                            float& M, int& n_finite, double& total, double& above_ref)
 {
     constexpr int N = Vec<BF16>::N;
@@ -610,7 +632,7 @@ __device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, 
     float mx = kNegInf;
     int n = 0;                                                                   // (of the wave)
     double sum_all = 0.0, sum_over = 0.0;
-    rs.each([&](int s, const uint4 (&raw)[kSplitStatsNV]) {
+    rs.each_from(ahead, [&](int s, const uint4 (&raw)[kSplitStatsNV]) {
         unsigned mask = 0u;
         double sum = 0.0;
         float mass = 0.f, over = 0.f;
@@ -653,6 +675,7 @@ __device__ __forceinline__ void first_pass(const RowStream<BF16>& rs, int part, 
     if constexpr (TOTAL || WAY == kHist) block_scan_excl(sum_all, sh.red, total);
     if constexpr (WAY == kHist) block_scan_excl(sum_over, sh.red, above_ref);
     __syncthreads();
+    if constexpr (WAY == kList) fill_list<BF16>(rs, min(sh.n, kSampleList), sh);
 }
 
 // The entry of the list's first n, from composite `from` on, with which the sum over the entries at or above it reaches the target: counts, or masses of 2^-kListShift.
@@ -898,6 +921,7 @@ __device__ __forceinline__ void second_pass(const RowStream<BF16>& rs, int part,
     n_above = (int)t;
     block_scan_excl(sum_all, sh.red, total);
     __syncthreads();
+    if constexpr (!MIN_P) fill_list<BF16>(rs, min(sh.n, kSampleList), sh);
 }
 
 // bf16 rows of one workgroup, top-p alone: the values themselves are counted.  A window of 16 octaves of magnitude less eight values, up to the end of the one that
@@ -984,6 +1008,7 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
     const int n_first = (int)-block_max(-(float)min((int)first[0], (int)first[1]), sh);
     const int n_small = sh.n;
     if (n_first < -kWindow || n_first > kWindow || n_small > kSmallList) return false;
+    fill_list<true>(rs, n_small, sh);
     M = value_at(n_first, base);
     if (n_first == 0) {
         float mx = kNegInf;
@@ -1087,7 +1112,7 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
 // A list of up to kST entries, an entry a thread: ordered by counting what lies in front of each (256 entries: a microsecond; a selection, whose histograms
 // are a dozen barriers each, takes two to three), then the kept ones by id in the same way.  False: the list does not reach the prefix's end.
 __device__ __forceinline__ bool finish_short(int n, int k, float p, double a_min, double row_total, bool whole_row, float u, const Weights& w, RowShared& sh,
-                                             int& tok, int& kept, double& total)
+                                             int& tok, float& z_tok, int& kept, double& total)
 {
     const int tid = threadIdx.x;
     unsigned long long c = tid < n ? sh.list[tid] : 0ull;
@@ -1127,7 +1152,7 @@ __device__ __forceinline__ bool finish_short(int n, int k, float p, double a_min
 #pragma unroll
             for (int i = 0; i < 8; ++i) rank += sh.count[j + i] < (uint32_t)x;
         }
-        if (tid < kept) { sh.mass[rank] = (unsigned long long)(uint32_t)x; sh.seg[rank] = one; }
+        if (tid < kept) { sh.mass[rank] = pack2((uint32_t)x, __float_as_uint(z)); sh.seg[rank] = one; }
     }
     __syncthreads();
     const double mine = tid < kept ? sh.seg[tid] : 0.0;
@@ -1137,7 +1162,9 @@ __device__ __forceinline__ bool finish_short(int n, int k, float p, double a_min
         atomicMax(&sh.last, tid);
     }
     __syncthreads();
-    tok = (int)sh.mass[sh.at != INT32_MAX ? sh.at : sh.last];
+    const unsigned long long drawn = sh.mass[sh.at != INT32_MAX ? sh.at : sh.last];
+    tok = (int)(uint32_t)drawn;
+    z_tok = __uint_as_float((uint32_t)(drawn >> 32));
     return true;
 }
 
@@ -1163,14 +1190,18 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     Cut cut{kNegInf, -1, a_min};
     Plan pl;
     Bracket br{false, 0.f, 0.f};
+    uint4 ahead[kSplitStatsNV];
     int kept = 0;
     float M = kNegInf;
     double total = 0.0, above_ref = 0.0;
     bool done = false, drawn = false;
     int tok = -1;
+    float z_tok = 0.f;
+    const float u = a.u[row];
     if (tid == 0) sh.n = 0;
     if constexpr (PHASE == 0) {
         if (parts > 1 && tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
+        rs.first_of(part, ahead);                                                // (under way while the peek is looked at)
         pl = peek<BF16>(rs, a.V, T, k, p, min_p, parts == 1, sh);
         w.set(pl.ref, T);
         if (parts > 1 && cut_p && k <= 0 && pl.way != kHist && part == 0 && tid == 0) RowScratch<BF16>(a, row).head[parts * 3] = 0ull;   // (nothing for the second launch)
@@ -1189,9 +1220,9 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     bool alone = parts == 1;
     if (pl.way == kSum || pl.way == kList) {
         if constexpr (PHASE == 0) {
-            if (pl.way == kSum) first_pass<BF16, kSum, false>(rs, part, parts, pl, w, T, sh, M, kept, total, above_ref);
-            else if (pl.total) first_pass<BF16, kList, true>(rs, part, parts, pl, w, T, sh, M, kept, total, above_ref);
-            else first_pass<BF16, kList, false>(rs, part, parts, pl, w, T, sh, M, kept, total, above_ref);
+            if (pl.way == kSum) first_pass<BF16, kSum, false>(rs, ahead, part, parts, pl, w, T, sh, M, kept, total, above_ref);
+            else if (pl.total) first_pass<BF16, kList, true>(rs, ahead, part, parts, pl, w, T, sh, M, kept, total, above_ref);
+            else first_pass<BF16, kList, false>(rs, ahead, part, parts, pl, w, T, sh, M, kept, total, above_ref);
             if (parts > 1 && !gather<BF16>(rs, RowScratch<BF16>(a, row), part, parts, pl.way == kSum, pl.way == kList, M, kept, total, sh)) return;
             const bool near = fabs(((double)M - (double)pl.ref) * w.c) < 500.0;   // (+inf: not)
             if (pl.way == kSum) {
@@ -1203,7 +1234,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                 unsigned long long last = 0;
                 done = k <= 0 || n >= k || !(pl.least > kNegInf);
                 if (done && n <= kST) {
-                    done = drawn = finish_short(n, k, p, a_min, total * scale, pl.total, a.u[row], w, sh, tok, kept, total);
+                    done = drawn = finish_short(n, k, p, a_min, total * scale, pl.total, u, w, sh, tok, z_tok, kept, total);
                 } else if (done) {
                     if (k > 0 && k < n) last = select<false>(n, 0ull, (double)k, w, sh);
                     if (cut_p) {
@@ -1235,7 +1266,8 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
             if (!alone) pl.far = (float)(kBins - 1);                             // (there is no third pass)
             for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
             __syncthreads();
-            first_pass<BF16, kHist, false>(rs, at, of, pl, w, T, sh, M, kept, total, above_ref);
+            rs.first_of(at, ahead);
+            first_pass<BF16, kHist, false>(rs, ahead, at, of, pl, w, T, sh, M, kept, total, above_ref);
             bool last = true;
             if (!alone) {
                 const RowScratch<BF16> rx(a, row);
@@ -1266,7 +1298,8 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                 pl.far = (float)(kBins - 1);
                 for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
                 __syncthreads();
-                first_pass<BF16, kHist, false>(rs, 0, 1, pl, w, T, sh, M, kept, total, above_ref);
+                rs.first_of(0, ahead);
+                first_pass<BF16, kHist, false>(rs, ahead, 0, 1, pl, w, T, sh, M, kept, total, above_ref);
                 found = bracket(p, total, above_ref, pl.far, sh, br);
             }
             good = found > 0;
@@ -1325,10 +1358,10 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
         kept = kept2;
         M = M2;
     }
-    if (!drawn && M > kNegInf) draw<BF16>(rs, w, cut, a.u[row], sh, tok, total);
+    if (!drawn && M > kNegInf) draw<BF16>(rs, w, cut, u, sh, tok, z_tok, total);
     if (tid == 0) {
         a.tok[row] = tok;
-        a.prob[row] = tok < 0 ? 0.f : (float)(w.weight(cleaned(logit_at<BF16>(a.logits, a.ld, row, tok))) / total);
+        a.prob[row] = tok < 0 ? 0.f : (float)(w.weight(z_tok) / total);
         a.count[row] = kept;
         a.lse[row] = tok < 0 ? kNegInf : (float)(w.ref / (double)T + log(total));
     }
