@@ -38,7 +38,8 @@ struct SampleArgs {
 // is that integer; 2^f = 1 + f P(f), |f| <= 1/2, P of degree 7 fitted for the smallest largest relative error, 1.1e-12, and exact at 0.
 struct Weights {
     double ref, c, d_min;                         // d_min = -1000 / c: what lies below, -inf and NaN too, weighs 2^-1000
-    __device__ __forceinline__ void set(float ref_, float T) { ref = (double)ref_; c = kLog2e / (double)T; d_min = -1000.0 / c; }
+    __device__ __forceinline__ void set(float ref_, float T) { ref = (double)ref_; c = kLog2e / (double)T; d_min = (double)T * (-1000.0 / kLog2e); }
+    __device__ __forceinline__ void move(float ref_) { ref = (double)ref_; }
     __device__ __forceinline__ double exponent(float z) const { return ((double)z - ref) * c; }
     __device__ __forceinline__ double weight(float z) const {
         const double d = fmax((double)z - ref, d_min);
@@ -81,7 +82,7 @@ struct RowShared {
     unsigned long long entry, ends[2][kSW];
     int at, last, n;
     float f[kSW + 1];
-    uint32_t votes[2][kSW];
+    uint32_t votes[2][3][kSW];
     int part_at[kWave];                           // ends of the parts' lists
 };
 static_assert(sizeof(RowShared) <= 80 * 1024, "two workgroups per CU");
@@ -471,7 +472,7 @@ __device__ __attribute__((noinline)) void sample_careful(const void* logits, int
 // Whatever the peek promised is checked against the row (lists that are short or overflow, a prefix that does not end in its bins, +inf): such
 // rows, and records beyond the list, take the careful way.
 enum Way : int { kCareful, kSum, kList, kHist };
-constexpr int kTopPList = 2048;
+constexpr int kTopPList = 1024;
 constexpr double kHistFar = 3e-5;                 // relative error allowed for the histogram's sums (checked in fp64 behind it)
 constexpr float kHistPerNat = 64.f;
 
@@ -522,25 +523,32 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
     const float least_max = -block_max(-mx, sh);                                // (every thread has one at or above the least of their largest)
     auto of_rank = [&](int rank) {
         uint32_t lo = key_of_bits(__float_as_uint(rank <= kST ? least_max : kNegInf)), hi = key_of_bits(__float_as_uint(ref));
-        for (int i = 0; lo < hi; ++i) {                                         // (count at or above lo >= rank, above hi: none; 32 halvings at most)
-            const uint32_t mid = lo + (hi - lo) / 2 + 1;
-            const float t = __uint_as_float(bits_of_key(mid));
-            uint32_t n = 0;
+        for (int i = 0; lo < hi; ++i) {                                         // (count at or above lo >= rank, above hi: none; a quarter is left every time)
+            const uint32_t span = hi - lo, key[3] = {lo + span / 4 + 1, lo + span / 2 + 1, lo + span / 2 + span / 4 + 1};
+            uint32_t n[3] = {0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
+            for (int m = 0; m < 3; ++m) {
+                const float t = __uint_as_float(bits_of_key(key[m]));
 #pragma unroll
-                for (int e = 0; e < N; ++e) n += (uint32_t)__builtin_popcountll(__ballot(v[j][e] >= t));
-            if (lane == 0) sh.votes[i & 1][wave] = n;
-            __syncthreads();
-            n = 0;
+                for (int j = 0; j < PER; ++j)
 #pragma unroll
-            for (int w = 0; w < kSW; ++w) n += sh.votes[i & 1][w];
-            if (n >= (uint32_t)rank) {
-                lo = mid;
-                if (n <= (uint32_t)(rank + rank / 4)) break;
-            } else {
-                hi = mid - 1;
+                    for (int e = 0; e < N; ++e) n[m] += (uint32_t)__builtin_popcountll(__ballot(v[j][e] >= t));
+                if (lane == 0) sh.votes[i & 1][m][wave] = n[m];
             }
+            __syncthreads();
+            uint32_t best = 0;
+#pragma unroll
+            for (int m = 0; m < 3; ++m) {
+                n[m] = 0;
+#pragma unroll
+                for (int w = 0; w < kSW; ++w) n[m] += sh.votes[i & 1][m][w];
+            }
+            // (the highest threshold that still has `rank`)
+            if (n[2] >= (uint32_t)rank) { lo = key[2]; best = n[2]; }
+            else if (n[1] >= (uint32_t)rank) { lo = key[1]; hi = key[2] - 1; best = n[1]; }
+            else if (n[0] >= (uint32_t)rank) { lo = key[0]; hi = key[1] - 1; best = n[0]; }
+            else hi = key[0] - 1;
+            if (best && best <= (uint32_t)(rank + rank / 4)) break;
         }
         __syncthreads();
         return __uint_as_float(bits_of_key(lo));
@@ -1015,7 +1023,7 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
         for (int i = tid; i < n_small; i += kST) mx = fmaxf(mx, composite_value(sh.list[i]));
         M = block_max(mx, sh);
     }
-    w.set(M, T);
+    w.move(M);
     const double small = ldexp((double)list_sum(n_small, 0ull, w, sh), -kListShift);
     // masses in order; the first bin with which they reach the target
     uint32_t n[kValuesPer];
@@ -1109,54 +1117,119 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
     return true;
 }
 
-// A list of up to kST entries, an entry a thread: ordered by counting what lies in front of each (256 entries: a microsecond; a selection, whose histograms
-// are a dozen barriers each, takes two to three), then the kept ones by id in the same way.  False: the list does not reach the prefix's end.
-__device__ __forceinline__ bool finish_short(int n, int k, float p, double a_min, double row_total, bool whole_row, float u, const Weights& w, RowShared& sh,
-                                             int& tok, float& z_tok, int& kept, double& total)
+// The list in its order, by one histogram: every entry's place is its bin's start and the number of entries of the bin in front of it.  False: a list of more than half the room, or
+// with a bin of more than kDeep entries (many equal logits).
+constexpr int kSortMost = kSampleList / 2, kDeep = 48;
+__device__ __forceinline__ bool sort_list(int n, RowShared& sh)
+{
+    constexpr int PER = (kSortMost + kST - 1) / kST;
+    const int tid = threadIdx.x;
+    if (n > kSortMost) return false;                                             // (uniform)
+    float hi_z = kNegInf, lo_z = kNegInf;
+    unsigned long long c[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int i = e * kST + tid;
+        c[e] = i < n ? sh.list[i] : 0ull;
+        if (i < n) { const float z = composite_value(c[e]); hi_z = fmaxf(hi_z, z); lo_z = fmaxf(lo_z, -z); }
+    }
+    for (int i = tid; i < kListBins; i += kST) sh.count[i] = 0u;
+    if (tid == 0) sh.at = 0;
+    const float top = block_max(hi_z, sh), bottom = -block_max(lo_z, sh);
+    // (bins even in the logit: of the keys, most lie near 0)
+    const float scale = (float)(kListBins - 1) / (top - bottom);                 // (0 or infinite where the two are far apart or equal)
+    int bin[PER], pos[PER], deep = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        if (e * kST + tid < n) {
+            bin[e] = (int)fminf(fmaxf((top - composite_value(c[e])) * scale, 0.f), (float)(kListBins - 1));
+            pos[e] = (int)atomicAdd(&sh.count[bin[e]], 1u);
+            deep = max(deep, pos[e]);
+        }
+    if (__ballot(deep >= kDeep) && (tid & (kWave - 1)) == 0) sh.at = 1;
+    __syncthreads();
+    if (sh.at) return false;
+    const uint32_t n0 = sh.count[2 * tid], n1 = sh.count[2 * tid + 1];
+    static_assert(kListBins == 2 * kST, "two bins a thread");
+    unsigned long long all;
+    const int start = (int)block_scan_excl((unsigned long long)(n0 + n1), sh.redu, all);
+    int* const starts = reinterpret_cast<int*>(sh.mass);
+    starts[2 * tid] = start;
+    starts[2 * tid + 1] = start + (int)n0;
+    __syncthreads();
+    unsigned long long* const by_bin = &sh.list[kSortMost];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) if (e * kST + tid < n) by_bin[starts[bin[e]] + pos[e]] = c[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        if (e * kST + tid < n) {
+            const int s0 = starts[bin[e]], m = (int)sh.count[bin[e]];
+            int rank = s0;
+            for (int i = 0; i < m; ++i) rank += by_bin[s0 + i] > c[e];
+            sh.list[rank] = c[e];
+        }
+    __syncthreads();
+    return true;
+}
+
+// Of the ordered list's first n_k entries: how many top-p (a prefix that reaches the target mass; infinite: all) and min-p leave.  `listed`: the mass of the n_k.
+__device__ __forceinline__ int kept_of_list(int n_k, double p, double target, double a_min, const Weights& w, RowShared& sh, double& listed)
+{
+    constexpr int PER = (kSortMost + kST - 1) / kST;
+    const int tid = threadIdx.x, each = (n_k + kST - 1) / kST, first = tid * each;
+    double one[PER], sum = 0.0;
+    int fails = INT32_MAX;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        one[e] = 0.0;
+        if (e < each && first + e < n_k) {
+            const float z = composite_value(sh.list[first + e]);
+            one[e] = w.weight(z);
+            if (w.exponent(z) < a_min) fails = min(fails, first + e);
+        }
+        sum += one[e];
+    }
+    if (tid == 0) sh.at = n_k;
+    double before = block_scan_excl(sum, sh.red, listed);
+    if (!(target < (double)INFINITY)) target = p * listed;                       // (of theirs)
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        if (e < each && first + e < n_k && !(before < target)) fails = min(fails, first + e);
+        before += one[e];
+    }
+    if (fails < n_k) atomicMin(&sh.at, fails);
+    __syncthreads();
+    const int kept = sh.at;
+    __syncthreads();
+    return kept;
+}
+
+// The draw from the ordered list's first `kept` <= kST entries, one a thread: their order by id is found by counting the ids in front of each.
+__device__ __forceinline__ void draw_short(int kept, float u, const Weights& w, RowShared& sh, int& tok, float& z_tok, double& total)
 {
     const int tid = threadIdx.x;
-    unsigned long long c = tid < n ? sh.list[tid] : 0ull;
-    if (tid < 8) sh.list[n + tid] = 0ull;
+    const unsigned long long c = tid < kept ? sh.list[tid] : 0ull;
+    const uint32_t x = (uint32_t)composite_id(c);
+    static_assert(kST + 16 <= kListBins && kST <= kSegs, "the arrays that lend their room");
+    if (tid < kept) sh.count[tid] = x;
+    if (tid < 16) sh.count[kept + tid] = 0xFFFFFFFFu;
     if (tid == 0) { sh.at = INT32_MAX; sh.last = -1; }
     __syncthreads();
-    static_assert(kST + 8 <= kSampleList && kST <= kListBins && kST <= kSegs, "the arrays that lend their room");
-    int rank = 0;
-    if ((tid & ~(kWave - 1)) < n) {
-        for (int j = 0; j < n; j += 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rank += sh.list[j + i] > c;
-        }
-        if (tid < n) sh.mass[rank] = c;
-    }
-    __syncthreads();
-    c = tid < n ? sh.mass[tid] : 0ull;
-    const bool in_k = tid < n && (k <= 0 || tid < k);
-    const float z = composite_value(c);
-    const int x = composite_id(c);
-    const double one = in_k ? w.weight(z) : 0.0;
-    double listed, before = block_scan_excl(one, sh.red, listed);
-    const double target = p > 0.f && p < 1.f ? (double)p * (whole_row ? row_total : listed) : (double)INFINITY;
-    if (whole_row && listed < target) return false;
-    if (!(in_k && before < target && w.exponent(z) >= a_min)) atomicMin(&sh.at, tid);
-    __syncthreads();
-    kept = min(sh.at, kST);
-    __syncthreads();
-    if (tid < kept) sh.count[tid] = (uint32_t)x;
-    else if (tid < kept + 8) sh.count[tid] = 0xFFFFFFFFu;
-    if (tid < 8 && kept + 8 > kST) sh.count[kST + tid] = 0xFFFFFFFFu;
-    if (tid == 0) sh.at = INT32_MAX;
-    __syncthreads();
-    rank = 0;
     if ((tid & ~(kWave - 1)) < kept) {
-        for (int j = 0; j < kept; j += 8) {
+        int rank = 0;
+        for (int j = 0; j < kept; j += 16) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rank += sh.count[j + i] < (uint32_t)x;
+            for (int i = 0; i < 16; ++i) rank += sh.count[j + i] < x;
         }
-        if (tid < kept) { sh.mass[rank] = pack2((uint32_t)x, __float_as_uint(z)); sh.seg[rank] = one; }
+        if (tid < kept) {
+            const float z = composite_value(c);
+            sh.mass[rank] = pack2(x, __float_as_uint(z));
+            sh.seg[rank] = w.weight(z);
+        }
     }
     __syncthreads();
-    const double mine = tid < kept ? sh.seg[tid] : 0.0;
-    before = block_scan_excl(mine, sh.red, total);
+    const double mine = tid < kept ? sh.seg[tid] : 0.0, before = block_scan_excl(mine, sh.red, total);
     if (mine > 0.0) {
         if (before + mine > (u >= 0.f ? (double)u : 0.0) * total) atomicMin(&sh.at, tid);
         atomicMax(&sh.last, tid);
@@ -1165,7 +1238,6 @@ __device__ __forceinline__ bool finish_short(int n, int k, float p, double a_min
     const unsigned long long drawn = sh.mass[sh.at != INT32_MAX ? sh.at : sh.last];
     tok = (int)(uint32_t)drawn;
     z_tok = __uint_as_float((uint32_t)(drawn >> 32));
-    return true;
 }
 
 // PHASE 0: everything but the second pass of histograms whose rows have several workgroups; 1: those.
@@ -1187,6 +1259,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     const double a_min = min_p > 0.f ? log2((double)fminf(min_p, 1.f)) : -__builtin_huge_val();
 
     Weights w;
+    w.set(0.f, T);
     Cut cut{kNegInf, -1, a_min};
     Plan pl;
     Bracket br{false, 0.f, 0.f};
@@ -1203,7 +1276,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
         if (parts > 1 && tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
         rs.first_of(part, ahead);                                                // (under way while the peek is looked at)
         pl = peek<BF16>(rs, a.V, T, k, p, min_p, parts == 1, sh);
-        w.set(pl.ref, T);
+        w.move(pl.ref);
         if (parts > 1 && cut_p && k <= 0 && pl.way != kHist && part == 0 && tid == 0) RowScratch<BF16>(a, row).head[parts * 3] = 0ull;   // (nothing for the second launch)
         __syncthreads();
     } else {
@@ -1229,17 +1302,30 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                 done = near;
             } else if (near && sh.n <= kSampleList) {
                 const int n = sh.n;
-                const double scale = exp2(((double)pl.ref - (double)M) * w.c);   // (the total was summed against the peek's largest)
-                w.set(M, T);
+                w.move(M);
+                const double row_total = pl.total ? total * w.weight(pl.ref) : 0.0;  // (it was summed against the peek's largest)
                 unsigned long long last = 0;
                 done = k <= 0 || n >= k || !(pl.least > kNegInf);
-                if (done && n <= kST) {
-                    done = drawn = finish_short(n, k, p, a_min, total * scale, pl.total, u, w, sh, tok, z_tok, kept, total);
+                if (done && sort_list(n, sh)) {
+                    double listed;
+                    const int n_k = k > 0 ? min(n, k) : n;
+                    const int m = kept_of_list(n_k, cut_p ? (double)p : 2.0, pl.total ? (double)p * row_total : (double)INFINITY, a_min, w, sh, listed);
+                    done = !pl.total || listed >= (double)p * row_total;
+                    if (done && m <= kST) {
+                        drawn = true;
+                        kept = m;
+                        draw_short(m, u, w, sh, tok, z_tok, total);
+                    } else if (done) {
+                        cut.t = composite_value(sh.list[m - 1]);
+                        cut.id = composite_id(sh.list[m - 1]);
+                        kept = list_to_segments<BF16>(rs, m, cut, w, false, sh);
+                    }
                 } else if (done) {
+                    __syncthreads();
                     if (k > 0 && k < n) last = select<false>(n, 0ull, (double)k, w, sh);
                     if (cut_p) {
                         const unsigned long long listed = list_sum(n, last, w, sh);
-                        const double target = k > 0 ? (double)p * (double)listed : ldexp((double)p * total * scale, kListShift);
+                        const double target = k > 0 ? (double)p * (double)listed : ldexp((double)p * row_total, kListShift);
                         done = target <= (double)listed;
                         if (done) last = max(last, select<true>(n, last, target, w, sh));
                     }
@@ -1261,7 +1347,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
         const int at = alone ? 0 : part, of = alone ? 1 : parts;
         bool good = PHASE == 1;
         if constexpr (PHASE == 0) {
-            w.set(pl.ref, T);
+            w.move(pl.ref);
             __syncthreads();
             if (!alone) pl.far = (float)(kBins - 1);                             // (there is no third pass)
             for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
@@ -1321,7 +1407,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
         }
         if constexpr (!COUNTS) {
             if (good) {
-                w.set(M, T);
+                w.move(M);
                 if (tid == 0) sh.n = 0;
                 __syncthreads();
                 if (br.by_min_p) second_pass<BF16, true>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
@@ -1334,11 +1420,21 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                     double above = 0.0, mine = 0.0;
                     for (int i = tid * kSegsPer; i < min((tid + 1) * kSegsPer, rs.n_seg); ++i) mine += sh.seg[i];
                     block_scan_excl(mine, sh.red, above);
-                    const double target = ldexp((double)p * total - above, kListShift);
-                    const unsigned long long listed = list_sum(n, 0ull, w, sh);
-                    done = target > 0.0 && target <= (double)listed;
+                    const double target = (double)p * total - above;
+                    unsigned long long last = 0;
+                    if (!(target > 0.0)) {
+                    } else if (sort_list(n, sh)) {
+                        double listed;
+                        const int m = kept_of_list(n, 1.0, target, -__builtin_huge_val(), w, sh, listed);
+                        done = target <= listed;
+                        if (done) last = sh.list[m - 1];
+                    } else {
+                        __syncthreads();
+                        const unsigned long long listed = list_sum(n, 0ull, w, sh);
+                        done = ldexp(target, kListShift) <= (double)listed;
+                        if (done) last = select<true>(n, 0ull, ldexp(target, kListShift), w, sh);
+                    }
                     if (done) {
-                        const unsigned long long last = select<true>(n, 0ull, target, w, sh);
                         cut = Cut{composite_value(last), composite_id(last), -__builtin_huge_val()};
                         kept += list_to_segments<BF16>(rs, n, cut, w, true, sh);
                     }
