@@ -1119,7 +1119,7 @@ __device__ __forceinline__ bool count_values(const RowStream<true>& rs, const Pl
 
 // The list in its order, by one histogram: every entry's place is its bin's start and the number of entries of the bin in front of it.  False: a list of more than half the room, or
 // with a bin of more than kDeep entries (many equal logits).
-constexpr int kSortMost = kSampleList / 2, kDeep = 48;
+constexpr int kSortMost = kSampleList / 2 - 4, kDeep = 192;
 __device__ __forceinline__ bool sort_list(int n, RowShared& sh)
 {
     constexpr int PER = (kSortMost + kST - 1) / kST;
@@ -1157,18 +1157,23 @@ __device__ __forceinline__ bool sort_list(int n, RowShared& sh)
     starts[2 * tid] = start;
     starts[2 * tid + 1] = start + (int)n0;
     __syncthreads();
-    unsigned long long* const by_bin = &sh.list[kSortMost];
+    unsigned long long* const by_bin = &sh.list[kSortMost];                      // (and four words behind its end)
 #pragma unroll
     for (int e = 0; e < PER; ++e) if (e * kST + tid < n) by_bin[starts[bin[e]] + pos[e]] = c[e];
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < PER; ++e)
+    for (int e = 0; e < PER; ++e) {
+        if (e * kST >= n) break;                                                 // (uniform)
         if (e * kST + tid < n) {
             const int s0 = starts[bin[e]], m = (int)sh.count[bin[e]];
             int rank = s0;
-            for (int i = 0; i < m; ++i) rank += by_bin[s0 + i] > c[e];
+            for (int i = 0; i < m; i += 4) {                                     // (entries behind the bin's, or the list's, are smaller or not counted)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) rank += i + j < m && by_bin[s0 + i + j] > c[e];
+            }
             sh.list[rank] = c[e];
         }
+    }
     __syncthreads();
     return true;
 }
@@ -1392,7 +1397,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
             if (good && a_min > -__builtin_huge_val()) {
                 // (min-p against where top-p ends: clearly above, clearly not, or the careful way)
                 const double x = ((double)pl.ref - ((double)M + a_min / kLog2e * (double)T)) * (double)per;
-                br.by_min_p = x < (double)br.from - 1.0;
+                br.by_min_p = br.from >= 1.f && x < (double)br.from - 1.0;       // (the first bin reaches up without end)
                 good = br.by_min_p || x > (double)br.to + 1.0;
             }
             if (!alone) {

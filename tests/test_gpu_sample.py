@@ -149,6 +149,24 @@ def test_masks_and_odd_values(gpu, ps, V, dtype, setting):
     compare(ps.sample(z, V, u, temperature=0.9, **s), z, 0.9, s["top_k"], s["top_p"], s["min_p"], u)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [6, 270])
+@pytest.mark.parametrize("top_p,min_p", [(0.9, 0.014), (0.9, 0.0), (0.5, 0.2), (0.99, 0.001), (0.97, 0.3)])
+def test_few_ids_far_above_the_rest(gpu, ps, top_p, min_p, rows, dtype):
+    """Rows whose largest logits lie far above the rest, at ids that a sample of the row may or may not hold: one to three of them have about 90 % of the mass."""
+    print(f"[case] sample outliers rows={rows} {dtype} top_p={top_p} min_p={min_p}", flush=True)
+    V = 40003
+    z, u = rows_of(rows, V, dtype, "normal", 12)
+    z.mul_(0.3).sub_(3.0)
+    rng = np.random.default_rng(31)
+    for r in range(rows):
+        at = rng.choice(V, 3, replace=False)
+        z[r, int(at[0])] = 10.0
+        z[r, int(at[1])] = float(rng.choice([6.25, 8.0, 9.5]))
+        z[r, int(at[2])] = float(rng.choice([-3.0, 5.0, 7.5]))
+    compare(ps.sample(z, V, u, top_p=top_p, min_p=min_p), z, 1.0, 0, top_p, min_p, u)
+
+
 @pytest.mark.parametrize("top_p", [0.0, 0.9])
 def test_the_ends_of_the_uniforms(gpu, ps, top_p):
     """u = 0 draws the first kept id, the largest u below 1 the last; outside [0, 1): the first and the last."""
