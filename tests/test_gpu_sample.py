@@ -149,6 +149,37 @@ def test_masks_and_odd_values(gpu, ps, V, dtype, setting):
     compare(ps.sample(z, V, u, temperature=0.9, **s), z, 0.9, s["top_k"], s["top_p"], s["min_p"], u)
 
 
+@pytest.mark.parametrize("setting", [dict(), dict(top_k=50, top_p=0.9), dict(top_k=1000), dict(top_k=4000), dict(top_p=0.9), dict(top_p=0.9, min_p=0.02), dict(min_p=0.02)], ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["normal", "trend"])
+def test_the_longest_rows(gpu, ps, kind, dtype, setting):
+    print(f"[case] sample longest {kind} {dtype} {setting}", flush=True)
+    V = 1 << 20
+    z, u = rows_of(2, V, dtype, kind, 6, 1, 1)
+    s = dict(dict(top_k=0, top_p=0.0, min_p=0.0), **setting)
+    compare(ps.sample(z, V, u, **s), z, 1.0, s["top_k"], s["top_p"], s["min_p"], u)
+
+
+@pytest.mark.parametrize("top_k,top_p,min_p", [(0, 0.0, 0.0), (50, 0.9, 0.0), (900, 0.9, 0.0), (0, 0.9, 0.0), (0, 0.0, 0.05)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_spread_rows_are_the_unspread_ones(gpu, ps, dtype, top_k, top_p, min_p):
+    """With scratch, without it and with too little of it: the same tokens and counts (masses are summed in another order: probabilities to their rounding)."""
+    print(f"[case] sample spread {dtype} {top_k} {top_p} {min_p}", flush=True)
+    rows, V = 9, 60007
+    z, u = rows_of(rows, V, dtype, "normal", 44)
+    got = ps.sample(z, V, u, temperature=0.7, top_k=top_k, top_p=top_p, min_p=min_p)
+    need = ps.scratch_bytes(ps.CALL_SAMPLE, ps.F32 if dtype == torch.float32 else ps.BF16, rows, 0, V, 0)
+    assert need > 0 and need == ps.workspace_bytes(ps.CALL_SAMPLE, ps.F32 if dtype == torch.float32 else ps.BF16, rows, V, 0)
+    for size in (0, need - 1):
+        ws = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+        o = ps.Sampled(torch.zeros_like(got.tok), torch.zeros_like(got.prob), torch.zeros_like(got.count), torch.zeros_like(got.lse))
+        assert ps.lib.picospec_sample(z.data_ptr(), 0 if dtype == torch.float32 else 1, V, rows, V, 0.7, top_k, top_p, min_p, None, None, None, None, u.data_ptr(), o.tok.data_ptr(),
+                                      o.prob.data_ptr(), o.count.data_ptr(), o.lse.data_ptr(), ws.data_ptr() if size else None, size, None) == ps.OK
+        torch.cuda.synchronize()
+        assert torch.equal(o.tok, got.tok) and torch.equal(o.count, got.count)
+        assert torch.allclose(o.prob, got.prob, rtol=2.0 ** -23, atol=0.0) and torch.allclose(o.lse, got.lse, rtol=2.0 ** -23, atol=0.0)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("rows", [6, 270])
 @pytest.mark.parametrize("top_p,min_p", [(0.9, 0.014), (0.9, 0.0), (0.5, 0.2), (0.99, 0.001), (0.97, 0.3)])
