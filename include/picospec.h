@@ -97,7 +97,7 @@ enum {
 
 enum { PICOSPEC_CALL_COMPRESS = 0, PICOSPEC_CALL_SAMPLE_DRAFT = 1, PICOSPEC_CALL_VERIFY = 2, PICOSPEC_CALL_SAMPLE_RESIDUAL = 3,
        PICOSPEC_CALL_COMPRESS_REJECTED = 4, PICOSPEC_CALL_RESAMPLE_SPARSE = 5, PICOSPEC_CALL_ROUND = 6,
-       PICOSPEC_CALL_VERIFY_SAMPLE = 7, PICOSPEC_CALL_ROW_STATS = 8, PICOSPEC_CALL_SAMPLE = 9 };
+       PICOSPEC_CALL_VERIFY_SAMPLE = 7, PICOSPEC_CALL_ROW_STATS = 8, PICOSPEC_CALL_SAMPLE = 9, PICOSPEC_CALL_DISTILL = 10 };
 enum { PICOSPEC_LIMIT_MAX_K = 0, PICOSPEC_LIMIT_MAX_V = 1 };
 
 /*
@@ -460,6 +460,8 @@ int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, i
  *   stats [n_rows, 4] fp64, nullable, on a 16-byte boundary: what picospec_distill_grad takes                        out
  *   grad [n_rows, ld_grad] in the logits' dtype, ld_grad >= V, nullable: weight * d loss / d logits, rounded once; may not overlap
  *            the logits                                                                                              out
+ *   workspace (optional): picospec_workspace_bytes(PICOSPEC_CALL_DISTILL, dtype, n_rows, V, 0) bytes of scratch, in which a call of few long rows gives a row
+ *            several workgroups; NULL or a smaller one: one workgroup per row (sums in another order: they agree to rounding)
  * Rows with count 0 (positions that are not trained on) and rows without a logit above -inf have loss, accept and gradient 0.
  * A record id whose logit is -inf has loss +inf (its gradient is finite); NaN and +inf logits make a row's results NaN.
  * picospec_distill_grad forms the gradient alone, from the stats of an earlier picospec_distill of the same logits and
@@ -467,7 +469,8 @@ int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, i
  */
 int picospec_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
                      const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,
-                     float* loss, float* accept, double* stats, void* grad, int64_t ld_grad, void* stream);
+                     float* loss, float* accept, double* stats, void* grad, int64_t ld_grad,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
                           const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,

@@ -27,7 +27,7 @@ F32, BF16 = 0, 1
 OK, EINVAL, EWORKSPACE, EDTYPE, EHIP, EUNSUPPORTED, ESCRATCH = 0, -1, -2, -3, -4, -5, -6
 FLAG_TOKEN_NOT_IN_SUPPORT, FLAG_NONFINITE, FLAG_RESIDUAL_EMPTY, FLAG_BAD_INPUT = 1, 2, 4, 8
 CALL_COMPRESS, CALL_SAMPLE_DRAFT, CALL_VERIFY, CALL_SAMPLE_RESIDUAL = 0, 1, 2, 3
-CALL_COMPRESS_REJECTED, CALL_RESAMPLE_SPARSE, CALL_ROUND, CALL_VERIFY_SAMPLE, CALL_ROW_STATS, CALL_SAMPLE = 4, 5, 6, 7, 8, 9
+CALL_COMPRESS_REJECTED, CALL_RESAMPLE_SPARSE, CALL_ROUND, CALL_VERIFY_SAMPLE, CALL_ROW_STATS, CALL_SAMPLE, CALL_DISTILL = 4, 5, 6, 7, 8, 9, 10
 LIMIT_MAX_K, LIMIT_MAX_V = 0, 1
 WIRE_FP32, WIRE_FP16, WIRE_BF16 = 0, 1, 2
 WIRE_BAD_HEADER, WIRE_BAD_BATCH, WIRE_CLAMPED, WIRE_TRUNCATED = 1, 2, 4, 8
@@ -81,7 +81,7 @@ lib.picospec_unpack_downlink.argtypes = [_p, _i64, _i32, _i32, _p, _p, _p, _p, _
 lib.picospec_pack_uplink.argtypes = [_i32, _i32, _p, _p, _p, C.c_int, _p, _i64, _p, _p]
 lib.picospec_unpack_uplink.argtypes = [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p]
 lib.picospec_sample.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _i32, _f, _f, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p]
-lib.picospec_distill.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _p, _p, _i64, _p]
+lib.picospec_distill.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _p, _p, _i64, _p, _sz, _p]
 lib.picospec_distill_grad.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _i64, _p]
 lib.picospec_downlink_bytes_max.argtypes = [_i32, _i32, C.c_int]
 lib.picospec_downlink_bytes_max.restype = _i64
@@ -440,7 +440,8 @@ def distill(logits: torch.Tensor, V: int, temperature: float, rec: Compressed, t
     dt, ld, rows = _distill_inputs(logits, rec, weight)
     loss, accept, stats = _nat.empty(logits, "ffd", rows, rows, (rows, 4))
     g = torch.empty((rows, V), dtype=logits.dtype, device=logits.device) if grad else None
-    _check(_nat.distill(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, loss, accept, stats, g, V, _stream()))
+    _check(_nat.distill(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, loss, accept, stats, g, V,
+                        _nat.scratch(logits, CALL_DISTILL, dt, rows, 0, V, 0), _stream()))
     return Distilled(loss, accept, stats, g)
 
 

@@ -540,12 +540,14 @@ int check_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, int
 
 int picospec_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
                      const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,
-                     float* loss, float* accept, double* stats, void* grad, int64_t ld_grad, void* stream)
+                     float* loss, float* accept, double* stats, void* grad, int64_t ld_grad,
+                     void* workspace, size_t workspace_bytes, void* stream)
 {
     if (int rc = check_distill(logits, dtype, ld, n_rows, V, temperature, idx, prob, count, k, tail, stats, grad, ld_grad)) return rc;
     if (n_rows > 0 && !loss) return PICOSPEC_EINVAL;
+    if ((uintptr_t)workspace & 15u) return PICOSPEC_EWORKSPACE;
     return hip_status(launch_distill(logits, dtype, ld, n_rows, V, temperature, idx, prob, count, k, tail, loss, accept, stats, weight,
-                                     grad, ld_grad, (hipStream_t)stream));
+                                     grad, ld_grad, workspace, workspace_bytes, (hipStream_t)stream));
 }
 
 int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
@@ -573,6 +575,7 @@ size_t picospec_workspace_bytes(int which_call, int dtype, int32_t rows, int32_t
             return split ? (table + 15) / 16 * 16 + split : table;
         }
         case PICOSPEC_CALL_SAMPLE: return sample_scratch_bytes(dtype, rows, V);
+        case PICOSPEC_CALL_DISTILL: return distill_scratch_bytes(dtype, rows, V);
         default:
             return 0;                           // every other kernel keeps its intermediate state in LDS
     }
@@ -596,6 +599,7 @@ size_t picospec_scratch_bytes(int which_call, int dtype, int32_t n_draft, int32_
             return (round_seg_table_bytes(dtype, rows, V) + 15) / 16 * 16 + split_scratch_bytes(dtype, n_draft, V, k);
         }
         case PICOSPEC_CALL_SAMPLE: return sample_scratch_bytes(dtype, n_draft, V);
+        case PICOSPEC_CALL_DISTILL: return distill_scratch_bytes(dtype, n_draft, V);
         default: return 0;
     }
 }

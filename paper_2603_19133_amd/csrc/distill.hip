@@ -17,10 +17,14 @@ namespace picospec {
 namespace {
 
 
+// two (bf16) or one (fp32) values of -inf
+template <bool BF16> constexpr uint32_t kMaskedPair = BF16 ? 0xFF80FF80u : 0xFF800000u;
+
 struct DistillArgs {
     const void* logits; int64_t ld; int V; float T;
     const int32_t* idx; const float* prob; const int32_t* count; int k, tail;
     float *loss, *accept; double4* stats; const float* weight; void* grad; int64_t ld_grad;
+    char* scratch; int parts;                     // workgroups of a row, 1 but for SPLIT
 };
 
 // sums of N doubles over the workgroup, the same bits in every thread (fixed order)
@@ -105,30 +109,33 @@ __device__ __forceinline__ void store_one(char* grad_row, int x, float g)
 //           entry of a marked element by counting bits; it leaves the element's logit there (FWD) and writes its gradient in place (GRAD).
 //   else    The logits are gathered, and the entries' gradients written over what the streaming left in their places: less to prepare, but every entry touches a line
 //           of the row each way.  For short records, and for vocabularies whose marks do not fit (kDistillLds).
-template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, int kDT, int HELD>
+// SPLIT: a row's workgroups take consecutive trips of it; forward, the last of them to arrive adds their sums up and goes on with the record.
+template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, bool SPLIT, int kDT, int HELD>
 __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
 {
     constexpr int N = Vec<BF16>::N, G = 2, kDW = kDT / kWave;    // G: vectors per step
-    static_assert(HELD % G == 0, "whole steps");
+    static_assert(HELD % G == 0 && (!SPLIT || (HELD == 0 && !SLOTS && FWD != GRAD)), "whole steps; split rows in the plainest form");
     __shared__ double sh[5 * kDW];
     extern __shared__ uint32_t on_record[];                      // (TAIL && FWD) || SLOTS: bit o + id
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const int64_t row = blockIdx.x;
+    const int parts = SPLIT ? a.parts : 1, part = SPLIT ? (int)(blockIdx.x % (unsigned)parts) : 0;
+    const int64_t row = SPLIT ? blockIdx.x / (unsigned)parts : blockIdx.x;
     const RowView rv = row_view<BF16>(a.logits, a.ld, row, a.V);
-    const int nq = (rv.L + N - 1) / N, trips = (nq + kDT - 1) / kDT;
+    const int nq = (rv.L + N - 1) / N, all_trips = (nq + kDT - 1) / kDT, share = SPLIT ? (all_trips + parts - 1) / parts : all_trips;
+    const int begin = SPLIT ? min(part * share, all_trips) : 0, trips = SPLIT ? min(begin + share, all_trips) : all_trips;
     const float c = 1.4426950408889634f / a.T;
     const double c64 = 1.4426950408889634 / (double)a.T;
     const int count = min(max(a.count[row], 0), a.k);
     char* const grad_row = (char*)a.grad + row * a.ld_grad * (BF16 ? 2 : 4);
     if (count == 0) {                                            // (a position that is not trained on)
-        if (FWD && tid == 0) {
+        if (FWD && tid == 0 && part == 0) {
             a.loss[row] = 0.f;
             if (a.accept) a.accept[row] = 0.f;
             if (a.stats) a.stats[row] = make_double4(0.0, 1.0, 0.0, 0.0);
         }
         if constexpr (GRAD) {
             const float zero[N] = {};
-            for (int q = tid; q < nq; q += kDT) store_vec<BF16>(grad_row, rv, q, zero);
+            for (int i = begin; i < trips; ++i) if (i * kDT + tid < nq) store_vec<BF16>(grad_row, rv, i * kDT + tid, zero);
         }
         return;
     }
@@ -142,6 +149,9 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
     using Keep = std::integral_constant<int, 0>;
     using First = std::conditional_t<GRAD, Keep, Stream>;        // (what is not held is read again by the gradient)
 
+    if constexpr (SPLIT && FWD) {
+        if (tid == 0) open_arrival(reinterpret_cast<unsigned long long*>(a.scratch + row * (int64_t)distill_scratch_row(parts)));
+    }
     uint4 held[HELD ? HELD : 1];
     if constexpr (HELD > 0) {
 #pragma unroll
@@ -152,7 +162,9 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
     struct Entry { int id; float p, z; };
     auto id_of = [&](int s) {
         const int id = s < count ? a.idx[row * a.k + s] : -1;
-        return (unsigned)id < (unsigned)a.V ? id : -1;
+        if ((unsigned)id >= (unsigned)a.V) return -1;
+        if (SPLIT && GRAD && ((rv.o + id) / (N * kDT) < begin || (rv.o + id) / (N * kDT) >= trips)) return -1;       // (another part's)
+        return id;
     };
     const int words = (rv.L + 31) / 32;
     constexpr bool MARKS = SLOTS || (TAIL && FWD);
@@ -163,7 +175,8 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
     Entry own{-1, 0.f, 0.f};
     if constexpr (!SLOTS) {
         own.id = id_of(tid);
-        if (own.id >= 0) { own.p = a.prob[row * a.k + tid]; own.z = logit_at<BF16>(a.logits, a.ld, row, own.id); }
+        if (own.id >= 0) own.p = a.prob[row * a.k + tid];
+        if (!(SPLIT && FWD) && own.id >= 0) own.z = logit_at<BF16>(a.logits, a.ld, row, own.id);      // (where the row is split, the one that needs it is not known yet)
     }
     if constexpr (MARKS) {
         constexpr int PER = kMaxK / kDT;
@@ -214,10 +227,18 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
             for (int s = tid; s < n_slots; s += kDT) f(Entry{0, slot_p[s], slot_z[s]});
         } else {
             if (own.id >= 0) f(own);
-#pragma unroll 2
-            for (int s = tid + kDT; s < count; s += kDT) {
-                const int id = id_of(s);
-                if (id >= 0) f(Entry{id, a.prob[row * a.k + s], logit_at<BF16>(a.logits, a.ld, row, id)});
+#pragma unroll 1
+            for (int s = tid + kDT; s < count; s += 4 * kDT) {                  // (four gathers under way at a time)
+                Entry e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[i].id = id_of(s + i * kDT);
+                    e[i].p = e[i].id >= 0 ? a.prob[row * a.k + s + i * kDT] : 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i].z = e[i].id >= 0 ? logit_at<BF16>(a.logits, a.ld, row, e[i].id) : 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (e[i].id >= 0) f(e[i]);
             }
         }
     };
@@ -279,10 +300,12 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
                 if (i < trips) { const uint4 raw[G] = {held[i], held[i + 1]}; add(i, raw); }
         }
         if (HELD == 0 || HELD < trips) {
+            const int from = SPLIT ? begin : HELD;
             uint4 cur[G], nxt[G];
 #pragma unroll
-            for (int g = 0; g < G; ++g) cur[g] = load(HELD + g, First{});
-            for (int i = HELD; i < trips; i += G) {
+            for (int g = 0; g < G; ++g) cur[g] = load(from + g, First{});
+            for (int i = from; i < trips; i += G) {
+                if (SPLIT && i + 1 == trips) cur[1] = make_uint4(kMaskedPair<BF16>, kMaskedPair<BF16>, kMaskedPair<BF16>, kMaskedPair<BF16>);   // (the next part's)
 #pragma unroll
                 for (int g = 0; g < G; ++g) nxt[g] = load(i + G + g, First{});
                 add(i, cur);
@@ -301,12 +324,31 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
         if (fabsf(M * c) < 16777216.f) {
             sums[0] = r == kNegInf ? (double)s : (double)s * exp2_split((double)r - (double)M * (double)c);
         } else if (M > kNegInf) {
-            for (int q = tid; q < nq; q += kDT) {
+            for (int i = begin; i < trips; ++i) {
                 float t[N];
-                values(q, load(q / kDT, Keep{}), t);
+                values(i * kDT + tid, load(i, Keep{}), t);
 #pragma unroll
                 for (int e = 0; e < N; ++e) sums[0] += (double)exp_stream(t[e], M, c);
             }
+        }
+        if constexpr (SPLIT) {
+            // (M and the sum of this part; together in the last of the row's workgroups to arrive)
+            unsigned long long* const word = reinterpret_cast<unsigned long long*>(a.scratch + row * (int64_t)distill_scratch_row(parts));
+            unsigned long long* const shares = word + kArrivalStride / 8;
+            double mine[1] = {sums[0]};
+            block_sums<kDW>(mine, sh);
+            if (tid == 0) {
+                put_shared(&shares[2 * part], (unsigned long long)__float_as_uint(M));
+                put_shared(&shares[2 * part + 1], (unsigned long long)__double_as_longlong(mine[0]));
+            }
+            if (!arrive_last(word, (unsigned)parts, tid == 0)) return;
+            if (own.id >= 0) own.z = logit_at<BF16>(a.logits, a.ld, row, own.id);
+            static_assert(kDistillMostParts <= kWave, "a lane for each part");
+            const float m = lane < parts ? __uint_as_float((uint32_t)get_shared(&shares[2 * lane])) : kNegInf;
+            const double s_part = lane < parts ? __longlong_as_double((long long)get_shared(&shares[2 * lane + 1])) : 0.0;
+            M = wave_max(m);
+            sums[0] = wave_sum(m == M ? s_part : s_part * exp2_split(((double)m - (double)M) * (double)c));
+            if (tid != 0) sums[0] = 0.0;
         }
         if constexpr (SLOTS) __syncthreads();                     // (the logits are in their slots)
         each_entry([&](const Entry& e) {
@@ -374,15 +416,16 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
             store_vec<BF16>(grad_row, rv, q, t);
         };
         if (far) {
-            for (int i = 0; i < trips; ++i) put(i, load(i, Keep{}), std::true_type{});
+            for (int i = begin; i < trips; ++i) put(i, load(i, Keep{}), std::true_type{});
         } else {
             // (what is not held, last first: it was read last)
-            for (int i = HELD + (trips - 1 - HELD) / 4 * 4; i >= HELD; i -= 4) {
+            const int from = SPLIT ? begin : HELD;
+            for (int i = from + (trips - 1 - from) / 4 * 4; i >= from; i -= 4) {
                 uint4 raw[4];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) raw[g] = load(i + g, Stream{});
 #pragma unroll
-                for (int g = 0; g < 4; ++g) put(i + g, raw[g], std::false_type{});
+                for (int g = 0; g < 4; ++g) if (!SPLIT || i + g < trips) put(i + g, raw[g], std::false_type{});
             }
             if constexpr (HELD > 0) {
 #pragma unroll
@@ -418,23 +461,23 @@ inline size_t mark_words(const DistillArgs& a) { return ((size_t)a.V + 8 + 31) /
 inline size_t marks_lds(const DistillArgs& a) { return mark_words(a) * 4; }
 inline size_t slots_lds(const DistillArgs& a, bool forward) { return (mark_words(a) + (mark_words(a) + 1) / 2 + (size_t)a.k * (forward ? 2 : 1)) * 4; }
 
-template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, int THREADS, int HELD>
+template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, bool SPLIT, int THREADS, int HELD>
 hipError_t launch_one(const DistillArgs& a, int64_t rows, size_t lds, hipStream_t stream)
 {
-    const auto kernel = distill_kernel<BF16, FWD, GRAD, TAIL, SLOTS, THREADS, HELD>;
+    const auto kernel = distill_kernel<BF16, FWD, GRAD, TAIL, SLOTS, SPLIT, THREADS, HELD>;
     static DeviceFlags done;
     int dev;
     if (lds > 32 * 1024)
         if (hipError_t e = raise_lds_limit_once((const void*)kernel, kDistillMostLds, done, dev)) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(THREADS), lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * a.parts)), dim3(THREADS), lds, stream, a);
     return hipGetLastError();
 }
 
-template <bool BF16, bool FWD, bool GRAD, bool SLOTS, int THREADS, int HELD>
+template <bool BF16, bool FWD, bool GRAD, bool SLOTS, int THREADS, int HELD, bool SPLIT = false>
 hipError_t launch(const DistillArgs& a, int64_t rows, hipStream_t stream)
 {
     const size_t lds = SLOTS ? slots_lds(a, FWD) : FWD && a.tail ? marks_lds(a) : 0;
-    return a.tail ? launch_one<BF16, FWD, GRAD, true, SLOTS, THREADS, HELD>(a, rows, lds, stream) : launch_one<BF16, FWD, GRAD, false, SLOTS, THREADS, HELD>(a, rows, lds, stream);
+    return a.tail ? launch_one<BF16, FWD, GRAD, true, SLOTS, SPLIT, THREADS, HELD>(a, rows, lds, stream) : launch_one<BF16, FWD, GRAD, false, SLOTS, SPLIT, THREADS, HELD>(a, rows, lds, stream);
 }
 
 // Which way, by rows, type and record length (us, 1500 rows of 128,256 unless said):
@@ -446,29 +489,40 @@ hipError_t launch(const DistillArgs& a, int64_t rows, hipStream_t stream)
 //             rows beyond 2048 (256 of 151,936: 1000 47 / 58, 2500 63 / 63).  512 threads that hold 12 vectors each, a third to two thirds of a row (4096 rows of 151,936 bf16: 500;
 //             with none held 560, with 40, all of the row and one workgroup per CU, 575); none with bf16 slots (1000 entries 183 against 210).
 template <bool BF16>
+hipError_t launch_backward(const DistillArgs& a, int64_t rows, hipStream_t stream)
+{
+    DistillArgs b = a;
+    b.parts = distill_parts(BF16, rows, a.V, kDistillBackward, true);
+    if (b.parts > 1) return launch<BF16, false, true, false, kDistillBackward, 0, true>(b, rows, stream);
+    return a.k > 256 && slots_lds(a, false) <= (size_t)kDistillLds ? launch<BF16, false, true, true, kDistillBackward, 0>(b, rows, stream) : launch<BF16, false, true, false, kDistillBackward, 0>(b, rows, stream);
+}
+
+template <bool BF16>
 hipError_t launch_forward(const DistillArgs& a, int64_t rows, hipStream_t stream)
 {
+    if (a.parts > 1) {
+        DistillArgs f = a;
+        if (!f.stats) f.stats = reinterpret_cast<double4*>(a.scratch + rows * (int64_t)distill_scratch_row(a.parts));
+        if (hipError_t e = launch<BF16, true, false, false, kDistillForward, 0, true>(f, rows, stream)) return e;
+        return a.grad ? launch_backward<BF16>(f, rows, stream) : hipSuccess;
+    }
     if (a.grad) {
         const bool slots = a.k > (BF16 ? (rows >= 512 ? 512 : 2048) : 256) && slots_lds(a, true) <= (size_t)kDistillLds;
         return slots ? launch<BF16, true, true, true, 512, BF16 ? 0 : 12>(a, rows, stream) : launch<BF16, true, true, false, 512, 12>(a, rows, stream);
     }
-    if (a.k > (BF16 ? 1536 : 768) && slots_lds(a, true) <= (size_t)kDistillLds) return launch<BF16, true, false, true, 512, 0>(a, rows, stream);
-    return rows >= 1024 && a.k <= 256 ? launch<BF16, true, false, false, 256, 0>(a, rows, stream) : launch<BF16, true, false, false, 512, 0>(a, rows, stream);
-}
-
-template <bool BF16>
-hipError_t launch_backward(const DistillArgs& a, int64_t rows, hipStream_t stream)
-{
-    return a.k > 256 && slots_lds(a, false) <= (size_t)kDistillLds ? launch<BF16, false, true, true, 1024, 0>(a, rows, stream) : launch<BF16, false, true, false, 1024, 0>(a, rows, stream);
+    if (a.k > (BF16 ? 1536 : 768) && slots_lds(a, true) <= (size_t)kDistillLds) return launch<BF16, true, false, true, kDistillForward, 0>(a, rows, stream);
+    return rows >= 1024 && a.k <= 256 ? launch<BF16, true, false, false, 256, 0>(a, rows, stream) : launch<BF16, true, false, false, kDistillForward, 0>(a, rows, stream);
 }
 
 }  // namespace
 
 hipError_t launch_distill(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature,
                           const int32_t* idx, const float* prob, const int32_t* count, int k, int tail,
-                          float* loss, float* accept, double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream)
+                          float* loss, float* accept, double* stats, const float* weight, void* grad, int64_t ld_grad, void* scratch, size_t scratch_bytes, hipStream_t stream)
 {
-    const DistillArgs a{logits, ld, V, temperature, idx, prob, count, k, tail, loss, accept, reinterpret_cast<double4*>(stats), weight, grad, ld_grad};
+    const size_t need = distill_scratch_bytes(dtype, n_rows, V);
+    const int parts = need && scratch && scratch_bytes >= need && (!grad || distill_splits(dtype == 1, n_rows, V, true)) ? distill_parts(dtype == 1, n_rows, V, kDistillForward, false) : 1;
+    const DistillArgs a{logits, ld, V, temperature, idx, prob, count, k, tail, loss, accept, reinterpret_cast<double4*>(stats), weight, grad, ld_grad, (char*)scratch, parts};
     if (n_rows == 0) return hipSuccess;
     return dtype == 1 ? launch_forward<true>(a, n_rows, stream) : launch_forward<false>(a, n_rows, stream);
 }
@@ -478,7 +532,7 @@ hipError_t launch_distill_grad(const void* logits, int dtype, int64_t ld, int n_
                                const double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream)
 {
     const DistillArgs a{logits, ld, V, temperature, idx, prob, count, k, tail, nullptr, nullptr,
-                        reinterpret_cast<double4*>(const_cast<double*>(stats)), weight, grad, ld_grad};
+                        reinterpret_cast<double4*>(const_cast<double*>(stats)), weight, grad, ld_grad, nullptr, 1};
     if (n_rows == 0) return hipSuccess;
     return dtype == 1 ? launch_backward<true>(a, n_rows, stream) : launch_backward<false>(a, n_rows, stream);
 }

@@ -441,10 +441,29 @@ hipError_t launch_sample(const void* logits, int dtype, int64_t ld, int n_rows, 
                          const float* temperature_rows, const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows,
                          const float* uniforms, int32_t* tok, float* prob, int32_t* count, float* lse, void* scratch, size_t scratch_bytes, hipStream_t stream);
 
-// ---- distillation on records (csrc/distill.hip)
+// ---- distillation on records (csrc/distill.hip).  Calls of few long rows give a row several workgroups, in scratch on a 16-byte boundary (forward: a word to arrive at and
+// two words a part for every row, and the statistics behind them, which a gradient in the same call, then a launch of its own, takes)
+constexpr int kDistillForward = 512, kDistillBackward = 1024, kDistillMostParts = 64;    // threads
+// Which, us, one workgroup per row / split: forward 64 rows of 64,000 bf16 (8000 vectors) 11.3 / 10.1, 96 of 32,000 fp32 (8000) 9.9 / 10.3, 128 of 151,936 fp32 (38,000) 27.5 / 20.8; with the
+// gradient, two launches then, 64 of 64,000 fp32 (16,000) 20.3 / 20.4, of 64,000 bf16 (8000) 17.5 / 19.4, 8 of 151,936 bf16 (19,000) 30.0 / 17.2, 64 of them 30.8 / 22.9, 96 30.9 / 30.8.
+inline bool distill_splits(bool bf16, int64_t rows, int V, bool gradient) {
+    const int vecs = row_vecs_max(bf16, V);
+    return rows >= 1 && V >= 1 && ((rows <= 64 && vecs >= (gradient ? 15000 : 8000)) || (!gradient && rows <= 128 && vecs >= 15000));
+}
+inline int distill_parts(bool bf16, int64_t rows, int V, int threads, bool gradient) {
+    if (!distill_splits(bf16, rows, V, gradient)) return 1;
+    const int64_t fit = 256 / rows, most = row_vecs_max(bf16, V) / (4 * threads);            // (four trips a part at least)
+    return (int)std::min<int64_t>(std::min(std::max<int64_t>(fit, 1), std::max<int64_t>(most, 1)), kDistillMostParts);
+}
+__host__ __device__ inline size_t distill_scratch_row(int parts) { return kArrivalStride + ((size_t)parts * 16 + 255) / 256 * 256; }
+inline size_t distill_scratch_bytes(int dtype, int64_t rows, int V) {
+    const int parts = distill_parts(dtype == 1, rows, V, kDistillForward, false);
+    return parts > 1 ? (size_t)rows * (distill_scratch_row(parts) + 32) : 0;
+}
 hipError_t launch_distill(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature,
                           const int32_t* idx, const float* prob, const int32_t* count, int k, int tail,
-                          float* loss, float* accept, double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream);
+                          float* loss, float* accept, double* stats, const float* weight, void* grad, int64_t ld_grad,
+                          void* scratch, size_t scratch_bytes, hipStream_t stream);
 hipError_t launch_distill_grad(const void* logits, int dtype, int64_t ld, int n_rows, int V, float temperature,
                                const int32_t* idx, const float* prob, const int32_t* count, int k, int tail,
                                const double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream);

@@ -241,8 +241,8 @@ PyObject* n_distill(PyObject*, PyObject* const* v, Py_ssize_t n) {
         auto z = a.ptr(); auto dt = a.i32(); auto ld = a.i64(); auto rows = a.i32(), V = a.i32(); auto T = a.f32();
         auto idx = a.ptr<int32_t>(); auto prob = a.ptr<float>(); auto count = a.ptr<int32_t>(); auto k = a.i32(), tail = a.i32();
         auto weight = a.ptr<float>(); auto loss = a.ptr<float>(); auto accept = a.ptr<float>(); auto stats = a.ptr<double>();
-        auto grad = a.ptr(); auto ldg = a.i64(); auto s = a.stream();
-        return [=] { return picospec_distill(z, dt, ld, rows, V, T, idx, prob, count, k, tail, weight, loss, accept, stats, grad, ldg, s); };
+        auto grad = a.ptr(); auto ldg = a.i64(); auto ws = a.buffer(); auto s = a.stream();
+        return [=] { return picospec_distill(z, dt, ld, rows, V, T, idx, prob, count, k, tail, weight, loss, accept, stats, grad, ldg, ws.p, ws.bytes, s); };
     });
 }
 
@@ -277,8 +277,11 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
         if (idx.dim() != 2 || idx.size(0) != rows) throw Refused{PICOSPEC_EINVAL};
         const auto f32 = z.options().dtype(at::kFloat);
         at::Tensor loss = at::empty({rows}, f32), accept = at::empty({rows}, f32), stats = at::empty({rows, 4}, z.options().dtype(at::kDouble));
+        const size_t bytes = V > 0 && V <= z.size(1) ? picospec_scratch_bytes(PICOSPEC_CALL_DISTILL, dt, (int32_t)rows, 0, (int32_t)V, 0) : 0;
+        const at::Tensor scratch = bytes ? at::empty({(int64_t)bytes}, z.options().dtype(at::kByte)) : at::Tensor();
         const int rc = picospec_distill(z.data_ptr(), dt, ld, (int32_t)rows, (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
-                                        (int)tail, nullptr, loss.data_ptr<float>(), accept.data_ptr<float>(), stats.data_ptr<double>(), nullptr, 0, c10::hip::getCurrentHIPStream().stream());
+                                        (int)tail, nullptr, loss.data_ptr<float>(), accept.data_ptr<float>(), stats.data_ptr<double>(), nullptr, 0,
+                                        bytes ? scratch.data_ptr() : nullptr, bytes, c10::hip::getCurrentHIPStream().stream());
         if (rc != PICOSPEC_OK) throw Refused{rc};
         ctx->save_for_backward({z, idx, prob, count, stats});
         ctx->saved_data["k"] = k;

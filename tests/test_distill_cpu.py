@@ -10,8 +10,8 @@ def B():
     return binding
 
 
-def _distill(B, z=FAKE, dt=0, ld=100, rows=2, V=100, T=1.0, rec=(FAKE,) * 3, k=10, tail=0, w=None, loss=FAKE, acc=None, stats=None, grad=None, ldg=100):
-    return B.lib.picospec_distill(z, dt, ld, rows, V, T, *rec, k, tail, w, loss, acc, stats, grad, ldg, None)
+def _distill(B, z=FAKE, dt=0, ld=100, rows=2, V=100, T=1.0, rec=(FAKE,) * 3, k=10, tail=0, w=None, loss=FAKE, acc=None, stats=None, grad=None, ldg=100, ws=None):
+    return B.lib.picospec_distill(z, dt, ld, rows, V, T, *rec, k, tail, w, loss, acc, stats, grad, ldg, ws, 0, None)
 
 
 def _grad(B, z=FAKE, dt=0, ld=100, rows=2, V=100, T=1.0, rec=(FAKE,) * 3, k=10, tail=0, w=None, stats=FAKE, grad=FAKE, ldg=100):
@@ -42,6 +42,7 @@ def test_misuse_is_refused(B, call):
 
 
 def test_outputs_are_required(B):
+    assert _distill(B, ws=FAKE + 4) == B.EWORKSPACE
     assert _distill(B, loss=None) == B.EINVAL
     assert _grad(B, stats=None) == B.EINVAL
     assert _grad(B, grad=None) == B.EINVAL

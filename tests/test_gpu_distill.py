@@ -151,6 +151,33 @@ def test_against_the_definition(gpu, ps, rows, V, k, T, pad, shift, ragged, dtyp
 
 @pytest.mark.parametrize("tail", [0, 1])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,k,shift", [(5, 90001, 30, 1), (20, 70003, 700, 3), (3, 200000, 4096, 0), (100, 130001, 12, 1), (60, 65001, 12, 1)])
+def test_split_rows(gpu, ps, rows, V, k, shift, dtype, tail):
+    """Few long rows: with scratch, without it and with too little of it, against the definition; masked parts, a row that is masked whole, one without entries."""
+    print(f"[case] distill split {rows} x {V} k={k} {dtype} tail={tail}", flush=True)
+    z, idx, prob, count = inputs(rows, V, k, dtype, 1.0, V, 2, shift)
+    z[1, : V // 2] = -math.inf
+    z[2] = -math.inf
+    count[0] = 0
+    weight = np.random.default_rng(V).uniform(0.5, 1.5, rows).astype(np.float32)
+    d = run_all(ps, z, V, 1.0, idx, prob, count, tail, weight)
+    loss, acc, grad, tol = reference(z.float().cpu().numpy(), V, 1.0, idx, prob, count, tail, weight)
+    dt, rec, w = 0 if dtype == torch.float32 else 1, record(ps, idx, prob, count), torch.from_numpy(weight).cuda()
+    need = ps.scratch_bytes(ps.CALL_DISTILL, dt, rows, 0, V, 0)
+    assert need == ps.workspace_bytes(ps.CALL_DISTILL, dt, rows, V, 0) and need > 0
+    for size in (0, max(need - 1, 0)):
+        ws = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+        lo, ac, g = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"), torch.zeros(rows, V, dtype=dtype, device="cuda")
+        assert ps.lib.picospec_distill(z.data_ptr(), dt, z.stride(0), rows, V, 1.0, rec.idx.data_ptr(), rec.prob.data_ptr(), rec.count.data_ptr(), k, tail, w.data_ptr(), lo.data_ptr(),
+                                       ac.data_ptr(), None, g.data_ptr(), V, ws.data_ptr() if size else None, size, None) == ps.OK
+        torch.cuda.synchronize()
+        check(lo, loss, E)
+        check(ac, acc, E)
+        check(g, grad, tol, dtype)
+
+
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("shift,T", [(1000.0, 1.0), (-3e7, 1e4), (2e9, 1.0), (0.0, 1e-3)])
 def test_logits_far_from_zero(gpu, ps, shift, T, dtype, tail):
     """Rows whose exponents are large: an offset that all logits share, beyond what the fused form of the exponents takes, a small temperature."""
