@@ -1395,10 +1395,11 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
             }
             good = found > 0;
             if (good && a_min > -__builtin_huge_val()) {
-                // (min-p against where top-p ends: clearly above, clearly not, or the careful way)
+                // min-p against where top-p ends, in bins: clearly above, then it alone decides (the first bin reaches up without end: nothing lies clearly above
+                // that); or else the list begins two bins earlier, so that whatever fails min-p is in it
                 const double x = ((double)pl.ref - ((double)M + a_min / kLog2e * (double)T)) * (double)per;
-                br.by_min_p = br.from >= 1.f && x < (double)br.from - 1.0;       // (the first bin reaches up without end)
-                good = br.by_min_p || x > (double)br.to + 1.0;
+                br.by_min_p = br.from >= 1.f && x < (double)br.from - 1.0;
+                if (!br.by_min_p && x < (double)br.to + 1.0) br.from = fmaxf(br.from - 2.f, 0.f);
             }
             if (!alone) {
                 if (tid == 0) {
@@ -1427,20 +1428,21 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                     block_scan_excl(mine, sh.red, above);
                     const double target = (double)p * total - above;
                     unsigned long long last = 0;
+                    int m = n;                                                   // (0: min-p leaves nothing of the list)
                     if (!(target > 0.0)) {
                     } else if (sort_list(n, sh)) {
                         double listed;
-                        const int m = kept_of_list(n, 1.0, target, -__builtin_huge_val(), w, sh, listed);
+                        m = kept_of_list(n, 1.0, target, a_min, w, sh, listed);
                         done = target <= listed;
-                        if (done) last = sh.list[m - 1];
+                        if (done && m > 0) last = sh.list[m - 1];
                     } else {
                         __syncthreads();
                         const unsigned long long listed = list_sum(n, 0ull, w, sh);
                         done = ldexp(target, kListShift) <= (double)listed;
                         if (done) last = select<true>(n, 0ull, ldexp(target, kListShift), w, sh);
                     }
-                    if (done) {
-                        cut = Cut{composite_value(last), composite_id(last), -__builtin_huge_val()};
+                    if (done && m > 0) {
+                        cut = Cut{composite_value(last), composite_id(last), a_min};
                         kept += list_to_segments<BF16>(rs, n, cut, w, true, sh);
                     }
                 }
