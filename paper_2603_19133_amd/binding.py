@@ -405,7 +405,7 @@ def sample(logits: torch.Tensor, V: int, uniforms: torch.Tensor, temperature=1.0
     """picospec_sample: one token per row of [rows, >=V] device logits.  Every setting is a number for all rows or a device tensor with one per
     row (float32, top_k int32)."""
     dt, ld, rows = _logits_2d(logits)
-    if uniforms.numel() != rows or uniforms.dtype != torch.float32 or not uniforms.is_contiguous():
+    if uniforms.numel() != rows or uniforms.dtype != torch.float32 or not uniforms.is_contiguous() or not uniforms.is_cuda:
         raise PicoSpecError(EINVAL)
     T, T_rows = _setting(temperature, rows, torch.float32)
     k, k_rows = _setting(top_k, rows, torch.int32)
@@ -426,10 +426,10 @@ class Distilled:
 
 
 def _distill_inputs(logits: torch.Tensor, rec: Compressed, weight: torch.Tensor | None):
-    """(dtype code, stride of a row, rows) of the logits; the record and the weights have to be theirs."""
-    dt, ld, rows = r = _logits_2d(logits)
-    if rec.idx.shape[0] != rows or (weight is not None and (weight.numel() != rows or weight.dtype != torch.float32 or not weight.is_contiguous())):
-        raise PicoSpecError(EINVAL)
+    """(dtype code, stride of a row, rows) of the logits; the record and the weights have to be theirs, without gaps."""
+    r = _nat.distill_inputs(logits, rec.idx, rec.prob, rec.count, rec.k, weight)
+    if r.__class__ is int:
+        raise PicoSpecError(r)
     return r
 
 
@@ -451,7 +451,8 @@ def distill_grad(logits: torch.Tensor, V: int, temperature: float, rec: Compress
     dt, ld, rows = _distill_inputs(logits, rec, weight)
     out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device) if out is None else out
     dt_g, ld_g, rows_g = _logits_2d(out)
-    if dt_g != dt or rows_g != rows or out.shape[1] < V or stats.numel() != 4 * rows or stats.dtype != torch.float64:
+    if dt_g != dt or rows_g != rows or out.shape[1] < V or stats.numel() != 4 * rows or stats.dtype != torch.float64 or not (
+            stats.is_contiguous() and stats.is_cuda):
         raise PicoSpecError(EINVAL)
     _check(_nat.distill_grad(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, stats, out, ld_g, _stream()))
     return out

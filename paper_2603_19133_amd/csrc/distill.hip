@@ -16,7 +16,6 @@ namespace picospec {
 
 namespace {
 
-
 // two (bf16) or one (fp32) values of -inf
 template <bool BF16> constexpr uint32_t kMaskedPair = BF16 ? 0xFF80FF80u : 0xFF800000u;
 
@@ -155,7 +154,7 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
     uint4 held[HELD ? HELD : 1];
     if constexpr (HELD > 0) {
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) if (i < trips) held[i] = load(i, Stream{});
+        for (int i = 0; i < HELD; ++i) held[i] = i < trips ? load(i, Stream{}) : make_uint4(0, 0, 0, 0);
     }
 
     // the record: entries tid, tid + kDT, .. (ids outside the vocabulary: no entry)

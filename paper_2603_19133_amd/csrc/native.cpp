@@ -33,6 +33,11 @@ struct Args {
         if (!THPVariable_Check(o)) throw BadArgument("a tensor or None is expected");
         return THPVariable_Unpack(o).data_ptr();
     }
+    const at::Tensor& tensor() {
+        PyObject* o = next();
+        if (!THPVariable_Check(o)) throw BadArgument("a tensor is expected");
+        return THPVariable_Unpack(o);
+    }
     template <class T> T* ptr() { return static_cast<T*>(ptr()); }
     int64_t i64() {
         const long long v = PyLong_AsLongLong(next());
@@ -268,13 +273,24 @@ int logits_code(const at::Tensor& t, int64_t& ld) {        // dtype code or erro
     return t.scalar_type() == at::kFloat ? PICOSPEC_F32 : PICOSPEC_BF16;
 }
 
+bool dense(const at::Tensor& t, at::ScalarType type, const at::Tensor& z) { return t.scalar_type() == type && t.is_contiguous() && t.device() == z.device(); }
+
+// the record's arrays are of the logits' rows and k entries each, without gaps
+void check_record(const at::Tensor& z, const at::Tensor& idx, const at::Tensor& prob, const at::Tensor& count, int64_t k) {
+    const int64_t rows = z.size(0);
+    for (const at::Tensor* t : {&idx, &prob})
+        if (t->dim() != 2 || t->size(0) != rows || t->size(1) != k) throw Refused{PICOSPEC_EINVAL};
+    if (count.dim() != 1 || count.size(0) != rows) throw Refused{PICOSPEC_EINVAL};
+    if (!dense(idx, at::kInt, z) || !dense(prob, at::kFloat, z) || !dense(count, at::kInt, z)) throw Refused{PICOSPEC_EINVAL};
+}
+
 struct DistillLoss : torch::autograd::Function<DistillLoss> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& z, const at::Tensor& idx, const at::Tensor& prob, const at::Tensor& count,
                                                   int64_t k, int64_t V, double T, int64_t tail) {
         int64_t ld;
         const int dt = logits_code(z, ld);
         const int64_t rows = z.size(0);
-        if (idx.dim() != 2 || idx.size(0) != rows) throw Refused{PICOSPEC_EINVAL};
+        check_record(z, idx, prob, count, k);
         const auto f32 = z.options().dtype(at::kFloat);
         at::Tensor loss = at::empty({rows}, f32), accept = at::empty({rows}, f32), stats = at::empty({rows, 4}, z.options().dtype(at::kDouble));
         const size_t bytes = V > 0 && V <= z.size(1) ? picospec_scratch_bytes(PICOSPEC_CALL_DISTILL, dt, (int32_t)rows, 0, (int32_t)V, 0) : 0;
@@ -320,11 +336,7 @@ PyObject* n_distill_loss(PyObject*, PyObject* const* v, Py_ssize_t n) {
     try {
         Args a{v, n};
         const at::Tensor* t[4];
-        for (auto& x : t) {
-            PyObject* o = a.next();
-            if (!THPVariable_Check(o)) throw BadArgument("a tensor is expected");
-            x = &THPVariable_Unpack(o);
-        }
+        for (auto& x : t) x = &a.tensor();
         const int64_t k = a.i64(), V = a.i64();
         const double T = a.f32();
         const int64_t tail = a.i64();
@@ -362,6 +374,33 @@ PyObject* n_rows2d(PyObject*, PyObject* o) {
     const int64_t rows = t.size(0);
     if (rows != 0 && t.stride(1) != 1) return PyLong_FromLong(PICOSPEC_EINVAL);
     return Py_BuildValue("(iLL)", dt, (long long)(rows ? t.stride(0) : t.size(1)), (long long)rows);
+    END_HANDLE_TH_ERRORS
+}
+
+// distill_inputs(logits, idx, prob, count, k, weight or None) -> rows2d(logits), or an error code where record or weights are not the rows'
+PyObject* n_distill_inputs(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    try {
+        Args a{v, n};
+        const at::Tensor &z = a.tensor(), &idx = a.tensor(), &prob = a.tensor(), &count = a.tensor();
+        const int64_t k = a.i64();
+        PyObject* const w = a.next();
+        a.done();
+        int64_t ld;
+        const int dt = logits_code(z, ld);
+        check_record(z, idx, prob, count, k);
+        if (w != Py_None) {
+            if (!THPVariable_Check(w)) throw BadArgument("a tensor or None is expected");
+            const at::Tensor& t = THPVariable_Unpack(w);
+            if (t.numel() != z.size(0) || !dense(t, at::kFloat, z)) throw Refused{PICOSPEC_EINVAL};
+        }
+        return Py_BuildValue("(iLL)", dt, (long long)ld, (long long)z.size(0));
+    } catch (const Refused& r) {
+        return PyLong_FromLong(r.code);
+    } catch (const BadArgument& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, e.what());
+        return nullptr;
+    }
     END_HANDLE_TH_ERRORS
 }
 
@@ -458,7 +497,7 @@ PyMethodDef methods[] = {
     FAST("round", n_round), FAST("verify_sample", n_verify_sample), FAST("verify_sample_static", n_verify_sample_static),
     FAST("sample_residual", n_sample_residual<picospec_sample_residual>), FAST("sample_residual_ws", n_sample_residual<picospec_sample_residual_ws>), FAST("row_stats", n_row_stats), FAST("compress_rejected", n_compress_rejected),
     FAST("resample_sparse", n_resample_sparse), FAST("pack_downlink", n_pack_downlink), FAST("unpack_downlink", n_unpack_downlink),
-    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("sample", n_sample), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("distill_loss", n_distill_loss), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
+    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("sample", n_sample), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("distill_loss", n_distill_loss), FAST("distill_inputs", n_distill_inputs), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
     {"rows2d", (PyCFunction)n_rows2d, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -9,6 +9,11 @@
 // Weights and their sums are fp64: where a prefix ends and which token is drawn are comparisons of sums over the whole vocabulary with tokens
 // of 10^-6 of it and less between their steps.  With fp32 weights (bf16 logits take few values, so their errors do not average out) sums are off by 10^-8 and
 // more of the row's mass, and one row in a hundred would end its prefix, or draw, an id off.  At 10^-12, the error of weight(), it is one in a million.
+//
+// What bounds it.  A row is read once (top-p alone: twice, the second time partly from the caches).  Plain draws, and top-p's second pass over fp32, are bound by the vector
+// ALU: a dozen fp64 operations an element (256 rows of 151,936 fp32, 156 MB, 38 us = 4.1 TB/s; a bare read 23).  Lists take a comparison an element and come near the memory
+// (512 rows of 100,000 fp32, top-k 50, 47 us = 4.4 TB/s); top-p alone is bound by the counting in LDS and the ALU (512 rows of 152,064 bf16 86 us; 256 of 128,256 56).  Few rows are
+// bound by latency: one of 32,000 with top-k and top-p 15 us, peek, pass, hand-over, ordering and draw behind each other.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -470,9 +475,10 @@ __device__ __attribute__((noinline)) void sample_careful(const void* logits, int
 //            masses above them and lists what lies in them.  (Counts, not masses: LDS adds a wave's 64 integers in 10 to 20 cycles, 64 floats in 195.)
 //            Elements that are likely behind the prefix are left out of the counts; a prefix that ends among them after all takes a third pass.
 // Whatever the peek promised is checked against the row (lists that are short or overflow, a prefix that does not end in its bins, +inf): such
-// rows, and records beyond the list, take the careful way.
+// rows, and a top_k beyond the list, take the careful way: up to ten passes of one workgroup (top_k = 9000, 151,936 fp32: one row 303 us, 256 rows 355).  Rows that are masked whole take it too, and
+// leave it after its first pass.
 enum Way : int { kCareful, kSum, kList, kHist };
-constexpr int kTopPList = 1024;
+constexpr int kTopPList = 1024;                   // (64 rows of 128,256 fp32 of that kind 41 us, spread ones, by the histogram, 58)
 constexpr double kHistFar = 3e-5;                 // relative error allowed for the histogram's sums (checked in fp64 behind it)
 constexpr float kHistPerNat = 64.f;
 

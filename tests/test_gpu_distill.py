@@ -320,3 +320,27 @@ def test_refusals_of_the_binding(gpu, ps):
         with pytest.raises(ps.PicoSpecError):
             call()
     torch.cuda.synchronize()
+
+
+def test_records_that_are_not_the_rows_are_refused(gpu, ps):
+    """Arrays with gaps, of another length, type or place: each is an error of both entry points, before anything runs."""
+    from paper_2603_19133_amd.training import distill_loss
+    z, idx, prob, count = inputs(6, 100, 8, torch.float32, 1.0, 2)
+    rec = record(ps, idx, prob, count)
+    of = lambda **kw: ps.Compressed(**{**dict(idx=rec.idx, prob=rec.prob, count=rec.count, mass=rec.mass, lse=rec.lse, k=8), **kw})       # noqa: E731
+    bad = [of(idx=rec.idx[:, :5], prob=rec.prob[:, :5], k=5), of(k=5), of(k=9), of(prob=rec.prob[:, :5]), of(prob=rec.prob[:3]), of(count=rec.count[:3]),
+           of(idx=rec.idx.long()), of(prob=rec.prob.double()), of(count=rec.count.long()), of(idx=rec.idx.cpu()), of(count=rec.count.cpu()),
+           of(prob=torch.rand(8, 6, device="cuda").t())]
+    for r in bad:
+        with pytest.raises(ps.PicoSpecError):
+            ps.distill(z, 100, 1.0, r)
+        with pytest.raises(ps.PicoSpecError):
+            distill_loss(z, r, 100, 1.0)
+    stats = ps.distill(z, 100, 1.0, rec).stats
+    for kw in (dict(weight=torch.ones(6)), dict(weight=torch.ones(12, device="cuda")[::2])):
+        with pytest.raises(ps.PicoSpecError):
+            ps.distill_grad(z, 100, 1.0, rec, stats, **kw)
+    for s in (stats.cpu(), torch.zeros(6, 8, dtype=torch.float64, device="cuda")[:, ::2]):
+        with pytest.raises(ps.PicoSpecError):
+            ps.distill_grad(z, 100, 1.0, rec, s)
+    torch.cuda.synchronize()

@@ -198,6 +198,20 @@ def test_few_ids_far_above_the_rest(gpu, ps, top_p, min_p, rows, dtype):
     compare(ps.sample(z, V, u, top_p=top_p, min_p=min_p), z, 1.0, 0, top_p, min_p, u)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(7, 60001), (56, 40000), (280, 20000)])
+def test_min_p_near_the_end_of_a_prefix(gpu, ps, rows, V, dtype):
+    """Spread rows whose min-p lies a little above, at, or below the weight of the last entry that top-p keeps."""
+    z, u = rows_of(rows, V, dtype, "flat", 77 + rows)
+    v = torch.sort(z.double(), dim=1, descending=True).values
+    w = torch.exp(v - v[:, :1])
+    mass = torch.cumsum(w, 1)
+    end = torch.gather(w, 1, (mass < 0.9 * mass[:, -1:]).sum(1, keepdim=True))[:, 0]
+    factor = torch.tensor([0.25, 0.9, 0.985, 0.9999, 1.0001, 1.015, 1.1, 4.0], dtype=torch.float64, device=z.device)
+    min_p = (end * factor[torch.arange(rows, device=z.device) % 8]).float()
+    compare(ps.sample(z, V, u, top_p=0.9, min_p=min_p), z, 1.0, 0, 0.9, min_p, u)
+
+
 @pytest.mark.parametrize("top_p", [0.0, 0.9])
 def test_the_ends_of_the_uniforms(gpu, ps, top_p):
     """u = 0 draws the first kept id, the largest u below 1 the last; outside [0, 1): the first and the last."""
@@ -254,7 +268,7 @@ def test_same_bits_streams_and_graph(gpu, ps):
 def test_refusals_of_the_binding(gpu, ps):
     z, u = rows_of(4, 100, torch.float32, "normal", 1)
     f = lambda *v: torch.tensor(v, device="cuda")
-    for call in (lambda: ps.sample(z, 100, u[:3]), lambda: ps.sample(z, 100, u.double()), lambda: ps.sample(z, 101, u), lambda: ps.sample(z[:, ::2], 50, u),
+    for call in (lambda: ps.sample(z, 100, u[:3]), lambda: ps.sample(z, 100, u.double()), lambda: ps.sample(z, 100, u.cpu()), lambda: ps.sample(z, 101, u), lambda: ps.sample(z[:, ::2], 50, u),
                  lambda: ps.sample(z.half(), 100, u), lambda: ps.sample(z, 100, u, temperature=-1.0), lambda: ps.sample(z, 100, u, min_p=2.0),
                  lambda: ps.sample(z, 100, u, temperature=f(1.0, 1.0, 1.0)), lambda: ps.sample(z, 100, u, top_k=f(1.0, 1.0, 1.0, 1.0)),
                  lambda: ps.sample(z, 100, u, top_p=u.cpu())):
