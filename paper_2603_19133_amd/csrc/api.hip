@@ -72,6 +72,28 @@ int64_t max_load_end(int which, int V, int o)
                 for (int part = 0; part < parts; ++part)
                     for (int lane = 0; lane < 64; ++lane)
                         end = std::max(end, buffer_lane_read_end(size, (int64_t)split_block(j, w, part, parts) * 1024, (int64_t)lane * 16));
+    } else if (which == PICOSPEC_CALL_SAMPLE) {
+        const int n_blocks = (nq + 63) / 64, blocks = kSamplePeek / (64 * N), segments = stats_segments(nq), waves = kSampleThreads / 64;
+        for (int i = 0; i < blocks; ++i)
+            for (int lane = 0; lane < 64; ++lane)
+                end = std::max(end, buffer_lane_read_end(size, 0, ((int64_t)peek_group_first(i, n_blocks, blocks) + lane) * 16));
+        for (int parts : {1, 2, kSampleMostParts})                              // ... and the segments, one trip further than the row
+            for (int part = 0; part < parts; ++part)
+                for (int w = 0; w < waves; ++w)
+                    for (int trip = 0; trip == 0 || shared_segment(part, w, trip - 1, parts, waves) < segments; ++trip)
+                        for (int j = 0; j < kSplitStatsNV; ++j)
+                            for (int lane = 0; lane < 64; ++lane)
+                                end = std::max(end, buffer_lane_read_end(size, (int64_t)stats_group_first(shared_segment(part, w, trip, parts, waves), j) * 16, (int64_t)lane * 16));
+        for (int s = 0; s < segments; ++s)                                      // ... and the one that is read again
+            for (int tid = 0; tid < 64 * kSplitStatsNV; ++tid)
+                end = std::max(end, buffer_lane_read_end(size, 0, ((int64_t)stats_group_first(s, 0) + tid) * 16));
+    } else if (which == PICOSPEC_CALL_DISTILL) {
+        for (int threads : {256, kDistillForward, kDistillBackward}) {
+            const int trips = (nq + threads - 1) / threads;
+            for (int trip = 0; trip <= std::max(trips, kDistillMostHeld) + kDistillAhead; ++trip)
+                for (int tid = 0; tid < threads; ++tid)
+                    end = std::max(end, buffer_lane_read_end(size, (int64_t)trip_group_first(trip, threads) * 16, (int64_t)tid * 16));
+        }
     } else {
         using G = ResidualGeom<BF16>;
         const int n_tiles = (L + kResidualTile - 1) / kResidualTile;
@@ -621,7 +643,7 @@ size_t picospec_one_launch_bytes(int which_call, int dtype, int32_t n_draft, int
 
 int64_t picospec_max_load_byte(int which_call, int dtype, int32_t V, int32_t misalign_bytes)
 {
-    if (which_call != PICOSPEC_CALL_COMPRESS && which_call != PICOSPEC_CALL_SAMPLE_RESIDUAL) return -1;
+    if (which_call != PICOSPEC_CALL_COMPRESS && which_call != PICOSPEC_CALL_SAMPLE_RESIDUAL && which_call != PICOSPEC_CALL_SAMPLE && which_call != PICOSPEC_CALL_DISTILL) return -1;
     if (dtype != PICOSPEC_F32 && dtype != PICOSPEC_BF16) return -1;
     const int esz = dtype == PICOSPEC_F32 ? 4 : 2;
     if (V < 1 || V > kMaxV || misalign_bytes < 0 || misalign_bytes > 15 || misalign_bytes % esz) return -1;

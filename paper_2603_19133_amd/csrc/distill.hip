@@ -113,7 +113,7 @@ template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, bool SPLIT, int
 __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
 {
     constexpr int N = Vec<BF16>::N, G = 2, kDW = kDT / kWave;    // G: vectors per step
-    static_assert(HELD % G == 0 && (!SPLIT || (HELD == 0 && !SLOTS && FWD != GRAD)), "whole steps; split rows in the plainest form");
+    static_assert(HELD % G == 0 && HELD <= kDistillMostHeld && G + 1 <= kDistillAhead && (!SPLIT || (HELD == 0 && !SLOTS && FWD != GRAD)), "whole steps; split rows in the plainest form");
     __shared__ double sh[5 * kDW];
     extern __shared__ uint32_t on_record[];                      // (TAIL && FWD) || SLOTS: bit o + id
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
 
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)rv.base, 0, nq * 16, 0x00020000);
     auto load = [&](int i, auto aux) {                           // vector i * kDT + tid; behind the row: zero
-        const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, i * (kDT * 16), decltype(aux)::value);
+        const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(rsrc, tid * 16, trip_group_first(i, kDT) * 16, decltype(aux)::value);
         return make_uint4(t.x, t.y, t.z, t.w);
     };
     using Stream = std::integral_constant<int, 2>;               // (read once: non-temporal)

@@ -76,6 +76,14 @@ __host__ __device__ inline int stats_group_first(int seg, int j) { return (seg *
 // segments of a row of `nq` vectors, and the workgroups that take them
 __host__ __device__ inline int stats_segments(int nq) { return (nq + 64 * kSplitStatsNV - 1) / (64 * kSplitStatsNV); }
 __host__ __device__ inline int stats_parts(int segments) { return (segments + 4 * kSplitStatsSpw - 1) / (4 * kSplitStatsSpw); }
+// One token per row (sample.hip): segments as above, taken by shared_segment, and beforehand a look at one row in `blocks` blocks of 64 vectors, taken evenly
+// from its n_blocks, or at all of them.  First vector of block i.
+constexpr int kSamplePeek = 8192;                             // elements that are looked at
+__host__ __device__ inline int peek_group_first(int i, int n_blocks, int blocks) { return (n_blocks <= blocks ? i : (int)((int64_t)i * n_blocks / blocks)) * 64; }
+// Distillation (distill.hip): first vector of a trip of a workgroup of `threads`, a vector a thread; kDistillAhead: trips behind the row's last, or behind those that are held in
+// registers, that are asked for
+constexpr int kDistillAhead = 3, kDistillMostHeld = 12;
+__host__ __device__ inline int trip_group_first(int trip, int threads) { return trip * threads; }
 // vectors of a row of V elements that lies off the 16-byte boundary, the most it can span: what a launch is sized for
 __host__ __device__ inline int row_vecs_max(bool bf16, int V) { return (int)(((int64_t)V * (bf16 ? 2 : 4) + 15) / 16) + 1; }
 

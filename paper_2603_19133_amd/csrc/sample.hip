@@ -27,7 +27,7 @@ constexpr int kSegs = kMaxV / 1024 + 2;           // segments of the longest row
 constexpr int kSegsPer = (kSegs + kST - 1) / kST;
 constexpr int kBins = 2048;                       // of a histogram over the row
 constexpr int kListBins = 1024;                   // ... over a list
-constexpr int kPeek = 8192;                       // elements that are looked at before the row is streamed
+constexpr int kPeek = kSamplePeek;                // elements that are looked at before the row is streamed
 constexpr double kLog2e = 1.4426950408889634;
 constexpr float kFloatMax = 3.4028234663852886e38f;
 
@@ -102,8 +102,13 @@ struct RowStream {
         n_seg = stats_segments(nq);
         rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)rv.base, 0, nq * 16, 0x00020000);
     }
-    __device__ __forceinline__ uint4 vec(int q) const {                      // (a vector behind the row reads as zero and touches no memory)
-        const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(rsrc, q * 16, 0, 0);
+    // (a vector behind the row reads as zero and touches no memory)
+    __device__ __forceinline__ uint4 peeked(int i, int n_blocks, int blocks) const {
+        const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (peek_group_first(i, n_blocks, blocks) + (int)(threadIdx.x & (kWave - 1))) * 16, 0, 0);
+        return make_uint4(t.x, t.y, t.z, t.w);
+    }
+    __device__ __forceinline__ uint4 of_segment(int s) const {               // vector tid of a segment
+        const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (stats_group_first(s, 0) + (int)threadIdx.x) * 16, 0, 0);
         return make_uint4(t.x, t.y, t.z, t.w);
     }
     __device__ __forceinline__ void load(int s, uint4 (&raw)[kSplitStatsNV]) const {
@@ -125,13 +130,13 @@ struct RowStream {
     }
     __device__ __forceinline__ int first_id(int q) const { return q * Vec<BF16>::N - rv.o; }
     // f(s, raw) for every segment of workgroup `part` of `parts`, a wave each, the next one's loads in flight; `cur` holds the first one's vectors (first_of)
-    __device__ __forceinline__ void first_of(int part, uint4 (&cur)[kSplitStatsNV]) const { load(part * kSW + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave), cur); }
+    __device__ __forceinline__ int segment(int part, int trip, int parts) const { return shared_segment(part, (int)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave), trip, parts, kSW); }
+    __device__ __forceinline__ void first_of(int part, uint4 (&cur)[kSplitStatsNV]) const { load(segment(part, 0, 1), cur); }
     template <class F>
     __device__ __forceinline__ void each_from(uint4 (&cur)[kSplitStatsNV], const F& f, int part, int parts) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         uint4 next[kSplitStatsNV];
-        for (int s = part * kSW + wave; s < n_seg; s += parts * kSW) {
-            load(s + parts * kSW, next);
+        for (int trip = 0, s = segment(part, 0, parts); s < n_seg; s = segment(part, ++trip, parts)) {
+            load(segment(part, trip + 1, parts), next);
             f(s, cur);
 #pragma unroll
             for (int j = 0; j < kSplitStatsNV; ++j) cur[j] = next[j];
@@ -238,10 +243,10 @@ __device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w
     if (tid == 0) { sh.at = INT32_MAX; sh.last = -1; }
     // that segment again, a vector a thread
     double kept[N], in_vec = 0.0;
-    const int q = s * (64 * kSplitStatsNV) + tid;
+    const int q = stats_group_first(s, 0) + tid;
     const bool have = s >= 0 && tid < 64 * kSplitStatsNV;
     float v[N];
-    rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, s, v);
+    rs.values(have ? rs.of_segment(s) : make_uint4(0, 0, 0, 0), q, s, v);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         const float z = cleaned(v[e]);
@@ -308,10 +313,10 @@ __device__ __forceinline__ int id_of_tie(const RowStream<BF16>& rs, const uint32
     if (tid == 0) sh.at = INT32_MAX;
     __syncthreads();
     if (s >= 0) {
-        const int q = s * (64 * kSplitStatsNV) + tid;
+        const int q = stats_group_first(s, 0) + tid;
         const bool have = tid < 64 * kSplitStatsNV;
         float v[N];
-        rs.values(have ? rs.vec(q) : make_uint4(0, 0, 0, 0), q, s, v);
+        rs.values(have ? rs.of_segment(s) : make_uint4(0, 0, 0, 0), q, s, v);
         unsigned long long mine = 0, all;
 #pragma unroll
         for (int e = 0; e < N; ++e) mine += have && cleaned(v[e]) == t;
@@ -496,8 +501,8 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         // (rows of fewer blocks than that: each once)
-        const int i = j * kSW + wave, blk = n_blocks <= BLOCKS ? i : (int)((int64_t)i * n_blocks / BLOCKS), q = blk * kWave + lane;
-        rs.values(rs.vec(q), q, 0, v[j]);
+        const int i = j * kSW + wave;
+        rs.values(rs.peeked(i, n_blocks, BLOCKS), peek_group_first(i, n_blocks, BLOCKS) + lane, 0, v[j]);
     }
     float mx = kNegInf;
 #pragma unroll

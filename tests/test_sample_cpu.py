@@ -39,3 +39,13 @@ def test_a_call_of_no_rows_does_nothing(B):
     assert _sample(B, z=None, rows=0, u=None, outs=(None,) * 4) == B.OK
     assert _sample(B, z=None, rows=0, T=0.0, u=None, outs=(None,) * 4) == B.OK        # (greedy)
     assert _sample(B, z=None, rows=0, T=NAN, p=NAN, m=NAN, per_row=(FAKE, None, FAKE, FAKE), u=None, outs=(None,) * 4) == B.OK   # (per row)
+
+
+def test_streaming_loads_stay_inside_the_row(B):
+    """The kernels' own rule of what their row loads address, evaluated on the host over every lane, look-ahead included."""
+    for dtype, esz in ((B.F32, 4), (B.BF16, 2)):
+        for V in (1, 2, 7, 8, 9, 255, 256, 257, 1025, 2047, 4096, 8191, 8193, 16384, 16387, 32000, 65537, 131073, 151936, (1 << 20) - 1, 1 << 20):
+            for mis in range(0, 16, esz):
+                end = B.max_load_byte(B.CALL_SAMPLE, dtype, V, mis)
+                assert V * esz - 15 <= end <= (mis + V * esz + 15) // 16 * 16 - mis, (dtype, V, mis, end)
+    assert B.max_load_byte(B.CALL_SAMPLE, B.F32, 0, 0) == -1 and B.max_load_byte(B.CALL_SAMPLE, B.BF16, 100, 3) == -1
