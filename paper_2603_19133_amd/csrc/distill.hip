@@ -19,6 +19,8 @@ namespace {
 // two (bf16) or one (fp32) values of -inf
 template <bool BF16> constexpr uint32_t kMaskedPair = BF16 ? 0xFF80FF80u : 0xFF800000u;
 
+enum Slots : int { kNone, kEntries, kHalves };  // of a long record, in LDS
+
 struct DistillArgs {
     const void* logits; int64_t ld; int V; float T;
     const int32_t* idx; const float* prob; const int32_t* count; int k, tail;
@@ -103,19 +105,23 @@ __device__ __forceinline__ void store_one(char* grad_row, int x, float g)
 // exponential per element (the product inside is exact, so the error is that of (z - M) c).  r moves up, and the lanes' sums are rescaled, only when an element
 // lies more than 2^64 above it.  Rows with |M c| >= 2^24, where r is no integer near M c any more, take (z - M) c and read the row once more.
 //
-// What the record's entries need of the row, and the row of them:
-//   SLOTS   The record lies in LDS in the order of its ids: a bit per element, the number of bits in front of every 32, and the entries' p.  The streaming finds the
+// What the record's entries need of the row, and the row of them (SLOTS):
+//   entries The record lies in LDS in the order of its ids: a bit per element, the number of bits in front of every 32, and the entries' p.  The streaming finds the
 //           entry of a marked element by counting bits; it leaves the element's logit there (FWD) and writes its gradient in place (GRAD).
-//   else    The logits are gathered, and the entries' gradients written over what the streaming left in their places: less to prepare, but every entry touches a line
+//   halves  The same without gradient, for bf16 records with the tail: a marked element's half of its vector goes to the slot of the half's first mark, as it came from
+//           memory (two writes a vector instead of one for each of its elements that some lane has marked), and the entries find their logits in them behind the stream.
+//   none    The logits are gathered, and the entries' gradients written over what the streaming left in their places: less to prepare, but every entry touches a line
 //           of the row each way.  For short records, and for vocabularies whose marks do not fit (kDistillLds).
 // SPLIT: a row's workgroups take consecutive trips of it; forward, the last of them to arrive adds their sums up and goes on with the record.
-template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, bool SPLIT, int kDT, int HELD>
+template <bool BF16, bool FWD, bool GRAD, bool TAIL, int SLOTS, bool SPLIT, int kDT, int HELD>
 __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
 {
     constexpr int N = Vec<BF16>::N, G = 2, kDW = kDT / kWave;    // G: vectors per step
     static_assert(HELD % G == 0 && HELD <= kDistillMostHeld && G + 1 <= kDistillAhead && (!SPLIT || (HELD == 0 && !SLOTS && FWD != GRAD)), "whole steps; split rows in the plainest form");
+    constexpr bool HALVES = SLOTS == kHalves;
+    static_assert(!HALVES || (FWD && !GRAD), "halves of vectors serve what only reads");
     __shared__ double sh[5 * kDW];
-    extern __shared__ uint32_t on_record[];                      // (TAIL && FWD) || SLOTS: bit o + id
+    extern __shared__ __attribute__((aligned(8))) uint32_t on_record[];   // (TAIL && FWD) || SLOTS: bit o + id
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int parts = SPLIT ? a.parts : 1, part = SPLIT ? (int)(blockIdx.x % (unsigned)parts) : 0;
     const int64_t row = SPLIT ? blockIdx.x / (unsigned)parts : blockIdx.x;
@@ -170,6 +176,7 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
     uint16_t* const in_front = reinterpret_cast<uint16_t*>(on_record + words);
     float* const slot_p = reinterpret_cast<float*>(on_record + words + (words + 1) / 2);
     float* const slot_z = slot_p + a.k;
+    uint2* const slot_half = reinterpret_cast<uint2*>(on_record + (words + (words + 1) / 2 + 1) / 2 * 2);
     int n_slots = 0;
     Entry own{-1, 0.f, 0.f};
     if constexpr (!SLOTS) {
@@ -184,7 +191,7 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             id[j] = id_of(j * kDT + tid);
-            p[j] = SLOTS && id[j] >= 0 ? a.prob[row * a.k + j * kDT + tid] : 0.f;
+            p[j] = SLOTS == kEntries && id[j] >= 0 ? a.prob[row * a.k + j * kDT + tid] : 0.f;
         }
         for (int w = tid; w < words; w += kDT) on_record[w] = 0u;
         __syncthreads();
@@ -205,13 +212,15 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
             for (int w = 0; w < kDW; ++w) { if (w < wave) before += wave_sums[w]; n_slots += wave_sums[w]; }
             for (int w = first; w < end; ++w) { in_front[w] = (uint16_t)before; before += __builtin_popcount(on_record[w]); }
             __syncthreads();
+            if constexpr (SLOTS == kEntries) {
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-                if (id[j] >= 0) {
-                    const int v = rv.o + id[j];
-                    slot_p[in_front[v >> 5] + __builtin_popcount(on_record[v >> 5] & ((1u << (v & 31)) - 1u))] = p[j];
-                }
-            __syncthreads();
+                for (int j = 0; j < PER; ++j)
+                    if (id[j] >= 0) {
+                        const int v = rv.o + id[j];
+                        slot_p[in_front[v >> 5] + __builtin_popcount(on_record[v >> 5] & ((1u << (v & 31)) - 1u))] = p[j];
+                    }
+                __syncthreads();
+            }
         }
     }
     // marks of vector q, and the slot of the first of them
@@ -221,8 +230,12 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
         if constexpr (SLOTS) slot = in_front[v >> 5] + __builtin_popcount(word & ((1u << at) - 1u));
         return (word >> at) & ((1u << N) - 1u);
     };
+    Entry mine[HALVES ? kMaxK / kDT : 1];                          // HALVES: entries tid, tid + kDT, ..
     auto each_entry = [&](auto f) {
-        if constexpr (SLOTS) {
+        if constexpr (HALVES) {
+#pragma unroll
+            for (int j = 0; j < kMaxK / kDT; ++j) if (mine[j].id >= 0) f(mine[j]);
+        } else if constexpr (SLOTS) {
             for (int s = tid; s < n_slots; s += kDT) f(Entry{0, slot_p[s], slot_z[s]});
         } else {
             if (own.id >= 0) f(own);
@@ -257,9 +270,15 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
 #pragma unroll
                 for (int e = 0; e < N; ++e) t[e] = (vm >> e) & 1u ? t[e] : kNegInf;
             }
+            if constexpr (TAIL && !SLOTS) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) mx = fmaxf(mx, t[e]);
-            if constexpr (SLOTS) {
+                for (int e = 0; e < N; ++e) mx = fmaxf(mx, t[e]);
+            }
+            if constexpr (HALVES) {
+                const unsigned in = q < nq ? out : 0u, low = in & ((1u << (N / 2)) - 1u);
+                if (low != 0u) slot_half[slot] = make_uint2(raw.x, raw.y);
+                if (in != low) slot_half[slot + __builtin_popcount(low)] = make_uint2(raw.z, raw.w);
+            } else if constexpr (SLOTS) {
                 const unsigned in = q < nq ? out : 0u;
                 if (__ballot(in != 0u)) {
 #pragma unroll
@@ -268,7 +287,7 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
             }
             if constexpr (TAIL) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) {                                  // (the bit as a mask over the value: two instructions)
+                for (int e = 0; e < N; ++e) {                                  // (the bit as a mask over the value)
                     const uint32_t on = (uint32_t)((int)(out << (31 - e)) >> 31);
                     t[e] = __uint_as_float((on & 0xFF800000u) | (~on & __float_as_uint(t[e])));
                 }
@@ -286,6 +305,7 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
             float bm = v[0];
 #pragma unroll
             for (int e = 1; e < G * N; ++e) bm = fmaxf(bm, v[e]);
+            if constexpr (!TAIL || SLOTS) mx = fmaxf(mx, bm);                  // (SLOTS: the record's come behind the stream)
             if (__ballot(bm * c > r + 64.f)) {                                // (uniform; the first step, and outliers)
                 const float rn = ceilf(wave_max(bm) * c);
                 if (rn > r) { s *= __builtin_amdgcn_exp2f(r - rn); r = rn; }   // (r = -inf: s is 0 and stays 0)
@@ -312,6 +332,23 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
                 for (int g = 0; g < G; ++g) cur[g] = nxt[g];
             }
         }
+        if constexpr (SLOTS) __syncthreads();                     // (the logits are in their slots)
+        if constexpr (HALVES) {
+#pragma unroll
+            for (int j = 0; j < kMaxK / kDT; ++j) {
+                mine[j].id = id_of(j * kDT + tid);
+                mine[j].p = mine[j].id >= 0 ? a.prob[row * a.k + j * kDT + tid] : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < kMaxK / kDT; ++j) {
+                if (mine[j].id < 0) continue;
+                const int v = rv.o + mine[j].id, first = v & 31 & ~(N / 2 - 1);
+                const int slot = in_front[v >> 5] + __builtin_popcount(on_record[v >> 5] & ((1u << first) - 1u));
+                const uint32_t bits = BF16 ? (uint32_t)reinterpret_cast<const uint16_t*>(&slot_half[slot])[v % (N / 2)] << 16 : reinterpret_cast<const uint32_t*>(&slot_half[slot])[v % (N / 2)];
+                mine[j].z = __uint_as_float(bits);
+            }
+        }
+        if constexpr (TAIL && SLOTS) each_entry([&](const Entry& e) { mx = fmaxf(mx, e.z); });
         const float wm = wave_max(mx);
         if (lane == 0) sh[wave] = (double)wm;
         __syncthreads();
@@ -349,7 +386,6 @@ __global__ __launch_bounds__(kDT) void distill_kernel(const DistillArgs a)
             sums[0] = wave_sum(m == M ? s_part : s_part * exp2_split(((double)m - (double)M) * (double)c));
             if (tid != 0) sums[0] = 0.0;
         }
-        if constexpr (SLOTS) __syncthreads();                     // (the logits are in their slots)
         each_entry([&](const Entry& e) {
             if constexpr (TAIL) sums[4] += exp_emit(e.z, M, c64);
             if (e.p > 0.f) {
@@ -458,9 +494,9 @@ constexpr int kDistillLds = 80 * 1024;            // two workgroups per CU: slot
 constexpr size_t kDistillMostLds = 144 * 1024;    // the marks of the longest row alone
 inline size_t mark_words(const DistillArgs& a) { return ((size_t)a.V + 8 + 31) / 32; }
 inline size_t marks_lds(const DistillArgs& a) { return mark_words(a) * 4; }
-inline size_t slots_lds(const DistillArgs& a, bool forward) { return (mark_words(a) + (mark_words(a) + 1) / 2 + (size_t)a.k * (forward ? 2 : 1)) * 4; }
+inline size_t slots_lds(const DistillArgs& a, bool forward) { return ((mark_words(a) + (mark_words(a) + 1) / 2 + 1) / 2 * 2 + (size_t)a.k * (forward ? 2 : 1)) * 4; }
 
-template <bool BF16, bool FWD, bool GRAD, bool TAIL, bool SLOTS, bool SPLIT, int THREADS, int HELD>
+template <bool BF16, bool FWD, bool GRAD, bool TAIL, int SLOTS, bool SPLIT, int THREADS, int HELD>
 hipError_t launch_one(const DistillArgs& a, int64_t rows, size_t lds, hipStream_t stream)
 {
     const auto kernel = distill_kernel<BF16, FWD, GRAD, TAIL, SLOTS, SPLIT, THREADS, HELD>;
@@ -472,7 +508,7 @@ hipError_t launch_one(const DistillArgs& a, int64_t rows, size_t lds, hipStream_
     return hipGetLastError();
 }
 
-template <bool BF16, bool FWD, bool GRAD, bool SLOTS, int THREADS, int HELD, bool SPLIT = false>
+template <bool BF16, bool FWD, bool GRAD, int SLOTS, int THREADS, int HELD, bool SPLIT = false>
 hipError_t launch(const DistillArgs& a, int64_t rows, hipStream_t stream)
 {
     const size_t lds = SLOTS ? slots_lds(a, FWD) : FWD && a.tail ? marks_lds(a) : 0;
@@ -480,8 +516,10 @@ hipError_t launch(const DistillArgs& a, int64_t rows, hipStream_t stream)
 }
 
 // Which way, by rows, type and record length (us, 1500 rows of 128,256 unless said):
-//   loss      gathered up to 768 entries (fp32) or 1536 (bf16, where the marks cost the vector ALU more than the memory takes), slots beyond: 300 entries 134 / 135
-//             fp32, 75 / 94 bf16; 1000 147 / 137, 91 / 101; 2500 184 / 149, 126 / 107.  512 threads; gathered calls of 1024 rows and more with up to 256 entries 256: 4096 rows of
+//   loss      gathered up to 768 entries (fp32 and with the tail) or 1536 (bf16 without, where the marks cost the vector ALU more than the memory takes), slots beyond: 300 entries
+//             134 / 135 fp32, 75 / 94 bf16; 1000 147 / 137, 91 / 101; 2500 184 / 149, 126 / 107.  Slots of halves, bf16 with the tail, gathered or by entries / so: 1088 rows of
+//             152,064, 700 entries 78.6 / 76.8, 1024 82.5 / 78, 2048 97 / 82, 2000 rows of 32,000, 700 46.7 / 47.4, 1024 53.6 / 48.5, 2048 58 / 54; without the tail (2048 entries 47.5 / 55)
+//             and in fp32 (1500 rows of 100,000 114 / 117) they lose.  512 threads; gathered calls of 1024 rows and more with up to 256 entries 256: 4096 rows of
 //             32,000 bf16 50 against 57, 1024 of 128,256 fp32 86 against 93; of 256 rows of 151,936 fp32 50 against 33.
 //   gradient  slots beyond 256 entries: 300 297 / 292, 147 / 144; 2500 418 / 294, 239 / 148.  1024 threads: 3000 rows of 100,000 450 against 469 with 512 (fp32), 233 against 250.
 //   both      slots beyond 256 entries (fp32: 300 352 / 331, 2500 538 / 348), beyond 512 (bf16: 300 169 / 177, 1000 211 / 183, 2500 315 / 196), where there are fewer than 512
@@ -492,8 +530,8 @@ hipError_t launch_backward(const DistillArgs& a, int64_t rows, hipStream_t strea
 {
     DistillArgs b = a;
     b.parts = distill_parts(BF16, rows, a.V, kDistillBackward, true);
-    if (b.parts > 1) return launch<BF16, false, true, false, kDistillBackward, 0, true>(b, rows, stream);
-    return a.k > 256 && slots_lds(a, false) <= (size_t)kDistillLds ? launch<BF16, false, true, true, kDistillBackward, 0>(b, rows, stream) : launch<BF16, false, true, false, kDistillBackward, 0>(b, rows, stream);
+    if (b.parts > 1) return launch<BF16, false, true, kNone, kDistillBackward, 0, true>(b, rows, stream);
+    return a.k > 256 && slots_lds(a, false) <= (size_t)kDistillLds ? launch<BF16, false, true, kEntries, kDistillBackward, 0>(b, rows, stream) : launch<BF16, false, true, kNone, kDistillBackward, 0>(b, rows, stream);
 }
 
 template <bool BF16>
@@ -502,15 +540,18 @@ hipError_t launch_forward(const DistillArgs& a, int64_t rows, hipStream_t stream
     if (a.parts > 1) {
         DistillArgs f = a;
         if (!f.stats) f.stats = reinterpret_cast<double4*>(a.scratch + rows * (int64_t)distill_scratch_row(a.parts));
-        if (hipError_t e = launch<BF16, true, false, false, kDistillForward, 0, true>(f, rows, stream)) return e;
+        if (hipError_t e = launch<BF16, true, false, kNone, kDistillForward, 0, true>(f, rows, stream)) return e;
         return a.grad ? launch_backward<BF16>(f, rows, stream) : hipSuccess;
     }
     if (a.grad) {
         const bool slots = a.k > (BF16 ? (rows >= 512 ? 512 : 2048) : 256) && slots_lds(a, true) <= (size_t)kDistillLds;
-        return slots ? launch<BF16, true, true, true, 512, BF16 ? 0 : 12>(a, rows, stream) : launch<BF16, true, true, false, 512, 12>(a, rows, stream);
+        return slots ? launch<BF16, true, true, kEntries, 512, BF16 ? 0 : 12>(a, rows, stream) : launch<BF16, true, true, kNone, 512, 12>(a, rows, stream);
     }
-    if (a.k > (BF16 ? 1536 : 768) && slots_lds(a, true) <= (size_t)kDistillLds) return launch<BF16, true, false, true, kDistillForward, 0>(a, rows, stream);
-    return rows >= 1024 && a.k <= 256 ? launch<BF16, true, false, false, 256, 0>(a, rows, stream) : launch<BF16, true, false, false, kDistillForward, 0>(a, rows, stream);
+    if constexpr (BF16)
+        if (a.tail && a.k > 768 && slots_lds(a, true) <= (size_t)kDistillLds)
+            return launch_one<BF16, true, false, true, kHalves, false, kDistillForward, 0>(a, rows, slots_lds(a, true), stream);
+    if (a.k > (BF16 ? 1536 : 768) && slots_lds(a, true) <= (size_t)kDistillLds) return launch<BF16, true, false, kEntries, kDistillForward, 0>(a, rows, stream);
+    return rows >= 1024 && a.k <= 256 ? launch<BF16, true, false, kNone, 256, 0>(a, rows, stream) : launch<BF16, true, false, kNone, kDistillForward, 0>(a, rows, stream);
 }
 
 }  // namespace
