@@ -944,7 +944,7 @@ __device__ __forceinline__ void second_pass(const RowStream<BF16>& rs, int part,
 }
 
 // bf16 rows of one workgroup, top-p alone: the values themselves are counted.  A window of 16 octaves of magnitude less eight values, up to the end of the one that
-// holds the peek's largest and what lies 50 T below it, has kWindow values of either sign; what is smaller lies between the two signs' and goes to the list; what lies
+// holds a quarter more than the peek's largest and what lies 50 T off it (the row's largest is seldom in the peek), has kWindow values of either sign; what is smaller lies between the two signs' and goes to the list; what lies
 // below weighs less than e^-50 and is passed over.  Counts times weights are the row's exact masses, so the prefix's end is known after one pass without an
 // exponential, and the second one looks weights up.  Elements are taken two at a time, as 16-bit integers.
 constexpr int kWindow = 16 * 128 - 8, kValues = 2 * kWindow + 1, kValuesPer = (kValues + kST - 1) / kST;
@@ -956,7 +956,7 @@ typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
 // 16-bit magnitude in front of the window's first: -1: no such window
 __device__ __forceinline__ int window_base(float ref, float T)
 {
-    const float x = fmaxf(fabsf(ref), fabsf(ref - 50.f * T));
+    const float x = fmaxf(1.25f * fabsf(ref), fabsf(ref) + 50.f * T);
     const int e = (int)(__float_as_uint(x) >> 23);
     return e <= 252 ? max(((e + 1) << 7) - kWindow, 128) - 1 : -1;
 }
