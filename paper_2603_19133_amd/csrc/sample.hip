@@ -475,7 +475,8 @@ __device__ __attribute__((noinline)) void sample_careful(const void* logits, int
 //   list     what may be kept is short: the elements at or above a threshold go to a list in LDS.  top-k: the value of rank optimistic_rank(..) of
 //            the peek.  min-p alone: what min-p leaves against the peek's largest, which is no larger than the row's.  top-p alone: about kTopPList elements, with the mass
 //            of the whole row beside, where the peek has its mass there.
-//   histogram  top-p alone on rows whose mass is spread: a first pass counts by logit (2048 bins of 1/64 nat below the peek's largest, with the mean place
+//   values  top-p alone on bf16 rows (count_values below), but for long rows in calls of few (sample_counts_alone).
+//   histogram  top-p alone otherwise, on rows whose mass is spread: a first pass counts by logit (2048 bins of 1/64 nat below the peek's largest, with the mean place
 //            of a bin's elements, of whose mass it gives 10^-5), which names the bin, or the few, in which the prefix ends; a second one sums the segments'
 //            masses above them and lists what lies in them.  (Counts, not masses: LDS adds a wave's 64 integers in 10 to 20 cycles, 64 floats in 195.)
 //            Elements that are likely behind the prefix are left out of the counts; a prefix that ends among them after all takes a third pass.
@@ -585,7 +586,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
     block_scan_excl((double)total, sh.red, t_all);
     if (a_all >= ((double)p + 0.3 * (1.0 - (double)p)) * t_all) return pl;
     pl.way = kHist;
-    if constexpr (BF16) return pl;                                               // (count_values, or several workgroups: neither leaves any out)
+    if constexpr (BF16) return pl;                                               // (several workgroups leave none out)
     // bins behind which the peek has less than 1 / 1.15 of what top-p leaves out
     float near = 0.f, far = (float)(kBins - 1);
     for (int i = 0; i < 7; ++i) {
@@ -943,7 +944,7 @@ __device__ __forceinline__ void second_pass(const RowStream<BF16>& rs, int part,
     if constexpr (!MIN_P) fill_list<BF16>(rs, min(sh.n, kSampleList), sh);
 }
 
-// bf16 rows of one workgroup, top-p alone: the values themselves are counted.  A window of 16 octaves of magnitude less eight values, up to the end of the one that
+// bf16 rows with top-p alone, by one workgroup: the values themselves are counted.  A window of 16 octaves of magnitude less eight values, up to the end of the one that
 // holds a quarter more than the peek's largest and what lies 50 T off it (the row's largest is seldom in the peek), has kWindow values of either sign; what is smaller lies between the two signs' and goes to the list; what lies
 // below weighs less than e^-50 and is passed over.  Counts times weights are the row's exact masses, so the prefix's end is known after one pass without an
 // exponential, and the second one looks weights up.  Elements are taken two at a time, as 16-bit integers.
@@ -1291,7 +1292,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     if constexpr (PHASE == 0) {
         if (parts > 1 && tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
         rs.first_of(part, ahead);                                                // (under way while the peek is looked at)
-        pl = peek<BF16>(rs, a.V, T, k, p, min_p, parts == 1, sh);
+        pl = peek<BF16>(rs, a.V, T, k, p, min_p, parts == 1 || sample_counts_alone(BF16, parts), sh);
         w.move(pl.ref);
         if (parts > 1 && cut_p && k <= 0 && pl.way != kHist && part == 0 && tid == 0) RowScratch<BF16>(a, row).head[parts * 3] = 0ull;   // (nothing for the second launch)
         __syncthreads();
@@ -1307,6 +1308,10 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     }
     if (pl.way == kCareful && part != 0) return;
     bool alone = parts == 1;
+    if (PHASE == 0 && pl.way == kHist && sample_counts_alone(BF16, parts)) {
+        if (part != 0) return;
+        alone = true;
+    }
     if (pl.way == kSum || pl.way == kList) {
         if constexpr (PHASE == 0) {
             if (pl.way == kSum) first_pass<BF16, kSum, false>(rs, ahead, part, parts, pl, w, T, sh, M, kept, total, above_ref);
@@ -1485,7 +1490,7 @@ template <bool BF16>
 hipError_t launch(const SampleArgs& a, int64_t rows, bool hist, hipStream_t stream)
 {
     hipLaunchKernelGGL((sample_kernel<BF16, 0>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
-    if (a.parts > 1 && hist) hipLaunchKernelGGL((sample_kernel<BF16, 1>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
+    if (a.parts > 1 && hist && !sample_counts_alone(BF16, a.parts)) hipLaunchKernelGGL((sample_kernel<BF16, 1>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
     return hipGetLastError();
 }
 

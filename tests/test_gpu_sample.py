@@ -212,6 +212,19 @@ def test_min_p_near_the_end_of_a_prefix(gpu, ps, rows, V, dtype):
     compare(ps.sample(z, V, u, top_p=0.9, min_p=min_p), z, 1.0, 0, 0.9, min_p, u)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("top,T", [(17.25, 0.6), (16.0, 0.05), (33.5, 0.6), (300.0, 0.6), (1e30, 0.6)])
+@pytest.mark.parametrize("rows,V", [(3, 30000), (40, 17001), (270, 9001)])
+def test_one_id_above_the_octave_of_the_others(gpu, ps, rows, V, top, T, dtype):
+    """A row's largest logit, at a place that a glance at the row may miss, lies one octave of magnitude or many above what the others reach."""
+    z, u = rows_of(rows, V, dtype, "normal", 5 + rows)
+    z.copy_((z.float() * 1.4).clamp(max=15.75).to(dtype))
+    at = torch.randint(0, V, (rows,), device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    z[torch.arange(rows, device="cuda"), at] = top
+    for top_p in (0.3, 0.95):
+        compare(ps.sample(z, V, u, temperature=T, top_p=top_p), z, T, 0, top_p, 0.0, u)
+
+
 @pytest.mark.parametrize("top_p", [0.0, 0.9])
 def test_the_ends_of_the_uniforms(gpu, ps, top_p):
     """u = 0 draws the first kept id, the largest u below 1 the last; outside [0, 1): the first and the last."""
