@@ -422,18 +422,16 @@ inline int sample_parts(int dtype, int64_t rows, int V) {
     const int64_t fit = kSampleSlots / rows;
     return (int)std::min<int64_t>(std::min(std::max<int64_t>(fit, 1), (int64_t)kSampleMostParts), most);
 }
-// bf16 rows with top-p alone are counted by value in one workgroup all the same, one pass and a second from the caches, instead of a histogram in parts and a launch behind it,
-// but for long rows in calls of few (us, alone / in parts: 33,000 elements 1 row 27 / 35-51, 64 28 / 40-60; 128,256 1 row 45 / 42, 64 50 / 61-87; 152,000 4 rows 50 / 43-74; 200,000 16 rows
-// 66 / 61-65; 400,000 1 row 113 / 52-55).
-constexpr int kSampleCountParts = 12;
-__host__ __device__ inline bool sample_counts_alone(bool bf16, int parts) { return bf16 && parts < kSampleCountParts; }
-// a row's share of it: the arrival word, three words a part and three for the row, the segments' masses, the parts' histograms, the parts' lists
+// bf16 rows with top-p alone are counted by value in one workgroup all the same, one pass and a second from the caches, instead of a histogram in parts and a launch behind it
+// (us, alone / in parts: 33,000 elements 1 row 27 / 35-51, 64 28 / 40-60; 128,256 1 row 45 / 42, 64 50 / 61-87; 152,000 4 rows 50 / 43-74; 200,000 16 rows 66 / 61-65; 262,144
+// 8 rows 80-90 / 52-57, but 1371 where more than a list of them are equal at the prefix's end).
+// a row's share of it: the arrival word, three words a part and three for the row, the segments' masses, the parts' histograms (fp32), the parts' lists
 struct SampleScratch { size_t seg_at, hist_at, list_at, row_bytes; int list_cap; };
 __host__ __device__ inline SampleScratch sample_scratch(bool bf16, int V, int parts) {
     SampleScratch l;
     l.seg_at = kArrivalStride + ((size_t)parts * 3 + 3 + 31) / 32 * 256;
     l.hist_at = l.seg_at + ((size_t)stats_segments(row_vecs_max(bf16, V)) + 31) / 32 * 256;
-    l.list_at = l.hist_at + (size_t)parts * 2048 * 8;
+    l.list_at = l.hist_at + (bf16 ? 0 : (size_t)parts * 2048 * 8);
     l.list_cap = kSampleList * 2 / parts + 512 < kSampleList ? kSampleList * 2 / parts + 512 : kSampleList;
     l.row_bytes = l.list_at + ((size_t)parts * l.list_cap * 8 + 255) / 256 * 256;
     return l;

@@ -472,11 +472,11 @@ __device__ __attribute__((noinline)) void sample_careful(const void* logits, int
 //
 // kPeek elements of the row, taken evenly from it, say beforehand how the row can be served in one pass over it, or in two:
 //   sum      nothing is cut off: the segments' masses, against the largest element of the peek.
-//   list     what may be kept is short: the elements at or above a threshold go to a list in LDS.  top-k: the value of rank optimistic_rank(..) of
+//   list     what may be kept is short (min-p alone that keeps more than the list holds takes a second pass, which sums): the elements at or above a threshold go to a list in LDS.  top-k: the value of rank optimistic_rank(..) of
 //            the peek.  min-p alone: what min-p leaves against the peek's largest, which is no larger than the row's.  top-p alone: about kTopPList elements, with the mass
 //            of the whole row beside, where the peek has its mass there.
-//   values  top-p alone on bf16 rows (count_values below), but for long rows in calls of few (sample_counts_alone).
-//   histogram  top-p alone otherwise, on rows whose mass is spread: a first pass counts by logit (2048 bins of 1/64 nat below the peek's largest, with the mean place
+//   values  top-p alone on bf16 rows (count_values below).
+//   histogram  top-p alone on fp32 rows whose mass is spread: a first pass counts by logit (2048 bins of 1/64 nat below the peek's largest, with the mean place
 //            of a bin's elements, of whose mass it gives 10^-5), which names the bin, or the few, in which the prefix ends; a second one sums the segments'
 //            masses above them and lists what lies in them.  (Counts, not masses: LDS adds a wave's 64 integers in 10 to 20 cycles, 64 floats in 195.)
 //            Elements that are likely behind the prefix are left out of the counts; a prefix that ends among them after all takes a third pass.
@@ -492,7 +492,7 @@ constexpr float kHistPerNat = 64.f;
 struct Plan { Way way; float ref, least; bool total; float far; };
 
 template <bool BF16>
-__device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, int k, float p, float min_p, bool alone, RowShared& sh)
+__device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, int k, float p, float min_p, RowShared& sh)
 {
     constexpr int N = Vec<BF16>::N, PER = kPeek / (kST * N);                    // vectors a thread
     constexpr int BLOCKS = PER * kSW;
@@ -524,7 +524,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
         pl.least = float_below(float_below((float)((double)ref + (double)T * log((double)fminf(min_p, 1.f)))));
         return pl;
     }
-    if (BF16 && alone && k <= 0) { pl.way = kHist; return pl; }                  // (values are counted whether the mass is spread or not)
+    if (BF16 && k <= 0) { pl.way = kHist; return pl; }                           // (values are counted whether the mass is spread or not)
     const int want = k > 0 ? k : kTopPList;
     const int rank = want <= kSampleList ? optimistic_rank(want, V, min(kPeek, V), kSampleList) : 0;
     if (rank == 0) {
@@ -567,7 +567,7 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
     };
     pl.least = of_rank(rank);
     pl.way = kList;
-    if (k > 0) return pl;
+    if (BF16 || k > 0) return pl;
     pl.total = true;
     const float c = (float)(kLog2e / (double)T);
     // (without the peek's eight largest: what is by chance among the row's few that hold much of it says nothing of the rest)
@@ -586,7 +586,6 @@ __device__ __forceinline__ Plan peek(const RowStream<BF16>& rs, int V, float T, 
     block_scan_excl((double)total, sh.red, t_all);
     if (a_all >= ((double)p + 0.3 * (1.0 - (double)p)) * t_all) return pl;
     pl.way = kHist;
-    if constexpr (BF16) return pl;                                               // (several workgroups leave none out)
     // bins behind which the peek has less than 1 / 1.15 of what top-p leaves out
     float near = 0.f, far = (float)(kBins - 1);
     for (int i = 0; i < 7; ++i) {
@@ -1292,9 +1291,9 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     if constexpr (PHASE == 0) {
         if (parts > 1 && tid == 0) open_arrival(RowScratch<BF16>(a, row).word);
         rs.first_of(part, ahead);                                                // (under way while the peek is looked at)
-        pl = peek<BF16>(rs, a.V, T, k, p, min_p, parts == 1 || sample_counts_alone(BF16, parts), sh);
+        pl = peek<BF16>(rs, a.V, T, k, p, min_p, sh);
         w.move(pl.ref);
-        if (parts > 1 && cut_p && k <= 0 && pl.way != kHist && part == 0 && tid == 0) RowScratch<BF16>(a, row).head[parts * 3] = 0ull;   // (nothing for the second launch)
+        if (!BF16 && parts > 1 && cut_p && k <= 0 && pl.way != kHist && part == 0 && tid == 0) RowScratch<BF16>(a, row).head[parts * 3] = 0ull;   // (nothing for the second launch)
         __syncthreads();
     } else {
         const RowScratch<BF16> rx(a, row);
@@ -1308,10 +1307,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     }
     if (pl.way == kCareful && part != 0) return;
     bool alone = parts == 1;
-    if (PHASE == 0 && pl.way == kHist && sample_counts_alone(BF16, parts)) {
-        if (part != 0) return;
-        alone = true;
-    }
+    if (BF16 && pl.way == kHist && part != 0) return;                            // (counted by one)
     if (pl.way == kSum || pl.way == kList) {
         if constexpr (PHASE == 0) {
             if (pl.way == kSum) first_pass<BF16, kSum, false>(rs, ahead, part, parts, pl, w, T, sh, M, kept, total, above_ref);
@@ -1357,14 +1353,17 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                 }
             }
             if (!done && near && pl.total) { pl.way = kHist; alone = true; }     // (the peek took a spread row for a peaked one)
+            if (!done && near && pl.way == kList && k <= 0 && !cut_p) {          // (min-p alone, and a list too short for it: a pass that sums)
+                w.move(M);
+                second_pass<BF16, true>(rs, 0, 1, br, pl.ref, per, w, a_min, sh, kept, total);
+                done = true;
+            }
         }
     }
-    constexpr bool COUNTS = PHASE == 0 && BF16;                                  // (then the histogram's second pass is the second launch's)
-    if constexpr (COUNTS) {
+    if constexpr (BF16) {
         __syncthreads();
-        if (pl.way == kHist && alone) done = count_values(rs, pl, T, p, a_min, w, cut, kept, M, sh);
-    }
-    if (pl.way == kHist && !(COUNTS && alone)) {
+        if (pl.way == kHist) done = count_values(rs, pl, T, p, a_min, w, cut, kept, M, sh);
+    } else if (pl.way == kHist) {
         const int at = alone ? 0 : part, of = alone ? 1 : parts;
         bool good = PHASE == 1;
         if constexpr (PHASE == 0) {
@@ -1401,7 +1400,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                 __syncthreads();
             }
             int found = M <= kFloatMax ? bracket(p, total, above_ref, pl.far, sh, br) : -1;
-            if (!BF16 && found == 0) {
+            if (found == 0) {
                 pl.far = (float)(kBins - 1);
                 for (int i = tid; i < 2 * kBins; i += kST) sh.hist[0][i] = 0ull;
                 __syncthreads();
@@ -1427,40 +1426,38 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
                 if (good) return;
             }
         }
-        if constexpr (!COUNTS) {
-            if (good) {
-                w.move(M);
-                if (tid == 0) sh.n = 0;
-                __syncthreads();
-                if (br.by_min_p) second_pass<BF16, true>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
-                else second_pass<BF16, false>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
-                if (!alone && !gather<BF16>(rs, RowScratch<BF16>(a, row), part, parts, true, true, M, kept, total, sh)) return;
-                if (br.by_min_p) {
-                    done = true;
-                } else if (sh.n <= kSampleList) {
-                    const int n = sh.n;
-                    double above = 0.0, mine = 0.0;
-                    for (int i = tid * kSegsPer; i < min((tid + 1) * kSegsPer, rs.n_seg); ++i) mine += sh.seg[i];
-                    block_scan_excl(mine, sh.red, above);
-                    const double target = (double)p * total - above;
-                    unsigned long long last = 0;
-                    int m = n;                                                   // (0: min-p leaves nothing of the list)
-                    if (!(target > 0.0)) {
-                    } else if (sort_list(n, sh)) {
-                        double listed;
-                        m = kept_of_list(n, 1.0, target, a_min, w, sh, listed);
-                        done = target <= listed;
-                        if (done && m > 0) last = sh.list[m - 1];
-                    } else {
-                        __syncthreads();
-                        const unsigned long long listed = list_sum(n, 0ull, w, sh);
-                        done = ldexp(target, kListShift) <= (double)listed;
-                        if (done) last = select<true>(n, 0ull, ldexp(target, kListShift), w, sh);
-                    }
-                    if (done && m > 0) {
-                        cut = Cut{composite_value(last), composite_id(last), a_min};
-                        kept += list_to_segments<BF16>(rs, n, cut, w, true, sh);
-                    }
+        if (good) {
+            w.move(M);
+            if (tid == 0) sh.n = 0;
+            __syncthreads();
+            if (br.by_min_p) second_pass<BF16, true>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
+            else second_pass<BF16, false>(rs, at, of, br, pl.ref, per, w, a_min, sh, kept, total);
+            if (!alone && !gather<BF16>(rs, RowScratch<BF16>(a, row), part, parts, true, true, M, kept, total, sh)) return;
+            if (br.by_min_p) {
+                done = true;
+            } else if (sh.n <= kSampleList) {
+                const int n = sh.n;
+                double above = 0.0, mine = 0.0;
+                for (int i = tid * kSegsPer; i < min((tid + 1) * kSegsPer, rs.n_seg); ++i) mine += sh.seg[i];
+                block_scan_excl(mine, sh.red, above);
+                const double target = (double)p * total - above;
+                unsigned long long last = 0;
+                int m = n;                                                   // (0: min-p leaves nothing of the list)
+                if (!(target > 0.0)) {
+                } else if (sort_list(n, sh)) {
+                    double listed;
+                    m = kept_of_list(n, 1.0, target, a_min, w, sh, listed);
+                    done = target <= listed;
+                    if (done && m > 0) last = sh.list[m - 1];
+                } else {
+                    __syncthreads();
+                    const unsigned long long listed = list_sum(n, 0ull, w, sh);
+                    done = ldexp(target, kListShift) <= (double)listed;
+                    if (done) last = select<true>(n, 0ull, ldexp(target, kListShift), w, sh);
+                }
+                if (done && m > 0) {
+                    cut = Cut{composite_value(last), composite_id(last), a_min};
+                    kept += list_to_segments<BF16>(rs, n, cut, w, true, sh);
                 }
             }
         }
@@ -1490,7 +1487,8 @@ template <bool BF16>
 hipError_t launch(const SampleArgs& a, int64_t rows, bool hist, hipStream_t stream)
 {
     hipLaunchKernelGGL((sample_kernel<BF16, 0>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
-    if (a.parts > 1 && hist && !sample_counts_alone(BF16, a.parts)) hipLaunchKernelGGL((sample_kernel<BF16, 1>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
+    if constexpr (!BF16)
+        if (a.parts > 1 && hist) hipLaunchKernelGGL((sample_kernel<BF16, 1>), dim3((unsigned)(rows * a.parts)), dim3(kST), 0, stream, a);
     return hipGetLastError();
 }
 

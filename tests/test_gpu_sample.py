@@ -225,6 +225,15 @@ def test_one_id_above_the_octave_of_the_others(gpu, ps, rows, V, top, T, dtype):
         compare(ps.sample(z, V, u, temperature=T, top_p=top_p), z, T, 0, top_p, 0.0, u)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,T,min_p", [(2, 100001, 1.0, 1e-3), (30, 40000, 3.0, 1e-3), (270, 20001, 3.0, 1e-4)])
+def test_min_p_that_keeps_thousands(gpu, ps, rows, V, T, min_p, dtype):
+    z, u = rows_of(rows, V, dtype, "flat", rows)
+    z[0, 5:9] = math.nan
+    z[1, ::3] = -math.inf
+    compare(ps.sample(z, V, u, temperature=T, min_p=min_p), z, T, 0, 0.0, min_p, u)
+
+
 @pytest.mark.parametrize("top_p", [0.0, 0.9])
 def test_the_ends_of_the_uniforms(gpu, ps, top_p):
     """u = 0 draws the first kept id, the largest u below 1 the last; outside [0, 1): the first and the last."""
