@@ -391,11 +391,11 @@ class Sampled:
     lse: torch.Tensor     # float32 [rows]: log of the kept mass
 
 
-def _setting(v, rows: int, dtype: torch.dtype):
+def _setting(v, rows: int, dtype: torch.dtype, device: torch.device):
     """(value, tensor): a number for all rows, or a tensor with one for each."""
     if not isinstance(v, torch.Tensor):
         return v, None
-    if v.dtype != dtype or v.dim() != 1 or v.numel() != rows or not v.is_contiguous() or not v.is_cuda:
+    if v.dtype != dtype or v.dim() != 1 or v.numel() != rows or not v.is_contiguous() or v.device != device:
         raise PicoSpecError(EINVAL)
     return 0, v
 
@@ -405,13 +405,19 @@ def sample(logits: torch.Tensor, V: int, uniforms: torch.Tensor, temperature=1.0
     """picospec_sample: one token per row of [rows, >=V] device logits.  Every setting is a number for all rows or a device tensor with one per
     row (float32, top_k int32)."""
     dt, ld, rows = _logits_2d(logits)
-    if uniforms.numel() != rows or uniforms.dtype != torch.float32 or not uniforms.is_contiguous() or not uniforms.is_cuda:
+    device = logits.device
+    if uniforms.numel() != rows or uniforms.dtype != torch.float32 or not uniforms.is_contiguous() or uniforms.device != device:
         raise PicoSpecError(EINVAL)
-    T, T_rows = _setting(temperature, rows, torch.float32)
-    k, k_rows = _setting(top_k, rows, torch.int32)
-    p, p_rows = _setting(top_p, rows, torch.float32)
-    m, m_rows = _setting(min_p, rows, torch.float32)
-    out = out or Sampled(*_nat.empty(logits, "ifif", rows, rows, rows, rows))
+    T, T_rows = _setting(temperature, rows, torch.float32, device)
+    k, k_rows = _setting(top_k, rows, torch.int32, device)
+    p, p_rows = _setting(top_p, rows, torch.float32, device)
+    m, m_rows = _setting(min_p, rows, torch.float32, device)
+    if out is None:
+        out = Sampled(*_nat.empty(logits, "ifif", rows, rows, rows, rows))
+    else:                                        # (a longer one is written as far as there are rows)
+        for t, dtype in ((out.tok, torch.int32), (out.prob, torch.float32), (out.count, torch.int32), (out.lse, torch.float32)):
+            if t.numel() < rows or t.dtype != dtype or not t.is_contiguous() or t.device != device:
+                raise PicoSpecError(EINVAL)
     _check(_nat.sample(logits, dt, ld, rows, V, T, k, p, m, T_rows, k_rows, p_rows, m_rows, uniforms, out.tok, out.prob, out.count, out.lse,
                        _nat.scratch(logits, CALL_SAMPLE, dt, rows, 0, V, 0), _stream()))
     return out
