@@ -457,8 +457,8 @@ def distill_grad(logits: torch.Tensor, V: int, temperature: float, rec: Compress
     dt, ld, rows = _distill_inputs(logits, rec, weight)
     out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device) if out is None else out
     dt_g, ld_g, rows_g = _logits_2d(out)
-    if dt_g != dt or rows_g != rows or out.shape[1] < V or stats.numel() != 4 * rows or stats.dtype != torch.float64 or not (
-            stats.is_contiguous() and stats.is_cuda):
+    if dt_g != dt or rows_g != rows or out.shape[1] < V or out.device != logits.device or stats.numel() != 4 * rows or stats.dtype != torch.float64 or not (
+            stats.is_contiguous() and stats.device == logits.device):
         raise PicoSpecError(EINVAL)
     _check(_nat.distill_grad(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, stats, out, ld_g, _stream()))
     return out

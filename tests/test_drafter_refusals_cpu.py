@@ -52,3 +52,17 @@ def test_sample_refuses_tensors_of_another_device(calls):
     assert not calls
     ps.sample(z, V, u, temperature=f, top_k=i, top_p=f, min_p=f)
     assert calls == ["sample"]
+
+
+def _record(rows=ROWS, k=5):
+    return ps.Compressed(torch.zeros(rows, k, dtype=torch.int32), torch.zeros(rows, k), torch.zeros(rows, dtype=torch.int32), torch.zeros(rows), torch.zeros(rows), k)
+
+
+def test_distill_grad_refuses_statistics_and_outputs_of_another_device(calls):
+    z, stats = torch.zeros(ROWS, V), torch.zeros(ROWS, 4, dtype=torch.float64)
+    for s, out in ((stats.to("meta"), torch.empty(ROWS, V)), (stats, torch.empty(ROWS, V, device="meta"))):
+        with pytest.raises(ps.PicoSpecError):
+            ps.distill_grad(z, V, 1.0, _record(), s, out=out)
+    assert not calls
+    ps.distill_grad(z, V, 1.0, _record(), stats, out=torch.empty(ROWS, V))
+    assert calls == ["distill_grad"]
