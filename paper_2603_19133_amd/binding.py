@@ -406,6 +406,8 @@ def sample(logits: torch.Tensor, V: int, uniforms: torch.Tensor, temperature=1.0
     row (float32, top_k int32)."""
     dt, ld, rows = _logits_2d(logits)
     device = logits.device
+    if V > logits.shape[1]:                      # (a view's rows end before its stride does, and behind the last one there may be nothing)
+        raise PicoSpecError(EINVAL)
     if uniforms.numel() != rows or uniforms.dtype != torch.float32 or not uniforms.is_contiguous() or uniforms.device != device:
         raise PicoSpecError(EINVAL)
     T, T_rows = _setting(temperature, rows, torch.float32, device)
@@ -431,11 +433,14 @@ class Distilled:
     grad: torch.Tensor | None     # [rows, V] in the logits' dtype
 
 
-def _distill_inputs(logits: torch.Tensor, rec: Compressed, weight: torch.Tensor | None):
-    """(dtype code, stride of a row, rows) of the logits; the record and the weights have to be theirs, without gaps."""
+def _distill_inputs(logits: torch.Tensor, V: int, rec: Compressed, weight: torch.Tensor | None):
+    """(dtype code, stride of a row, rows) of the logits; the vocabulary has to lie in their columns, the record and the weights have to be theirs,
+    without gaps."""
     r = _nat.distill_inputs(logits, rec.idx, rec.prob, rec.count, rec.k, weight)
     if r.__class__ is int:
         raise PicoSpecError(r)
+    if V > logits.shape[1]:
+        raise PicoSpecError(EINVAL)
     return r
 
 
@@ -443,7 +448,7 @@ def distill(logits: torch.Tensor, V: int, temperature: float, rec: Compressed, t
             grad: bool = False) -> Distilled:
     """picospec_distill of [rows, >=V] drafter logits on the target's records: loss and expected acceptance per row and, with `grad`,
     weight * d loss / d logits in the same call.  training.distill_loss is the same for torch's autograd."""
-    dt, ld, rows = _distill_inputs(logits, rec, weight)
+    dt, ld, rows = _distill_inputs(logits, V, rec, weight)
     loss, accept, stats = _nat.empty(logits, "ffd", rows, rows, (rows, 4))
     g = torch.empty((rows, V), dtype=logits.dtype, device=logits.device) if grad else None
     _check(_nat.distill(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, loss, accept, stats, g, V,
@@ -454,7 +459,7 @@ def distill(logits: torch.Tensor, V: int, temperature: float, rec: Compressed, t
 def distill_grad(logits: torch.Tensor, V: int, temperature: float, rec: Compressed, stats: torch.Tensor, tail: int = 0,
                  weight: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """picospec_distill_grad: weight * d loss / d logits [rows, V] from the stats of an earlier distill of the same logits and records."""
-    dt, ld, rows = _distill_inputs(logits, rec, weight)
+    dt, ld, rows = _distill_inputs(logits, V, rec, weight)
     out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device) if out is None else out
     dt_g, ld_g, rows_g = _logits_2d(out)
     if dt_g != dt or rows_g != rows or out.shape[1] < V or out.device != logits.device or stats.numel() != 4 * rows or stats.dtype != torch.float64 or not (

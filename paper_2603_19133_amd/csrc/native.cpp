@@ -291,9 +291,10 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
         const int dt = logits_code(z, ld);
         const int64_t rows = z.size(0);
         check_record(z, idx, prob, count, k);
+        if (V > z.size(1)) throw Refused{PICOSPEC_EINVAL};                                          // (a view's rows end before its stride does)
         const auto f32 = z.options().dtype(at::kFloat);
         at::Tensor loss = at::empty({rows}, f32), accept = at::empty({rows}, f32), stats = at::empty({rows, 4}, z.options().dtype(at::kDouble));
-        const size_t bytes = V > 0 && V <= z.size(1) ? picospec_scratch_bytes(PICOSPEC_CALL_DISTILL, dt, (int32_t)rows, 0, (int32_t)V, 0) : 0;
+        const size_t bytes = picospec_scratch_bytes(PICOSPEC_CALL_DISTILL, dt, (int32_t)rows, 0, (int32_t)V, 0);
         const at::Tensor scratch = bytes ? at::empty({(int64_t)bytes}, z.options().dtype(at::kByte)) : at::Tensor();
         const int rc = picospec_distill(z.data_ptr(), dt, ld, (int32_t)rows, (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
                                         (int)tail, nullptr, loss.data_ptr<float>(), accept.data_ptr<float>(), stats.data_ptr<double>(), nullptr, 0,

@@ -66,3 +66,15 @@ def test_distill_grad_refuses_statistics_and_outputs_of_another_device(calls):
     assert not calls
     ps.distill_grad(z, V, 1.0, _record(), stats, out=torch.empty(ROWS, V))
     assert calls == ["distill_grad"]
+
+
+def test_a_vocabulary_wider_than_the_view_is_refused(calls):
+    """The last columns of a wider tensor: its rows are as far apart as the vocabulary is long, but the last one ends with the tensor."""
+    z = torch.zeros(ROWS, 2 * V)[:, V:]
+    assert z.stride(0) >= V + 1
+    for call in (lambda v: ps.sample(z, v, torch.zeros(ROWS)), lambda v: ps.distill(z, v, 1.0, _record()),
+                 lambda v: ps.distill_grad(z, v, 1.0, _record(), torch.zeros(ROWS, 4, dtype=torch.float64), out=torch.empty(ROWS, 2 * V))):
+        with pytest.raises(ps.PicoSpecError):
+            call(V + 1)
+        call(V)
+    assert calls == ["sample", "distill", "distill_grad"]
