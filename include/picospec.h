@@ -433,7 +433,7 @@ int picospec_unpack_uplink(const void* wire, int64_t wire_bytes, int32_t B, int3
  *   top_k        <= 0: no limit      top_p  <= 0 or >= 1: all      min_p  <= 0: all; at most 1
  *   temperature_rows, top_k_rows, top_p_rows, min_p_rows [n_rows], each nullable: a setting per row instead.  What the host would refuse counts
  *                as greedy (temperature), 1 (min_p above it) or none (NaN)
- *   uniforms     [n_rows] in [0,1)                                                                            in
+ *   uniforms     [n_rows] in [0,1); none, 0 included, draws an id that weighs less than 2^-978 of the kept mass (a masked one)    in
  *   tok [n_rows] int32, prob [n_rows] fp32 = the token's share of the kept mass, count [n_rows] int32 = how many ids are kept,
  *   lse [n_rows] fp32 = max z / T + ln(kept mass)                                                             out
  *   workspace    (optional): picospec_workspace_bytes(PICOSPEC_CALL_SAMPLE, dtype, n_rows, V, 0) bytes of scratch, in which a call of few rows spreads

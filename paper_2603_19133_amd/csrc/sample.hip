@@ -203,6 +203,11 @@ __device__ __forceinline__ T block_scan_excl(T v, T* red, T& total)
 }
 
 // ---------------------------------------------------------------- the draw
+//
+// What weighs 2^-1000 (weight()) may lie below that by any distance, masked ids above all: no uniform, 0 included, may draw it. So a segment of less than
+// 2^-978 of the kept mass counts as empty, and so does an id of less than 2^-990 of it. The kept mass is 1 at least: a segment's 2^11 ids of 2^-1000 stay below
+// the one, and a segment that does not count as empty has an id that does not.
+constexpr double kNoSegment = 0x1p-978, kNoId = 0x1p-990;
 
 // The segments' kept masses are in sh.seg: their sum, the token and its probability.
 template <bool BF16>
@@ -219,14 +224,14 @@ __device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w
     }
     if (tid == 0) { sh.at = INT32_MAX; sh.last = -1; }
     double before = block_scan_excl(sum, sh.red, total);
-    const double target = (u >= 0.f ? (double)u : 0.0) * total;
+    const double target = (u >= 0.f ? (double)u : 0.0) * total, no_segment = total * kNoSegment, no_id = total * kNoId;
     // the first segment whose end exceeds the target; where rounding leaves none, the last with any mass
     {
         double b = before, b_hit = 0.0;
         int hit = INT32_MAX;
 #pragma unroll
         for (int i = 0; i < kSegsPer; ++i) {
-            if (mine[i] > 0.0) {
+            if (mine[i] > no_segment) {
                 if (b + mine[i] > target && hit == INT32_MAX) { hit = tid * kSegsPer + i; b_hit = b; atomicMin(&sh.at, hit); }
                 atomicMax(&sh.last, tid * kSegsPer + i);
             }
@@ -251,6 +256,7 @@ __device__ __forceinline__ void draw(const RowStream<BF16>& rs, const Weights& w
     for (int e = 0; e < N; ++e) {
         const float z = cleaned(v[e]);
         kept[e] = have && z > kNegInf && cut.keeps(z, rs.first_id(q) + e, w) ? w.weight(z) : 0.0;
+        kept[e] = kept[e] > no_id ? kept[e] : 0.0;
         in_vec += kept[e];
     }
     double all;
@@ -1241,7 +1247,8 @@ __device__ __forceinline__ void draw_short(int kept, float u, const Weights& w, 
         if (tid < kept) {
             const float z = composite_value(c);
             sh.mass[rank] = pack2(x, __float_as_uint(z));
-            sh.seg[rank] = w.weight(z);
+            const double one = w.weight(z);
+            sh.seg[rank] = one > kNoId * kST ? one : 0.0;                        // (of a kept mass of kST at most)
         }
     }
     __syncthreads();

@@ -28,3 +28,56 @@ def test_a_vocabulary_wider_than_the_view_is_refused(gpu, ps):
             call(101)
         call(100)
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------- the sampler: uniforms at the ends over masked ids
+
+def _masked(rows, V, dtype, seed, T=1.0):
+    """Rows whose first and last ids are masked, whole segments of them: with -inf, with the type's lowest value, with both in turn, or all but 20 ids."""
+    z, _ = ts.rows_of(rows, V, dtype, "normal", seed, 3, 1)
+    low, a, b = torch.finfo(dtype).min, V // 5, V - V // 7
+    for r in range(rows):
+        fill = torch.full((V,), -math.inf if r % 2 == 0 else low, dtype=dtype, device="cuda")
+        if r % 6 >= 4:                                             # (both in turn)
+            fill[::2] = -math.inf if r % 2 else low
+        if r % 3 == 2:                                             # (a grammar that allows 20 ids)
+            keep = torch.zeros(V, dtype=torch.bool, device="cuda")
+            keep[torch.from_numpy(np.random.default_rng(r).choice(np.arange(a, b), min(20, b - a), replace=False)).cuda()] = True
+        else:
+            keep = torch.zeros(V, dtype=torch.bool, device="cuda")
+            keep[a:b] = True
+        z[r] = torch.where(keep, z[r], fill)
+    return z
+
+
+@pytest.mark.parametrize("setting", [dict(), dict(top_k=50), dict(top_k=50, top_p=0.9), dict(top_k=700), dict(top_k=900, min_p=1e-30), dict(top_k=9000), dict(top_p=0.9), dict(top_p=0.999), dict(min_p=0.02)],
+                         ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(6, 37), (6, 5003), (6, 40009), (138, 20011)])
+def test_uniforms_at_the_ends_over_masked_ids(gpu, ps, rows, V, dtype, setting):
+    """u = 0 draws the first id with any weight in 64 bits, the largest u below 1 the last but for 2^-24 of the mass: masked ids in front of and behind them
+    are not drawn, whether they hold -inf or the type's lowest value, and also where top-k keeps more ids than are allowed.  (Of many rows u = 0 alone: the other
+    two lie near steps of some 10^-8 of the mass.)"""
+    print(f"[case] sample ends {rows} x {V} {dtype} {setting}", flush=True)
+    z = _masked(rows, V, dtype, rows + V)
+    s = dict(dict(top_k=0, top_p=0.0, min_p=0.0), **setting)
+    for v in (0.0, 2.0 ** -24, 1.0 - 2.0 ** -24) if rows < 10 else (0.0,):
+        u = torch.full((rows,), v, device="cuda")
+        ts.compare(ps.sample(z, V, u, temperature=0.8, **s), z, 0.8, s["top_k"], s["top_p"], s["min_p"], u)
+    got = ps.sample(z, V, torch.ones(rows, device="cuda"), temperature=0.8, **s)              # (outside the range: the last)
+    torch.cuda.synchronize()
+    tok = got.tok.long()
+    assert (z[torch.arange(rows, device="cuda"), tok] > -1e30).all() and (tok >= 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(5, 30011), (138, 9001)])
+def test_a_uniform_on_the_border_of_a_masked_segment(gpu, ps, rows, V, dtype):
+    """Equal logits on either side of a masked block, u at the border exactly: the first id behind the block."""
+    z = torch.full((rows, V), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+    z[::2] = -math.inf
+    z[:, 16:528], z[:, 8200:8712] = 0.0, 0.0
+    u = torch.full((rows,), 0.5, device="cuda")
+    for s in (dict(), dict(top_k=2000), dict(top_k=400), dict(top_p=0.75), dict(min_p=0.5)):
+        s = dict(dict(top_k=0, top_p=0.0, min_p=0.0), **s)
+        ts.compare(ps.sample(z, V, u, **s), z, 1.0, s["top_k"], s["top_p"], s["min_p"], u)
