@@ -771,23 +771,29 @@ __device__ __forceinline__ unsigned long long list_sum(int n, unsigned long long
     return all;
 }
 
-// Adds the masses of the kept entries to their segments' (as integers of 2^-kListShift: exact, whatever the order) and counts them.
+// Adds the masses of the kept entries to their segments' (as integers of 2^-kListShift: exact, whatever the order) and counts them. A segment that keeps nothing but
+// what rounds to no unit, and more than draw() calls empty, is marked with 2^-60: a uniform of 0 draws its first kept id.
 template <bool BF16>
 __device__ __forceinline__ int list_to_segments(const RowStream<BF16>& rs, int n, const Cut& cut, const Weights& w, bool add, RowShared& sh)
 {
     unsigned long long* const extra = sh.mass;                                  // (segments in blocks of kListBins: one, but for fp32 rows of a million)
     unsigned long long mine = 0, all;
     for (int first = 0; first < rs.n_seg; first += kListBins) {
-        for (int i = threadIdx.x; i < kListBins; i += kST) extra[i] = 0;
+        for (int i = threadIdx.x; i < kListBins; i += kST) { extra[i] = 0; sh.count[i] = 0u; }
         __syncthreads();
         for (int i = threadIdx.x; i < n; i += kST) {
             const unsigned long long c = sh.list[i];
             const int x = composite_id(c), s = (rs.rv.o + x) / (64 * kSplitStatsNV * Vec<BF16>::N) - first;
-            if (s >= 0 && s < kListBins && cut.keeps(composite_value(c), x, w)) { ++mine; atomicAdd(&extra[s], list_mass(c, w)); }
+            if (s >= 0 && s < kListBins && cut.keeps(composite_value(c), x, w)) {
+                const unsigned long long m = list_mass(c, w);
+                ++mine;
+                if (m) atomicAdd(&extra[s], m);
+                else if (w.weight(composite_value(c)) > kNoSegment * kSampleList) sh.count[s] = 1u;
+            }
         }
         __syncthreads();
         for (int i = threadIdx.x; i < kListBins && first + i < rs.n_seg; i += kST) {
-            const double m = ldexp((double)extra[i], -kListShift);
+            const double m = extra[i] || !sh.count[i] ? ldexp((double)extra[i], -kListShift) : 0x1p-60;
             sh.seg[first + i] = add ? sh.seg[first + i] + m : m;
         }
         __syncthreads();

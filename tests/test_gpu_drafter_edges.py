@@ -81,3 +81,14 @@ def test_a_uniform_on_the_border_of_a_masked_segment(gpu, ps, rows, V, dtype):
     for s in (dict(), dict(top_k=2000), dict(top_k=400), dict(top_p=0.75), dict(min_p=0.5)):
         s = dict(dict(top_k=0, top_p=0.0, min_p=0.0), **s)
         ts.compare(ps.sample(z, V, u, **s), z, 1.0, s["top_k"], s["top_p"], s["min_p"], u)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("setting", [dict(top_k=300), dict(top_k=1500), dict(top_k=4000, top_p=0.999), dict(min_p=1e-25), dict()], ids=str)
+@pytest.mark.parametrize("rows,V", [(3, 5003), (4, 40009), (138, 20011)])
+def test_the_first_kept_id_of_hardly_any_weight(gpu, ps, rows, V, dtype, setting):
+    """u = 0 where the kept ids' weights lie up to e^-300 apart: the first kept id, however little it weighs."""
+    z, _ = ts.rows_of(rows, V, dtype, "normal", 5 * V)
+    s = dict(dict(top_k=0, top_p=0.0, min_p=0.0), **setting)
+    u = torch.zeros(rows, device="cuda")
+    ts.compare(ps.sample(z, V, u, temperature=0.08, **s), z, 0.08, s["top_k"], s["top_p"], s["min_p"], u)
