@@ -1280,8 +1280,7 @@ __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
     float T = a.T_rows ? a.T_rows[row] : a.T;
     int k = a.k_rows ? a.k_rows[row] : a.top_k;
     const float p = a.p_rows ? a.p_rows[row] : a.top_p, min_p = a.minp_rows ? a.minp_rows[row] : a.min_p;
-    if (!(T > 0.f)) { T = 1.f; k = 1; }                                          // (greedy)
-    T = fminf(T, kFloatMax);
+    if (!(T > 0.f && T <= kFloatMax)) { T = 1.f; k = 1; }                        // (greedy)
     const bool cut_p = p > 0.f && p < 1.f;
     if (PHASE == 1 && (k > 0 || !cut_p)) return;
     const float per = kHistPerNat / T;

@@ -92,3 +92,11 @@ def test_the_first_kept_id_of_hardly_any_weight(gpu, ps, rows, V, dtype, setting
     s = dict(dict(top_k=0, top_p=0.0, min_p=0.0), **setting)
     u = torch.zeros(rows, device="cuda")
     ts.compare(ps.sample(z, V, u, temperature=0.08, **s), z, 0.08, s["top_k"], s["top_p"], s["min_p"], u)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_a_temperature_per_row_that_the_host_would_refuse_is_greedy(gpu, ps, dtype):
+    z, u = ts.rows_of(8, 9001, dtype, "normal", 15)
+    T = torch.tensor([math.inf, 1.0, math.nan, -1.0, -math.inf, 0.0, 3.0e38, 0.5], device="cuda")
+    as_said = torch.where(torch.isfinite(T) & (T > 0), T, torch.zeros_like(T))
+    ts.compare(ps.sample(z, 9001, u, temperature=T), z, as_said, 0, 0.0, 0.0, u)
