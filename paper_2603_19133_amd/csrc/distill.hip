@@ -19,6 +19,8 @@ namespace {
 // two (bf16) or one (fp32) values of -inf
 template <bool BF16> constexpr uint32_t kMaskedPair = BF16 ? 0xFF80FF80u : 0xFF800000u;
 
+constexpr float kNoReference = -67108864.f;      // -2^26: above it r is no more than 2 below the largest exponent
+
 enum Slots : int { kNone, kEntries, kHalves };  // of a long record, in LDS
 
 struct DistillArgs {
@@ -104,7 +106,8 @@ __device__ __forceinline__ void store_one(char* grad_row, int x, float g)
 //
 // Weights are 2^(z c - r), c = log2(e) / T in fp32 and r an integer that is the same for a wave, near its largest exponent: one fused multiply-add and one
 // exponential per element (the product inside is exact, so the error is that of (z - M) c).  r moves up, and the lanes' sums are rescaled, only when an element
-// lies more than 2^64 above it.  Rows with |M c| >= 2^24, where r is no integer near M c any more, take (z - M) c and read the row once more.
+// lies more than 2^64 above it.  What a wave has seen so far may be ids masked with a finite value, of which r would have no more than fp32's 24 bits and the exponents
+// be what its rounding leaves, 2^439 for -1e10: below kNoReference r is not taken and the weights are 0 (a row of no more than that has |M c| >= 2^24).  Rows with |M c| >= 2^24, where r is no integer near M c any more, take (z - M) c and read the row once more.
 //
 // What the record's entries need of the row, and the row of them (SLOTS):
 //   entries The record lies in LDS in the order of its ids: a bit per element, the number of bits in front of every 32, and the entries' p.  The streaming finds the
@@ -309,7 +312,7 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : kDT / 256) void distill_kernel(cons
             if constexpr (!TAIL || SLOTS) mx = fmaxf(mx, bm);                  // (SLOTS: the record's come behind the stream)
             if (__ballot(bm * c > r + 64.f)) {                                // (uniform; the first step, and outliers)
                 const float rn = ceilf(wave_max(bm) * c);
-                if (rn > r) { s *= __builtin_amdgcn_exp2f(r - rn); r = rn; }   // (r = -inf: s is 0 and stays 0)
+                if (rn > r && rn > kNoReference) { s *= __builtin_amdgcn_exp2f(r - rn); r = rn; }   // (r = -inf: s is 0 and stays 0)
             }
             const float nr = r == kNegInf ? 0.f : -r;
             s += tree_sum<0, G * N>([&](int e) { return __builtin_amdgcn_exp2f(fmaf(v[e], c, nr)); });

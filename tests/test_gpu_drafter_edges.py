@@ -100,3 +100,44 @@ def test_a_temperature_per_row_that_the_host_would_refuse_is_greedy(gpu, ps, dty
     T = torch.tensor([math.inf, 1.0, math.nan, -1.0, -math.inf, 0.0, 3.0e38, 0.5], device="cuda")
     as_said = torch.where(torch.isfinite(T) & (T > 0), T, torch.zeros_like(T))
     ts.compare(ps.sample(z, 9001, u, temperature=T), z, as_said, 0, 0.0, 0.0, u)
+
+
+# ---------------------------------------------------------------- the loss: masks of finite values in blocks
+
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("low,T", [(-1e4, 1.0), (-1e9, 1.0), (-1e10, 1.0), (-1e20, 1.0), (-1e30, 0.7), (None, 1.0), (None, 2.0), (None, 0.5), (-5e7, 1.0), (-2e7, 1.0)], ids=str)
+@pytest.mark.parametrize("rows,V,k", [(3, 700, 8), (5, 9001, 40), (5, 9001, 700), (3, 70001, 12), (4, 40003, 2000)])
+def test_blocks_of_ids_masked_with_finite_values(gpu, ps, rows, V, k, low, T, dtype, tail):
+    """A vocabulary's first ids, its last ones or whole stretches in between, masked with a finite value: what a wave sees first is masked, all that it sees or what it
+    sees last, and so is a whole part of a row that several workgroups share."""
+    print(f"[case] distill blocks {rows} x {V} k={k} low={low} T={T} {dtype} tail={tail}", flush=True)
+    z, idx, prob, count = td.inputs(rows, V, k, dtype, T, V + k, 1, 1)
+    low = torch.finfo(dtype).min if low is None else low
+    on = torch.zeros(rows, V, dtype=torch.bool, device="cuda")
+    on.scatter_(1, torch.from_numpy(idx.astype(np.int64)).cuda(), True)
+    off = torch.zeros(rows, V, dtype=torch.bool, device="cuda")
+    off[0, : V // 2] = True
+    off[1, V // 2:] = True
+    off[2, V // 3: 2 * V // 3] = True
+    if rows > 3:
+        off[3, : 9 * V // 10] = True
+        off[3, ::2] = True
+    if rows > 4:
+        off[4] = True
+        off[4, V // 2: V // 2 + 64] = False
+    z[off & ~on] = low
+    td.run_all(ps, z, V, T, idx, prob, count, tail, np.random.default_rng(k).uniform(0.5, 1.5, rows).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("low,T", [(-1e10, 1.0), (-1e30, 2.0), (None, 2.0)], ids=str)
+def test_a_masked_block_with_record_ids_in_it(gpu, ps, low, T, dtype):
+    """The same with record ids masked as well: they have probability 0 there."""
+    rows, V, k = 4, 9001, 40
+    z, idx, prob, count = td.inputs(rows, V, k, dtype, T, 5, 1, 1)
+    low = torch.finfo(dtype).min if low is None else low
+    z[:, : V // 2] = low
+    prob[idx < V // 2] = 0.0
+    for tail in (0, 1):
+        td.run_all(ps, z, V, T, idx, prob, count, tail, np.ones(rows, np.float32))
