@@ -8,7 +8,9 @@
 // What bounds it: the row is read once (forward) and the gradient written once, at the rate of a copy where both are in one call (2048 rows of 128,256 fp32 with records of
 // 1024 450 us = 4.7 TB/s, 4096 of 151,936 bf16 500 us = 5.0 TB/s); the forward alone is at 5.5 TB/s with short records.  With the gradient in the same call a row is
 // read twice by its workgroup, but for what a thread holds of it, and the second time from the caches.
-// qt is summed directly: 1 - sum_j q_j loses it where the record holds nearly all of q, and the gradient off the record has pt / qt in it.
+// qt is summed directly: 1 - sum_j q_j loses it where the record holds nearly all of q, and the gradient off the record has pt / qt in it. What is off the record is summed and, in
+// the gradient, formed against its own largest logit R, not M: 87 T below M fp32 weights are 0, where pt q_v / qt still is of the size of pt. Against M stands one factor,
+// 2^((R - M) c), in 64 bits; where they do not hold it either (745 T) nothing is off the record.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -20,6 +22,18 @@ namespace {
 template <bool BF16> constexpr uint32_t kMaskedPair = BF16 ? 0xFF80FF80u : 0xFF800000u;
 
 constexpr float kNoReference = -67108864.f;      // -2^26: above it r is no more than 2 below the largest exponent
+
+// 2^a, -1200 <= a <= 0 (common.hpp's without its branch, behind which the compiler takes 40 registers more here)
+__device__ __forceinline__ double exp2_down(double a)
+{
+    const double n = rint(a);
+    return ldexp((double)__builtin_amdgcn_exp2f((float)(a - n)), (int)n);
+}
+
+// two floats as one word, of a hand-over or of the statistics
+__device__ __forceinline__ unsigned long long two_floats(float a, float b) { return (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32; }
+__device__ __forceinline__ float first_float(unsigned long long w) { return __uint_as_float((uint32_t)w); }
+__device__ __forceinline__ float second_float(unsigned long long w) { return __uint_as_float((uint32_t)(w >> 32)); }
 
 enum Slots : int { kNone, kEntries, kHalves };  // of a long record, in LDS
 
@@ -107,7 +121,7 @@ __device__ __forceinline__ void store_one(char* grad_row, int x, float g)
 // Weights are 2^(z c - r), c = log2(e) / T in fp32 and r an integer that is the same for a wave, near its largest exponent: one fused multiply-add and one
 // exponential per element (the product inside is exact, so the error is that of (z - M) c).  r moves up, and the lanes' sums are rescaled, only when an element
 // lies more than 2^64 above it.  What a wave has seen so far may be ids masked with a finite value, of which r would have no more than fp32's 24 bits and the exponents
-// be what its rounding leaves, 2^439 for -1e10: below kNoReference r is not taken and the weights are 0 (a row of no more than that has |M c| >= 2^24).  Rows with |M c| >= 2^24, where r is no integer near M c any more, take (z - M) c and read the row once more.
+// be what its rounding leaves, 2^439 for -1e10: below kNoReference r is not taken and the weights are 0 (a row of no more than that has |R c| >= 2^24).  Rows with |R c| >= 2^24, where r is no integer near R c any more, take (z - R) c and read the row once more.
 //
 // What the record's entries need of the row, and the row of them (SLOTS):
 //   entries The record lies in LDS in the order of its ids: a bit per element, the number of bits in front of every 32, and the entries' p.  The streaming finds the
@@ -118,7 +132,7 @@ __device__ __forceinline__ void store_one(char* grad_row, int x, float g)
 //           of the row each way.  For short records, and for vocabularies whose marks do not fit (kDistillLds).
 // SPLIT: a row's workgroups take consecutive trips of it; forward, the last of them to arrive adds their sums up and goes on with the record.
 template <bool BF16, bool FWD, bool GRAD, bool TAIL, int SLOTS, bool SPLIT, int kDT, int HELD>
-__global__ __launch_bounds__(kDT, HELD ? 4 : kDT / 256) void distill_kernel(const DistillArgs a)
+__global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 8 : kDT / 256) void distill_kernel(const DistillArgs a)
 {
     constexpr int N = Vec<BF16>::N, G = 2, kDW = kDT / kWave;    // G: vectors per step
     static_assert(HELD % G == 0 && HELD <= kDistillMostHeld && G + 1 <= kDistillAhead && (!SPLIT || (HELD == 0 && !SLOTS && FWD != GRAD)), "whole steps; split rows in the plainest form");
@@ -259,11 +273,11 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : kDT / 256) void distill_kernel(cons
         }
     };
 
-    float M;
-    double S, b, mass, whole;
+    float M, R;                                                     // largest logits: of the row, and of what is off the record (without TAIL: of the row)
+    double S, b, mass, whole;                                       // sum of weights against M; of what is off the record: T dL/dz per weight against R; sum p; W
     if constexpr (FWD) {
-        // the row's maximum and the sum: over all elements, TAIL over those off the record
-        float mx = kNegInf, r = kNegInf, s = 0.f;
+        // the row's maximum and the sum: over all elements, TAIL over those off the record, whose maximum is mo
+        float mx = kNegInf, mo = kNegInf, r = kNegInf, s = 0.f;
         auto values = [&](int q, const uint4& raw, float (&t)[N]) {           // -inf: not in the sum
             unpack<BF16>(raw, t);
             unsigned out = 0u;
@@ -309,7 +323,8 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : kDT / 256) void distill_kernel(cons
             float bm = v[0];
 #pragma unroll
             for (int e = 1; e < G * N; ++e) bm = fmaxf(bm, v[e]);
-            if constexpr (!TAIL || SLOTS) mx = fmaxf(mx, bm);                  // (SLOTS: the record's come behind the stream)
+            if constexpr (TAIL) mo = fmaxf(mo, bm);
+            else mx = fmaxf(mx, bm);
             if (__ballot(bm * c > r + 64.f)) {                                // (uniform; the first step, and outliers)
                 const float rn = ceilf(wave_max(bm) * c);
                 if (rn > r && rn > kNoReference) { s *= __builtin_amdgcn_exp2f(r - rn); r = rn; }   // (r = -inf: s is 0 and stays 0)
@@ -352,42 +367,48 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : kDT / 256) void distill_kernel(cons
                 mine[j].z = __uint_as_float(bits);
             }
         }
-        if constexpr (TAIL && SLOTS) each_entry([&](const Entry& e) { mx = fmaxf(mx, e.z); });
-        const float wm = wave_max(mx);
-        if (lane == 0) sh[wave] = (double)wm;
+        if constexpr (TAIL && SLOTS) {                            // (the record's come behind the stream)
+            mx = mo;
+            each_entry([&](const Entry& e) { mx = fmaxf(mx, e.z); });
+        }
+        const float wm = wave_max(mx), wo = TAIL ? wave_max(mo) : wm;
+        unsigned long long* const maxima = reinterpret_cast<unsigned long long*>(sh);
+        if (lane == 0) maxima[wave] = two_floats(wm, wo);
         __syncthreads();
-        M = kNegInf;
+        M = R = kNegInf;
 #pragma unroll
-        for (int w = 0; w < kDW; ++w) M = fmaxf(M, (float)sh[w]);
+        for (int w = 0; w < kDW; ++w) { M = fmaxf(M, first_float(maxima[w])); R = TAIL ? fmaxf(R, second_float(maxima[w])) : M; }
         __syncthreads();
-        double sums[5] = {0.0, 0.0, 0.0, 0.0, 0.0};               // the weights; p, p log2 p, p log2(e) y and (TAIL) w of the record
-        if (fabsf(M * c) < 16777216.f) {
-            sums[0] = r == kNegInf ? (double)s : (double)s * exp2_split((double)r - (double)M * (double)c);
-        } else if (M > kNegInf) {
+        double sums[5] = {0.0, 0.0, 0.0, 0.0, 0.0};               // the weights against R; p, p log2 p, p log2(e) y and (TAIL) w of the record, against M
+        if (fabsf(R * c) < 16777216.f) {
+            sums[0] = r == kNegInf ? (double)s : (double)s * exp2_split((double)r - (double)R * (double)c);
+        } else if (R > kNegInf) {
             for (int i = begin; i < trips; ++i) {
                 float t[N];
                 values(i * kDT + tid, load(i, Keep{}), t);
 #pragma unroll
-                for (int e = 0; e < N; ++e) sums[0] += (double)exp_stream(t[e], M, c);
+                for (int e = 0; e < N; ++e) sums[0] += (double)exp_stream(t[e], R, c);
             }
         }
         if constexpr (SPLIT) {
-            // (M and the sum of this part; together in the last of the row's workgroups to arrive)
+            // (the maxima and the sum of this part; together in the last of the row's workgroups to arrive)
             unsigned long long* const word = reinterpret_cast<unsigned long long*>(a.scratch + row * (int64_t)distill_scratch_row(parts));
             unsigned long long* const shares = word + kArrivalStride / 8;
             double mine[1] = {sums[0]};
             block_sums<kDW>(mine, sh);
             if (tid == 0) {
-                put_shared(&shares[2 * part], (unsigned long long)__float_as_uint(M));
+                put_shared(&shares[2 * part], two_floats(M, R));
                 put_shared(&shares[2 * part + 1], (unsigned long long)__double_as_longlong(mine[0]));
             }
             if (!arrive_last(word, (unsigned)parts, tid == 0)) return;
             if (own.id >= 0) own.z = logit_at<BF16>(a.logits, a.ld, row, own.id);
             static_assert(kDistillMostParts <= kWave, "a lane for each part");
-            const float m = lane < parts ? __uint_as_float((uint32_t)get_shared(&shares[2 * lane])) : kNegInf;
+            const unsigned long long of_part = lane < parts ? get_shared(&shares[2 * lane]) : two_floats(kNegInf, kNegInf);
             const double s_part = lane < parts ? __longlong_as_double((long long)get_shared(&shares[2 * lane + 1])) : 0.0;
-            M = wave_max(m);
-            sums[0] = wave_sum(m == M ? s_part : s_part * exp2_split(((double)m - (double)M) * (double)c));
+            const float ref = second_float(of_part);
+            M = wave_max(first_float(of_part));
+            R = wave_max(ref);
+            sums[0] = wave_sum(ref == R ? s_part : s_part * exp2_split(((double)ref - (double)R) * (double)c));
             if (tid != 0) sums[0] = 0.0;
         }
         each_entry([&](const Entry& e) {
@@ -400,48 +421,53 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : kDT / 256) void distill_kernel(cons
         });
         block_sums<kDW>(sums, sh);
         mass = sums[1];
-        S = sums[0] + sums[4];
+        const double gap = TAIL ? fmax(((double)R - (double)M) * c64, -1200.0) : 0.0, to_M = TAIL ? exp2_down(gap) : 1.0, off_mass = sums[0] * to_M;
+        S = off_mass + sums[4];
         double pt = 0.0;
         if constexpr (TAIL) {
             pt = mass < 1.0 ? 1.0 - mass : 0.0;
-            b = whole = mass + pt;
-            if (pt > 0.0) b = sums[0] > 0.0 ? whole - pt * S / sums[0] : 0.0;  // (nothing left off the record: every q there is 0)
+            whole = mass + pt;
+            b = off_mass > 0.0 ? whole * to_M / S - pt / sums[0] : 0.0;       // (nothing off the record: every q there is 0)
         } else {
-            b = whole = mass > 0.0 ? 1.0 : 0.0;
+            whole = mass > 0.0 ? 1.0 : 0.0;
+            b = S > 0.0 ? whole / S : 0.0;
         }
         if (tid == 0) {
             const double lnS = log(S);
             double loss = 0.0;
             const double plain = (sums[2] - sums[3]) * 0.69314718055994531;    // sum of p (ln p - y)
             if (mass > 0.0) loss = TAIL ? plain + mass * lnS : plain / mass - log(mass) + lnS;
-            if (pt > 0.0) loss += pt * (log(pt) - log(sums[0]) + lnS);
+            if (pt > 0.0) loss += off_mass > 0.0 ? pt * (log(pt) - (log(sums[0]) + gap * 0.69314718055994531) + lnS) : (double)INFINITY;
             // (a row that is masked whole: there is no q, and nothing is learnt from it)
             a.loss[row] = M == kNegInf ? 0.f : (float)loss;
-            if (a.stats) a.stats[row] = make_double4((double)M, S, b, mass);
+            if (a.stats) a.stats[row] = make_double4(__longlong_as_double((long long)two_floats(M, R)), S, b, TAIL ? whole : mass);
         }
     } else {
         const double4 st = a.stats[row];
-        M = (float)st.x; S = st.y; b = st.z; mass = st.w;
-        whole = TAIL ? mass + (mass < 1.0 ? 1.0 - mass : 0.0) : b;
+        const unsigned long long maxima = (unsigned long long)__double_as_longlong(st.x);
+        M = first_float(maxima); R = second_float(maxima); S = st.y; b = st.z; mass = st.w;
+        whole = TAIL ? st.w : mass > 0.0 ? 1.0 : 0.0;
     }
 
     if constexpr (GRAD) {
         const double scale = (a.weight ? (double)a.weight[row] : 1.0) / (double)a.T;
-        const bool masked = M == kNegInf, far = !(fabsf(M * c) < 16777216.f);
-        const float nr = far ? 0.f : -(M * c);
-        // (what the rounding of M c puts into every exponent is taken out of the factor)
-        const float off = masked ? 0.f : (float)(scale * b / S * (far ? 1.0 : exp2_split((double)M * -(double)c - (double)nr)));
-        // of a marked element: on_w w - on_p p, in 64 bits (the two are often near each other)
-        const double on_w = masked ? 0.0 : scale * whole / S * (far ? 1.0 : exp2_split((double)M * -(double)c - (double)nr));
+        const bool masked = M == kNegInf;
+        const bool near = fabsf(R * c) < 16777216.f, far = !near && R > kNegInf;
+        const float nr = near ? -(R * c) : 0.f;
+        // (what the rounding of R c puts into every exponent is taken out of the factor)
+        const double fix = near ? exp2_split((double)R * -(double)c - (double)nr) : 1.0;
+        const float off = masked ? 0.f : (float)(scale * b * fix);
+        // of a marked element: on_w w - on_p p, w against M (with TAIL as (z - M) c), in 64 bits (the two are often near each other)
+        const double on_w = masked ? 0.0 : scale * whole / S * (TAIL ? 1.0 : fix);
         const double on_p = masked ? 0.0 : TAIL ? scale : mass > 0.0 ? scale / mass : 0.0;
         auto put = [&](int i, const uint4& raw, auto far_tag) {
             const int q = i * kDT + tid;
             if (q >= nq) return;
-            float t[N], w[N];
-            unpack<BF16>(raw, t);
+            float z[N], t[N], w[N];
+            unpack<BF16>(raw, z);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                w[e] = decltype(far_tag)::value ? exp_stream(t[e], masked ? 0.f : M, c) : __builtin_amdgcn_exp2f(fmaf(t[e], c, nr));
+                w[e] = decltype(far_tag)::value ? exp_stream(z[e], R, c) : __builtin_amdgcn_exp2f(fmaf(z[e], c, nr));
                 t[e] = off * w[e];
             }
             if constexpr (SLOTS) {
@@ -449,7 +475,11 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : kDT / 256) void distill_kernel(cons
                 const unsigned in = marks(q, slot);
                 if (__ballot(in != 0u)) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) if ((in >> e) & 1u) t[e] = (float)((double)w[e] * on_w - (double)slot_p[slot++] * on_p);
+                    for (int e = 0; e < N; ++e)
+                        if ((in >> e) & 1u) {
+                            if constexpr (TAIL) w[e] = exp_stream(z[e], masked ? 0.f : M, c);
+                            t[e] = (float)((double)w[e] * on_w - (double)slot_p[slot++] * on_p);
+                        }
                 }
             }
             store_vec<BF16>(grad_row, rv, q, t);

@@ -141,3 +141,44 @@ def test_a_masked_block_with_record_ids_in_it(gpu, ps, low, T, dtype):
     prob[idx < V // 2] = 0.0
     for tail in (0, 1):
         td.run_all(ps, z, V, T, idx, prob, count, tail, np.ones(rows, np.float32))
+
+
+# ---------------------------------------------------------------- the loss: what is off the record far below what is on it
+
+def _gapped(rows, V, k, dtype, T, gap, seed):
+    """Logits whose record ids lie `gap` nats above all others, and records with 0.99 of the mass."""
+    rng = np.random.default_rng(seed)
+    s = rng.normal(size=(rows, V)) - gap
+    idx = np.stack([rng.choice(V, k, replace=False) for _ in range(rows)]).astype(np.int32)
+    np.put_along_axis(s, idx, np.clip(rng.normal(size=(rows, k)), -3.0, 3.0), 1)
+    p = rng.random((rows, k)) + 0.1
+    z = torch.zeros(rows, V + 3, dtype=dtype, device="cuda")[:, :V]
+    z.copy_(torch.from_numpy(s * T).to(dtype))
+    return z, idx, (p / p.sum(1, keepdims=True) * 0.99).astype(np.float32), np.full(rows, k, np.int32)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("gap,T", [(20.0, 1.0), (80.0, 1.0), (95.0, 1.0), (110.0, 1.0), (110.0, 0.1), (300.0, 1.0), (300.0, 4.0), (700.0, 1.0), (700.0, 0.01)], ids=str)
+@pytest.mark.parametrize("rows,V,k", [(3, 1000, 12), (4, 9001, 300), (4, 9001, 1500), (600, 2049, 600), (3, 70001, 20), (66, 61001, 900)], ids=str)
+def test_the_tail_far_below_the_record(gpu, ps, rows, V, k, gap, T, dtype):
+    """The gradient off the record has a sum of -pt q_v / qt = -pt however small qt is, as long as 64 bits hold it."""
+    print(f"[case] distill gap {gap} T={T} {rows} x {V} k={k} {dtype}", flush=True)
+    z, idx, prob, count = _gapped(rows, V, k, dtype, T, gap, k)
+    d = td.run_all(ps, z, V, T, idx, prob, count, 1, np.ones(rows, np.float32))
+    on = torch.from_numpy(idx.astype(np.int64)).cuda()
+    off = d.grad.double().scatter(1, on, 0.0)
+    assert ((off.sum(1) * T + 0.01).abs() <= 0.01 * 2.0 ** -7).all()             # (all of one sign: bf16's roundings, 2^-8 relative each)
+
+
+def test_the_tail_far_below_a_record_far_from_zero(gpu, ps):
+    """The same where the exponents are beyond the fused form: offsets that all logits share, of which fp32 holds steps of 2 nats."""
+    rows, V, k = 4, 9001, 300
+    for k in (12, 300):
+        rng = np.random.default_rng(8)
+        s = 3.0e7 - 300.0 + 2.0 * rng.integers(0, 6, (rows, V))
+        idx = np.stack([rng.choice(V, k, replace=False) for _ in range(rows)]).astype(np.int32)
+        np.put_along_axis(s, idx, 3.0e7 + 2.0 * rng.integers(0, 4, (rows, k)), 1)
+        p = rng.random((rows, k)) + 0.1
+        z = torch.from_numpy(s).float().cuda()
+        assert (z.double().cpu().numpy() == s).all()
+        td.run_all(ps, z, V, 1.0, idx, (p / p.sum(1, keepdims=True) * 0.99).astype(np.float32), np.full(rows, k, np.int32), 1, np.ones(rows, np.float32))
