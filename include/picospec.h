@@ -451,7 +451,8 @@ int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, i
  * Distillation on the target's Top-K records (what picospec_compress makes of the target's rows): for each of n_rows rows of
  * the drafter's logits, q = softmax(z / T), the Kullback-Leibler divergence of q from the record (id_j, p_j), j < count:
  *   tail 0   loss = sum_j ph_j (ln ph_j - ln q_j),  ph_j = p_j / sum p
- *   tail 1   loss = sum_j p_j (ln p_j - ln q_j) + pt (ln pt - ln qt),  pt = max(0, 1 - sum p) and qt = the mass of q off the record
+ *   tail 1   loss = sum_j p_j (ln p_j - ln q_j) + pt (ln pt - ln qt),  pt = max(0, 1 - sum p) and qt = the mass of q off the record;
+ *            where qt = 0, a pt of at most 2^-20 is what rounding left of a record of all that the row allows, and counts as 0
  * and accept = sum_j min(p_j, q_j), the probability with which a token drawn from q is accepted against the record's p.
  *   logits [n_rows, ld]; idx, prob [n_rows, k], count [n_rows]: k in 1..min(V, picospec_limit(MAX_K)), count clamped to
  *            0..k, p_j >= 0; the ids of a record differ; entries whose id lies outside [0, V) are passed over        in

@@ -21,6 +21,10 @@ namespace {
 // two (bf16) or one (fp32) values of -inf
 template <bool BF16> constexpr uint32_t kMaskedPair = BF16 ? 0xFF80FF80u : 0xFF800000u;
 
+// What the roundings of a record's entries may leave of 1: half a step of fp32 each, 2^-24 of their sum, and what they share of the error of their
+// row's sum (records of picospec_compress: a few 10^-7)
+constexpr double kRounding = 0x1p-20;
+
 constexpr float kNoReference = -67108864.f;      // -2^26: above it r is no more than 2 below the largest exponent
 
 // 2^a, -1200 <= a <= 0 (common.hpp's without its branch, behind which the compiler takes 40 registers more here)
@@ -426,6 +430,7 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 
         double pt = 0.0;
         if constexpr (TAIL) {
             pt = mass < 1.0 ? 1.0 - mass : 0.0;
+            if (off_mass == 0.0 && pt <= kRounding) pt = 0.0;                  // (a record of all that the row allows)
             whole = mass + pt;
             b = off_mass > 0.0 ? whole * to_M / S - pt / sums[0] : 0.0;       // (nothing off the record: every q there is 0)
         } else {

@@ -182,3 +182,57 @@ def test_the_tail_far_below_a_record_far_from_zero(gpu, ps):
         z = torch.from_numpy(s).float().cuda()
         assert (z.double().cpu().numpy() == s).all()
         td.run_all(ps, z, V, 1.0, idx, (p / p.sum(1, keepdims=True) * 0.99).astype(np.float32), np.full(rows, k, np.int32), 1, np.ones(rows, np.float32))
+
+
+# ---------------------------------------------------------------- the loss: records that hold all of the row's support
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,k,low", [(4, 300, 300, 0.0), (4, 4096, 4096, 0.0), (5, 9001, 20, -math.inf), (5, 9001, 1500, None), (600, 2049, 600, None), (3, 70001, 20, -1e30)], ids=str)
+def test_a_record_of_all_of_the_support(gpu, ps, rows, V, k, low, dtype):
+    """All that top-k can keep is in the record, and nothing has any mass off it: what the entries' roundings leave of 1 is no tail.  Where a record leaves more than
+    that, the loss is infinite."""
+    rng = np.random.default_rng(k)
+    idx = np.stack([rng.choice(V, k, replace=False) for _ in range(rows)]).astype(np.int32)
+    z = torch.full((rows, V), torch.finfo(dtype).min if low is None else low, dtype=dtype, device="cuda")
+    z.scatter_(1, torch.from_numpy(idx.astype(np.int64)).cuda(), torch.from_numpy(rng.normal(size=(rows, k))).to(dtype).cuda())
+    p = rng.random((rows, k)) + 0.1
+    p /= p.sum(1, keepdims=True)
+    left = np.array([2.0 ** -24, 2.0 ** -22, -2.0 ** -23, 2.0 ** -21, 1e-3])[np.arange(rows) % 5]
+    prob = (p * (1.0 - left[:, None])).astype(np.float32)
+    count = np.full(rows, k, np.int32)
+    short = left == 1e-3
+    z64, p64 = z.double().cpu().numpy(), prob.astype(np.float64)
+    assert (1.0 - p64.sum(1))[left > 0].min() > 0.0
+    lnq = np.take_along_axis(z64 - np.log(np.exp(z64).sum(1, keepdims=True)), idx, 1)
+    loss = (p64 * (np.log(p64) - lnq)).sum(1)
+    loss[short] = np.inf
+    whole = np.where(short, 1.0, p64.sum(1))
+    grad, tol = np.zeros((rows, V)), np.zeros((rows, V))
+    np.put_along_axis(grad, idx, whole[:, None] * np.exp(lnq) - p64, 1)
+    np.put_along_axis(tol, idx, td.E * np.exp(lnq) + 2.0 ** -40, 1)
+    from paper_2603_19133_amd.training import distill_loss
+    rec = td.record(ps, idx, prob, count)
+    d = ps.distill(z, V, 1.0, rec, tail=1, grad=True)
+    f = ps.distill(z, V, 1.0, rec, tail=1)
+    leaf = z.detach().requires_grad_()
+    lo, _ = distill_loss(leaf, rec, V, 1.0, tail=1)
+    lo.sum().backward()
+    for t in (d.loss, f.loss, lo):
+        assert torch.equal(torch.isinf(t.detach().cpu()), torch.from_numpy(short))
+        td.check(t, loss, td.E)
+    for t in (d.grad, ps.distill_grad(z, V, 1.0, rec, f.stats, tail=1), leaf.grad):
+        td.check(t, grad, tol, dtype)
+
+
+def test_records_of_compress_of_all_of_the_support(gpu, ps):
+    """What the framework's own records of a whole vocabulary, and of rows of which a grammar allows fewer ids than the record has places, leave of 1 by rounding."""
+    for V, k in ((4096, 4096), (5003, 64)):
+        z, _ = ts.rows_of(64, V, torch.float32, "normal", V)
+        if k < V:
+            z[:, : V - 50] = -math.inf
+        rec = ps.compress(z, V, 0.9, k)
+        left = 1.0 - rec.prob.double().sum(1) if k == V else 1.0 - torch.where(torch.arange(k, device="cuda") < rec.count[:, None], rec.prob, 0.0).double().sum(1)
+        assert (left > 0).any() and left.max() < 2.0 ** -20
+        s = torch.where(z > -1e30, z * 0.9, z)
+        d = ps.distill(s, V, 0.9, rec, tail=1, grad=True)
+        assert torch.isfinite(d.loss).all() and torch.isfinite(d.grad).all()
