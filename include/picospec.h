@@ -465,7 +465,7 @@ int picospec_sample(const void* logits, int dtype, int64_t ld, int32_t n_rows, i
  *            several workgroups; NULL or a smaller one: one workgroup per row (sums in another order: they agree to rounding)
  * What is off the record has mass as long as 64 bits hold it: from 745 T below the row's largest logit on, as ids masked with a finite value are, it has none.
  * Rows with count 0 (positions that are not trained on) and rows without a logit above -inf have loss, accept and gradient 0.
- * A record id whose logit is -inf has loss +inf (its gradient is finite); NaN and +inf logits make a row's results NaN.
+ * A record id whose logit is -inf has loss +inf (its gradient is finite); NaN and +inf logits, wherever they lie, make all of a row's results NaN.
  * picospec_distill_grad forms the gradient alone, from the stats of an earlier picospec_distill of the same logits and
  * records: what a framework with a tape calls backwards.
  */

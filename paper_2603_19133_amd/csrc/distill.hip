@@ -11,6 +11,7 @@
 // qt is summed directly: 1 - sum_j q_j loses it where the record holds nearly all of q, and the gradient off the record has pt / qt in it. What is off the record is summed and, in
 // the gradient, formed against its own largest logit R, not M: 87 T below M fp32 weights are 0, where pt q_v / qt still is of the size of pt. Against M stands one factor,
 // 2^((R - M) c), in 64 bits; where they do not hold it either (745 T) nothing is off the record.
+// The maxima pass NaN by; the sums carry it: S of a row with NaN or +inf in it is NaN, M of it may be anything, -inf as of a row that is masked whole.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -384,9 +385,9 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 
         for (int w = 0; w < kDW; ++w) { M = fmaxf(M, first_float(maxima[w])); R = TAIL ? fmaxf(R, second_float(maxima[w])) : M; }
         __syncthreads();
         double sums[5] = {0.0, 0.0, 0.0, 0.0, 0.0};               // the weights against R; p, p log2 p, p log2(e) y and (TAIL) w of the record, against M
-        if (fabsf(R * c) < 16777216.f) {
+        if (fabsf(R * c) < 16777216.f || R == kNegInf) {         // (nothing but masked ids: s is 0, or NaN)
             sums[0] = r == kNegInf ? (double)s : (double)s * exp2_split((double)r - (double)R * (double)c);
-        } else if (R > kNegInf) {
+        } else {
             for (int i = begin; i < trips; ++i) {
                 float t[N];
                 values(i * kDT + tid, load(i, Keep{}), t);
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 
             if (tid != 0) sums[0] = 0.0;
         }
         each_entry([&](const Entry& e) {
-            if constexpr (TAIL) sums[4] += exp_emit(e.z, M, c64);
+            if constexpr (TAIL) sums[4] += e.z < __builtin_huge_valf() ? exp_emit(e.z, M, c64) : (double)NAN;
             if (e.p > 0.f) {
                 sums[1] += (double)e.p;
                 sums[2] += (double)e.p * log2_of(e.p);
@@ -432,19 +433,19 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 
             pt = mass < 1.0 ? 1.0 - mass : 0.0;
             if (off_mass == 0.0 && pt <= kRounding) pt = 0.0;                  // (a record of all that the row allows)
             whole = mass + pt;
-            b = off_mass > 0.0 ? whole * to_M / S - pt / sums[0] : 0.0;       // (nothing off the record: every q there is 0)
+            b = off_mass > 0.0 ? whole * to_M / S - pt / sums[0] : S - S;     // (nothing off the record: every q there is 0; or NaN)
         } else {
             whole = mass > 0.0 ? 1.0 : 0.0;
-            b = S > 0.0 ? whole / S : 0.0;
+            b = S == 0.0 ? 0.0 : whole / S;
         }
         if (tid == 0) {
             const double lnS = log(S);
-            double loss = 0.0;
+            double loss = S - S;                                              // (0, or NaN)
             const double plain = (sums[2] - sums[3]) * 0.69314718055994531;    // sum of p (ln p - y)
-            if (mass > 0.0) loss = TAIL ? plain + mass * lnS : plain / mass - log(mass) + lnS;
+            if (mass > 0.0) loss += TAIL ? plain + mass * lnS : plain / mass - log(mass) + lnS;
             if (pt > 0.0) loss += off_mass > 0.0 ? pt * (log(pt) - (log(sums[0]) + gap * 0.69314718055994531) + lnS) : (double)INFINITY;
             // (a row that is masked whole: there is no q, and nothing is learnt from it)
-            a.loss[row] = M == kNegInf ? 0.f : (float)loss;
+            a.loss[row] = S == 0.0 ? 0.f : (float)loss;
             if (a.stats) a.stats[row] = make_double4(__longlong_as_double((long long)two_floats(M, R)), S, b, TAIL ? whole : mass);
         }
     } else {
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 
 
     if constexpr (GRAD) {
         const double scale = (a.weight ? (double)a.weight[row] : 1.0) / (double)a.T;
-        const bool masked = M == kNegInf;
+        const bool masked = S == 0.0;
         const bool near = fabsf(R * c) < 16777216.f, far = !near && R > kNegInf;
         const float nr = near ? -(R * c) : 0.f;
         // (what the rounding of R c puts into every exponent is taken out of the factor)
@@ -513,13 +514,13 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 
             const double per_S = 1.0 / S;
             each_entry([&](const Entry& e) { acc[0] += fmin((double)e.p, exp_emit(e.z, M, c64) * per_S); });
             block_sums<kDW>(acc, sh);
-            if (tid == 0) a.accept[row] = M == kNegInf ? 0.f : (float)acc[0];
+            if (tid == 0) a.accept[row] = S == 0.0 ? 0.f : (float)(acc[0] + (S - S));
         }
     }
     if constexpr (GRAD && !SLOTS) {
         // the record's own entries over what the streaming wrote in their places
         const double scale = (a.weight ? (double)a.weight[row] : 1.0) / (double)a.T;
-        const bool masked = M == kNegInf;
+        const bool masked = S == 0.0;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         const double on = TAIL ? 1.0 : mass > 0.0 ? 1.0 / mass : 0.0, per_S = whole / S;

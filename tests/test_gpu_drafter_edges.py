@@ -236,3 +236,47 @@ def test_records_of_compress_of_all_of_the_support(gpu, ps):
         s = torch.where(z > -1e30, z * 0.9, z)
         d = ps.distill(s, V, 0.9, rec, tail=1, grad=True)
         assert torch.isfinite(d.loss).all() and torch.isfinite(d.grad).all()
+
+
+# ---------------------------------------------------------------- the loss: NaN and +inf
+
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V,k", [(3001, 16), (9001, 300), (9001, 2000), (90001, 16)])
+def test_nan_and_inf_make_a_row_nan(gpu, ps, V, k, dtype, tail):
+    """Loss, acceptance and every element of the gradient: NaN throughout the row, among nothing but masked ids, in all of one workgroup's share of it, on the record
+    (with probability 0 as well), off it; +inf on and off it.  The other rows keep their bits."""
+    from paper_2603_19133_amd.training import distill_loss
+    z, idx, prob, count = td.inputs(12, V, k, dtype, 1.0, 3)
+    prob[6, 4] = 0.0
+    rec = td.record(ps, idx, prob, count)
+
+    def outputs():
+        d = ps.distill(z, V, 1.0, rec, tail=tail, grad=True)
+        f = ps.distill(z, V, 1.0, rec, tail=tail)
+        g = ps.distill_grad(z, V, 1.0, rec, f.stats, tail=tail)
+        leaf = z.detach().requires_grad_()
+        lo, ac = distill_loss(leaf, rec, V, 1.0, tail=tail)
+        lo.sum().backward()
+        torch.cuda.synchronize()
+        return [d.loss, f.loss, lo.detach(), d.accept, f.accept, ac], [d.grad, g, leaf.grad]
+    want = outputs()
+    off = [next(x for x in range(V // 2, V) if x not in set(idx[r].tolist())) for r in range(12)]
+    z[1] = math.nan
+    z[2] = -math.inf
+    z[2, off[2]] = math.nan
+    z[3, : V // 3] = math.nan
+    z[4, int(idx[4, 4])] = math.nan
+    z[5, off[5]] = math.nan
+    z[6, int(idx[6, 4])] = math.nan
+    z[7, int(idx[7, 4])] = math.inf
+    z[8, off[8]] = math.inf
+    z[9] = math.inf
+    z[10, ::2], z[10, 1::2] = math.inf, math.nan
+    got = outputs()
+    for t in got[0]:
+        assert torch.isnan(t[1:11]).all(), t
+    for t in got[1]:
+        assert torch.isnan(t[1:11].float()).all(), (~torch.isnan(t.float())).sum(1)
+    for a, b in zip(got[0] + got[1], want[0] + want[1]):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[11], b[11])
