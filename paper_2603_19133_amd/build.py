@@ -3,6 +3,7 @@ Run as ``python -m paper_2603_19133_amd.build``."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 
@@ -37,6 +38,17 @@ def build(verbose: bool = False, extra: list[str] | None = None, out: str | None
     return out
 
 
+def hip_include() -> str:
+    """ROCm's include directory: the compiler's own where HIPCC names it by path or finds it on PATH, else the one of ROCM_PATH or of the default place."""
+    found = shutil.which(HIPCC)
+    roots = [os.path.dirname(os.path.dirname(os.path.realpath(found)))] if found else []
+    roots += [os.environ.get("ROCM_PATH", ""), "/opt/rocm"]
+    for root in roots:
+        if root and os.path.isfile(os.path.join(root, "include", "hip", "hip_runtime_api.h")):
+            return os.path.join(root, "include")
+    raise RuntimeError(f"no HIP headers beside {HIPCC}, nor in {' or '.join(r for r in roots if r)}")
+
+
 def build_native(verbose: bool = False) -> str:
     """Compiles the binding's extension module against the torch that is installed; links libpicospec.so, which must be built."""
     import sysconfig
@@ -47,7 +59,7 @@ def build_native(verbose: bool = False) -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           *[f"-I{p}" for p in (*include_paths(), sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"))],
+           *[f"-I{p}" for p in (*include_paths(), sysconfig.get_paths()["include"], hip_include())],
            "-o", NATIVE, os.path.join(CSRC, "native.cpp"),
            f"-L{HERE}", "-l:libpicospec.so", "-Wl,-rpath,$ORIGIN", f"-L{torch_lib}", f"-Wl,-rpath,{torch_lib}",
            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"]
