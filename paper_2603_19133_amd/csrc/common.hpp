@@ -441,6 +441,10 @@ __device__ __forceinline__ void row_stats_row(
     }
 }
 
+// Whether a sum of 2^(z c - r), z <= m, stays in fp32's range: r is an fp32 number near m c. Where m is a mask of a large finite value, that is off by up to half of its own step,
+// 2^9 for -1e10, and sums of such terms are infinite, which no factor of 0 takes back when they meet those of ids that are not masked.
+__device__ __forceinline__ bool reference_holds(float m, float c, float r) { return !(fmaf(m, c, -r) > 64.f); }
+
 // The same statistics, and besides them the row's exponential sums segment by segment (what lets the residual draw
 // locate its token without a second pass over the row).  A wave owns NV * 64 consecutive vectors per trip, one
 // segment; segment `it * WAVES + wave` of the row gets (t, r): the sum over its elements of 2^(z c - r), c = log2(e) / T,
@@ -521,10 +525,10 @@ __device__ __forceinline__ void row_stats_seg_row(
             for (int e = 1; e < E; ++e) bm = fmaxf(bm, v[e]);
             mx[f] = fmaxf(mx[f], bm);
             if (__ballot(bm * c > r_w[f] + 64.f)) {                  // (uniform; the first trip, and outliers)
-                const float rn = ceilf(wave_max(bm) * c);
-                if (rn > r_w[f]) { s[f] *= __builtin_amdgcn_exp2f(r_w[f] - rn); r_w[f] = rn; }   // r_w = -inf: s is 0 and stays 0
+                const float wm = wave_max(bm), rn = ceilf(wm * c);
+                if (rn > r_w[f] && reference_holds(wm, c, rn)) { s[f] *= __builtin_amdgcn_exp2f(r_w[f] - rn); r_w[f] = rn; }   // r_w = -inf: s is 0 and stays 0
             }
-            const float nr = r_w[f] == kNegInf ? 0.f : -r_w[f];     // waves that have seen only -inf so far
+            const float nr = r_w[f] == kNegInf ? 0.f : -r_w[f];     // waves that have seen only masked ids so far: weights of 0
             float acc = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) acc += __builtin_amdgcn_exp2f(fmaf(v[e], c, nr));
@@ -584,9 +588,9 @@ __device__ __forceinline__ float tree_sum(const F& f) {
 // a workgroup of four waves, each wave SPW consecutive segments of NV * 64 vectors whose loads are all in flight at once.
 // Entry: (sum of 2^(z c - r), m), m = the segment's largest logit and r = split_ref(m, c); a NaN in the segment makes its sum NaN.
 // The lanes' sums are added in fp64.
-__device__ __forceinline__ bool split_ref_fused(float m, float c) { return fabsf(m * c) < __builtin_huge_valf(); }
-// m c as the sums' reference: rounded to fp32 as in the fused form of their terms; exact where that overflows (a segment of
-// nothing but masked entries of the type's lowest value), whose terms are formed as (z - m) c
+__device__ __forceinline__ bool split_ref_fused(float m, float c) { return fabsf(m * c) < __builtin_huge_valf() && fabsf(fmaf(m, c, -(m * c))) <= 64.f; }
+// m c as the sums' reference: rounded to fp32 as in the fused form of their terms; exact where that overflows or is off by more than 64 (a segment of
+// nothing but ids masked with the type's lowest value, or with -1e10), whose terms are formed as (z - m) c
 __device__ __forceinline__ double split_ref(float m, float c) { return split_ref_fused(m, c) ? (double)(m * c) : (double)m * (double)c; }
 // The entry of segment s, whose vectors are raw, in every lane of the wave that holds them.
 template <bool BF16>

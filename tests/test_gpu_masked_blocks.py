@@ -1,0 +1,84 @@
+"""Vocabularies of which whole stretches are masked with a finite value, of which fp32 holds steps of hundreds: what a thread, a wave, a segment or a workgroup's share
+of a row sees may be masked altogether, and its reference exponent is then the mask's."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+import parity_util as pu
+from paper_2603_19133_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+
+LOW = [-1e9, -1e10, -1e20, -1e30, None]
+
+
+@pytest.fixture(scope="module")
+def ps():
+    from paper_2603_19133_amd import binding
+    return binding
+
+
+def _rows(n, V, dtype, low, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+    z = torch.randn(n, V, device="cuda", generator=g) * 3
+    m = torch.zeros(n, V, dtype=torch.bool, device="cuda")
+    m[0::5, : V // 2] = True
+    m[1::5, V // 2:] = True
+    m[2::5, V // 3: 2 * V // 3] = True
+    m[3::5] = True
+    m[3::5, V // 2: V // 2 + 500] = False
+    m[4::5, : V - 300] = True
+    return torch.where(m, torch.full_like(z, torch.finfo(dtype).min if low is None else low), z).to(dtype)
+
+
+def _close(got, want, rtol, what, atol=0.0):
+    assert np.isfinite(got).all(), what                            # (a comparison with NaN is no failure by itself)
+    pu.assert_close(got, want, rtol, what, atol)
+
+
+SHAPES = [(5, 700), (5, 9001), (5, 70001), (60, 40003), (300, 9001), (300, 40003)]
+TEMPERATURES = [1.0, 0.7, 2.0]
+
+
+@pytest.mark.parametrize("low", LOW, ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", TEMPERATURES)
+def test_row_statistics(gpu, ps, T, dtype, low):
+    for n, V in SHAPES:
+        print(f"[case] row_stats {n} x {V} {dtype} T={T} {low}", flush=True)
+        z = _rows(n, V, dtype, low, n + V)
+        want = torch.logsumexp(z.double() / float(np.float32(T)), 1).cpu().numpy()
+        mx, sm, lse = ps.row_stats(z, V, T)
+        _close(pu.n(lse), want, pu.RTOL_LSE, "lse", atol=1e-6)
+        _close(pu.n(mx) / T + np.log(pu.n(sm).astype(np.float64)), want, pu.RTOL_LSE, "max, sum", atol=1e-6)
+
+
+@pytest.mark.parametrize("low,T", [(-1e10, 1.0), (-1e20, 0.7), (None, 2.0)], ids=str)
+@pytest.mark.parametrize("name,scale", [("cfg1", {}), ("cfg2", {"B": 4, "V": 9001}), ("cfg3", {"B": 6, "V": 40003, "k": 200}), ("cfg5", {"B": 60, "V": 20011, "k": 300}),
+                                        ("cfg4", {"B": 12, "V": 50021, "k": 500})], ids=str)
+def test_rounds(gpu, ps, name, scale, low, T):
+    """A round whose draft and target rows are masked in blocks, by its separate calls and as one, with and without the target rows' segment table."""
+    print(f"[case] round {name} {scale} {low} T={T}", flush=True)
+    w = dataclasses.replace(W.WORKLOADS[name].scaled(**scale), T=T)
+    r = W.build_round(w)
+    dtype = torch.float32 if w.dtype == "f32" else torch.bfloat16
+    fill = np.float32(torch.finfo(dtype).min if low is None else low)
+    fill = fill if w.dtype == "f32" else W.to_bf16_bits(np.array([fill], np.float32))[0]
+    for a in (r.draft_logits, r.tgt_logits):
+        a[:, : w.V // 2] = fill
+        a[1::2, 3 * w.V // 4:] = fill
+        a[2::3, w.V // 2: w.V // 2 + w.V // 8] = fill
+    o = pu.oracle_round(r)
+
+    def compare(g):
+        assert all(torch.isfinite(t.float()).all() for t in (g.q.prob, g.q.mass, g.q.lse, g.ver.p_tok, g.ver.q_tok, g.ver.tgt_max, g.ver.tgt_sum, g.ver.tgt_lse, g.res.resid_mass))
+        pu.compare_round(g, o, r, max_excluded_frac=0.34)
+    for seg in (False, True):
+        compare(pu.gpu_round(r, o.tok, gpu, seg=seg))
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(gpu)                                # noqa: E731
+    for ws in (None, ps.alloc_workspace(dtype, r.N + r.B, w.V, gpu, ps.CALL_ROUND)):
+        q, ver, res = ps.round(pu.to_device(r.draft_logits, gpu), pu.to_device(r.tgt_logits, gpu), w.V, w.T, d(r.seq_off), r.N, d(o.tok), w.k, d(r.uniforms), top_p=w.top_p,
+                               workspace=ws)
+        compare(pu.GpuRound(q, ver, res))
