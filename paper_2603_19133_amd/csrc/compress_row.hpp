@@ -712,9 +712,9 @@ __device__ __forceinline__ RowSelection select_row(
         if (bm > os.mx) {
             os.mx = bm;
             const float rn = ceilf(bm * c);
-            if (rn > os.r) { os.s *= __builtin_amdgcn_exp2f(os.r - rn); os.r = rn; }   // r = -inf: s is 0 and stays 0
+            if (rn > os.r && reference_holds(bm, c, rn)) { os.s *= __builtin_amdgcn_exp2f(os.r - rn); os.r = rn; }   // r = -inf: s is 0 and stays 0
         }
-        const float nr = os.r == kNegInf ? 0.f : -os.r;             // rows of only -inf so far
+        const float nr = os.r == kNegInf ? 0.f : -os.r;             // rows of only masked ids so far: weights of 0
         float acc = 0.f;
         if (edge) {
 #pragma unroll

@@ -123,7 +123,8 @@ __device__ __forceinline__ void split_select(
     const float mx = hi;
     // the share's softmax sum, against an integer reference exponent
     const float ref = hi > kNegInf ? ceilf(hi * c) : 0.f;
-    const float acc = tree_sum<0, E>([&](int e) { return __builtin_amdgcn_exp2f(fmaf(v[e], c, -ref)); });   // (masked: 2^-inf = 0)
+    const float nr = reference_holds(hi, c, ref) ? -ref : 0.f;               // (a share that is masked with a finite value: weights of 0)
+    const float acc = tree_sum<0, E>([&](int e) { return __builtin_amdgcn_exp2f(fmaf(v[e], c, nr)); });   // (masked: 2^-inf = 0)
 
     // ---- threshold: a linear histogram of [lo, hi]; a pivot bin that is crowded is refined over the keys (the order-preserving
     //      integers) of its values.  A linear scale that outliers or masked entries of a finite value stretch (the type's

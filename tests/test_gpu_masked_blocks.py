@@ -55,6 +55,22 @@ def test_row_statistics(gpu, ps, T, dtype, low):
         _close(pu.n(mx) / T + np.log(pu.n(sm).astype(np.float64)), want, pu.RTOL_LSE, "max, sum", atol=1e-6)
 
 
+@pytest.mark.parametrize("low", LOW, ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", TEMPERATURES)
+def test_records(gpu, ps, T, dtype, low):
+    for n, V in SHAPES:
+        z = _rows(n, V, dtype, low, n + V)
+        y = z.double() / float(np.float32(T))
+        want = torch.logsumexp(y, 1)
+        for k in (10, 64, 200):
+            print(f"[case] compress {n} x {V} k={k} {dtype} T={T} {low}", flush=True)
+            c = ps.compress(z, V, T, k)
+            assert torch.equal(c.idx.long(), torch.sort(z.double(), dim=1, descending=True, stable=True).indices[:, :k]) and (c.count == k).all()
+            _close(pu.n(c.lse), want.cpu().numpy(), pu.RTOL_LSE, "lse", atol=1e-6)
+            _close(pu.n(c.prob), torch.exp(y.gather(1, c.idx.long()) - want[:, None]).cpu().numpy(), pu.RTOL, "prob", atol=1e-37)
+
+
 @pytest.mark.parametrize("low,T", [(-1e10, 1.0), (-1e20, 0.7), (None, 2.0)], ids=str)
 @pytest.mark.parametrize("name,scale", [("cfg1", {}), ("cfg2", {"B": 4, "V": 9001}), ("cfg3", {"B": 6, "V": 40003, "k": 200}), ("cfg5", {"B": 60, "V": 20011, "k": 300}),
                                         ("cfg4", {"B": 12, "V": 50021, "k": 500})], ids=str)
