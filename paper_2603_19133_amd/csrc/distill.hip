@@ -135,6 +135,7 @@ __device__ __forceinline__ void store_one(char* grad_row, int x, float g)
 //           memory (two writes a vector instead of one for each of its elements that some lane has marked), and the entries find their logits in them behind the stream.
 //   none    The logits are gathered, and the entries' gradients written over what the streaming left in their places: less to prepare, but every entry touches a line
 //           of the row each way.  For short records, and for vocabularies whose marks do not fit (kDistillLds).
+// Forward kernels but for halves are held to 64 registers, eight waves per SIMD (with the tail the compiler took 66 to 68 of its own accord).
 // SPLIT: a row's workgroups take consecutive trips of it; forward, the last of them to arrive adds their sums up and goes on with the record.
 template <bool BF16, bool FWD, bool GRAD, bool TAIL, int SLOTS, bool SPLIT, int kDT, int HELD>
 __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 8 : kDT / 256) void distill_kernel(const DistillArgs a)
@@ -530,7 +531,7 @@ __global__ __launch_bounds__(kDT, HELD ? 4 : FWD && !GRAD && SLOTS != kHalves ? 
     }
 }
 
-constexpr int kDistillLds = 80 * 1024;            // two workgroups per CU: slots of 4096 entries for vocabularies of up to 262,000, of 512 up to 408,000
+constexpr int kDistillLds = 80 * 1024;            // a bound: slots of 4096 entries for vocabularies of up to 262,000, of 512 up to 408,000 (shorter ones leave room: 2048 entries of 152,064 ids, 45 KB, for three workgroups per CU)
 constexpr size_t kDistillMostLds = 144 * 1024;    // the marks of the longest row alone
 inline size_t mark_words(const DistillArgs& a) { return ((size_t)a.V + 8 + 31) / 32; }
 inline size_t marks_lds(const DistillArgs& a) { return mark_words(a) * 4; }

@@ -10,10 +10,11 @@
 // of 10^-6 of it and less between their steps.  With fp32 weights (bf16 logits take few values, so their errors do not average out) sums are off by 10^-8 and
 // more of the row's mass, and one row in a hundred would end its prefix, or draw, an id off.  At 10^-12, the error of weight(), it is one in a million.
 //
-// What bounds it.  A row is read once (top-p alone: twice, the second time partly from the caches).  Plain draws, and top-p's second pass over fp32, are bound by the vector
-// ALU: a dozen fp64 operations an element (256 rows of 151,936 fp32, 156 MB, 38 us = 4.1 TB/s; a bare read 23).  Lists take a comparison an element and come near the memory
-// (512 rows of 100,000 fp32, top-k 50, 47 us = 4.4 TB/s); top-p alone is bound by the counting in LDS and the ALU (512 rows of 152,064 bf16 86 us; 256 of 128,256 56).  Few rows are
-// bound by latency: one of 32,000 with top-k and top-p 15 us, peek, pass, hand-over, ordering and draw behind each other.
+// What bounds it.  A row is read once (top-p alone: twice, the second time partly from the caches).  Plain draws, and top-p's second pass over fp32, are bound by a workgroup's own arithmetic,
+// a dozen fp64 operations an element, and its waits: 256 rows of 151,936 fp32, 156 MB, one workgroup per CU, 38 to 41 us = 4.0 TB/s (a bare read 23), 129 of them 35, 512, two per CU, 71 = 4.4 TB/s.
+// Lists take a comparison an element and come near the memory (512 rows of 100,000 fp32, top-k 50, 47 us = 4.4 TB/s), short ones are a chain of peek, pass, the list's logits, ordering and draw (min-p
+// on rows of 50,001 bf16: 16 us for 129 to 256 rows, 20 to 21 for 300 to 512); top-p alone is bound by the counting in LDS and the ALU (64 to 256 rows of 152,064 bf16 57 to 59 us, 512, two per CU, 86).
+// Few rows are bound by latency: one of 32,000 with top-k and top-p 15 us, peek, pass, hand-over, ordering and draw behind each other.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -1270,6 +1271,8 @@ __device__ __forceinline__ void draw_short(int kept, float u, const Weights& w, 
 }
 
 // PHASE 0: everything but the second pass of histograms whose rows have several workgroups; 1: those.
+// (128 registers, so that two workgroups share a CU with their LDS.  What they do not hold, 8 to 16 values a thread, is written to scratch between the passes, once a row, and in none of their loops;
+// only sample_careful has a few such accesses in its loops.)
 template <bool BF16, int PHASE>
 __global__ __launch_bounds__(kST, 4) void sample_kernel(const SampleArgs a)
 {
