@@ -1268,7 +1268,13 @@ __device__ __forceinline__ RowSelection select_row(
             for (int w = 0; w < kW; ++w) M = fmaxf(M, (float)sh.red[w]);
             // (optimistic pass: values so far above the sample's that the sums may have overflowed; the same for every thread)
             if (optimistic && !(M * c - os.r < 100.f)) { enough = false; n_held = -1; fill = false; }
-            const double mine = os.r == kNegInf ? 0.0 : (double)os.s * exp2_split((double)os.r - (double)M * (double)c);
+            double mine = os.r == kNegInf ? 0.0 : (double)os.s * exp2_split((double)os.r - (double)M * (double)c);
+            if (optimistic && M * c - os.r < -64.f) {
+                // (a sample that was masked whole, its reference 0, in a row of low values, whose terms are lost: all that it has above -inf is held)
+                float held_s = 0.f;
+                for (int i = tid; i < n_held; i += kT) held_s += exp_stream(__uint_as_float(sh.cand_val[i]), M, c);
+                mine = (double)(held_s + (os.s - os.s));        // (NaN is held by the sums alone)
+            }
             const double ws = wave_sum(mine);
             if (lane == 0) sh.red[kW + wave] = ws;
             __syncthreads();

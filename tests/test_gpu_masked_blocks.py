@@ -98,3 +98,35 @@ def test_rounds(gpu, ps, name, scale, low, T):
         q, ver, res = ps.round(pu.to_device(r.draft_logits, gpu), pu.to_device(r.tgt_logits, gpu), w.V, w.T, d(r.seq_off), r.N, d(o.tok), w.k, d(r.uniforms), top_p=w.top_p,
                                workspace=ws)
         compare(pu.GpuRound(q, ver, res))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("at,T", [(0.0, 1.0), (-60.0, 1.0), (-75.0, 1.0), (-100.0, 1.0), (-1e4, 1.0), (-9.0, 0.05), (100.0, 1.0)], ids=str)
+def test_records_of_few_allowed_ids_of_low_value(gpu, ps, at, T, dtype):
+    """A vocabulary mask (-inf) that leaves a stretch of some ids, none of which a look at the row meets, with logits far below 0."""
+    for n, V, k, allowed in ((3, 12331, 19, 20), (8, 128256, 50, 400), (300, 40003, 64, 20), (300, 40003, 300, 200), (256, 128256, 1024, 700)):
+        print(f"[case] compress {n} x {V} k={k} {allowed} allowed {dtype} at {at} T={T}", flush=True)
+        rng = np.random.default_rng(V + k)
+        z = torch.full((n, V), -np.inf, dtype=dtype, device="cuda")
+        z[:, V // 2: V // 2 + allowed] = torch.from_numpy(rng.normal(size=(n, allowed)) * 3 * T + at).to(dtype).cuda()
+        y = z.double() / float(np.float32(T))
+        want = torch.logsumexp(y, 1)
+        c = ps.compress(z, V, T, k)
+        m = min(k, allowed)
+        assert torch.equal(c.idx[:, :m].long(), torch.sort(z.double(), dim=1, descending=True, stable=True).indices[:, :m])
+        # (what fp32 holds of the exponents of values at -10^4: 2^-24 of 14427 each)
+        far = abs(at) / T * 2.0 ** -24
+        _close(pu.n(c.lse), want.cpu().numpy(), pu.RTOL_LSE, "lse", atol=1e-6 + far)
+        _close(pu.n(c.prob[:, :m]), torch.exp(y.gather(1, c.idx[:, :m].long()) - want[:, None]).cpu().numpy(), pu.RTOL + far, "prob", atol=1e-37)
+
+
+def test_a_row_of_low_values_keeps_its_nan(gpu, ps):
+    z = torch.full((300, 40003), -np.inf, device="cuda")
+    z[:, 20000:20020] = -200.0 + torch.arange(20, device="cuda")
+    want = ps.compress(z, 40003, 1.0, 64)
+    z[7, 30000] = float("nan")
+    got = ps.compress(z, 40003, 1.0, 64)
+    torch.cuda.synchronize()
+    assert torch.isnan(got.lse[7]) and torch.isfinite(want.lse).all()
+    keep = torch.arange(300, device="cuda") != 7
+    assert torch.equal(got.lse[keep], want.lse[keep]) and torch.equal(got.prob[keep], want.prob[keep])
