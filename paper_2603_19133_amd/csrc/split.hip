@@ -565,7 +565,10 @@ __device__ __forceinline__ void split_finish(
             int l, q;
             const int f = u * kT + tid;
             place_of(f, l, q);
-            if (u * kT < n_slots) valid |= f < n_slots && q < __shfl(held, l, kWave) ? 1u << u : 0u;
+            if (u * kT < n_slots) {
+                const int its = __shfl(held, l, kWave);      // (in every lane, behind the last slot too: lane l may be one of those)
+                valid |= f < n_slots && q < its ? 1u << u : 0u;
+            }
         }
         __syncthreads();
         const Few did = finish_few<BF16>(sh, e, valid, n, V, low, high, M, T == kNegInf ? 0u : short_key<BF16>(__float_as_uint(T)), row, k,

@@ -130,3 +130,16 @@ def test_a_row_of_low_values_keeps_its_nan(gpu, ps):
     assert torch.isnan(got.lse[7]) and torch.isfinite(want.lse).all()
     keep = torch.arange(300, device="cuda") != 7
     assert torch.equal(got.lse[keep], want.lse[keep]) and torch.equal(got.prob[keep], want.prob[keep])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,V,k,block", [(30, 199536, 1516, 64), (30, 199536, 1516, 256), (30, 199536, 1400, 256), (60, 151936, 1000, 64), (60, 100003, 700, 256), (90, 128256, 900, 64)])
+def test_full_lists(gpu, ps, n, V, k, block, dtype):
+    """Rows of which every other block of ids is masked: half of a workgroup's lanes hold nothing, the others more than their share, and some of the lists that the
+    workgroups of a row leave are full to the last place."""
+    print(f"[case] full lists {n} x {V} k={k} blocks of {block} {dtype}", flush=True)
+    g = torch.Generator("cuda").manual_seed(24526895)
+    z = torch.randn(n, V, device="cuda", generator=g) * 6.77 + 100
+    z = torch.where(torch.arange(V, device="cuda") // block % 2 == 0, torch.full_like(z, -np.inf), z).to(dtype)
+    want = torch.sort(z.double(), dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(ps.compress(z, V, 1.0, k).idx.long(), want)
