@@ -1171,6 +1171,9 @@ __device__ __forceinline__ RowSelection select_row(
                 }
 #pragma unroll
                 for (int r = 0; r < RING; ++r) ragged(sub + r, rb[(T0 + 1 + r) % RING]);
+                // (the candidates are in LDS before anyone passes the barrier: put_asm's writes are in an asm statement, of which the compiler, that waits for its own
+                // in front of a barrier, knows nothing)
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
             __syncthreads();
             const int words = (int)((unsigned)sh.cnt - val_addr) >> 2;  // (this pass's counter is an LDS byte address)
