@@ -143,3 +143,20 @@ def test_full_lists(gpu, ps, n, V, k, block, dtype):
     z = torch.where(torch.arange(V, device="cuda") // block % 2 == 0, torch.full_like(z, -np.inf), z).to(dtype)
     want = torch.sort(z.double(), dim=1, descending=True, stable=True).indices[:, :k]
     assert torch.equal(ps.compress(z, V, 1.0, k).idx.long(), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,V,k,allowed,values,at", [(56, 142226, 12, 400, "two", 0.0), (56, 142226, 64, 400, "one", 5.0), (64, 131072, 64, 400, "one", 5.0), (8, 51528, 25, 5000, "normal", 1e4),
+                                                     (64, 22807, 112, 7000, "normal", -1e4), (300, 40003, 64, 400, "one", 5.0), (300, 128256, 3000, 7000, "two", 0.0)])
+def test_ties_among_allowed_ids(gpu, ps, n, V, k, allowed, values, at, dtype):
+    """A stretch of allowed ids of few values: more entries of one value than a list holds, of which the lowest ids are kept."""
+    print(f"[case] ties {n} x {V} k={k} {allowed} {values} {dtype}", flush=True)
+    for seed in range(4):
+        g = torch.Generator("cuda").manual_seed(seed)
+        t = torch.randn(n, allowed, device="cuda", generator=g)
+        t = {"two": torch.where(t > 0, 0.22, -0.22), "one": torch.zeros_like(t), "normal": t * 0.3}[values] + at
+        z = torch.full((n, V), -np.inf, dtype=dtype, device="cuda")
+        z[:, V // 2: V // 2 + allowed] = t.to(dtype)
+        want = torch.sort(z.double(), dim=1, descending=True, stable=True).indices[:, :k]
+        for _ in range(2):
+            assert torch.equal(ps.compress(z, V, 1.0, k).idx.long(), want)
