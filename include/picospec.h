@@ -21,6 +21,11 @@
  *   picospec_sample          one token per row of logits with temperature, top-k, top-p and min-p
  *   picospec_distill / picospec_distill_grad
  *                            its divergence from the target's Top-K records and the gradient
+ *   picospec_adjust / picospec_adjust_grad
+ *                            rows of logits with penalties, biases and grammar masks, and the gradient
+ *   picospec_embed / picospec_embed_grad
+ *                            token embeddings and the table's gradient
+ *   picospec_clip_grad       the norm over all gradients, and their clipping
  *
  * Conventions shared by all calls
  *   - Every data pointer is a DEVICE pointer (HBM) unless marked "host".  The caller owns all
@@ -43,7 +48,7 @@
  *     the raw probability P(id), not renormalised), ordered by (logit descending, id ascending);
  *     count used slots, the rest hold idx = -1, prob = 0; mass = sum of the kept prob.
  *     8 bytes per kept component, as in the paper's payload arithmetic.
- *   - Workspace: optional everywhere (NULL: the call works without it).  picospec_verify, picospec_verify_sample and
+ *   - Workspace: optional but for picospec_embed_grad and picospec_clip_grad (NULL: the call works without it).  picospec_verify, picospec_verify_sample and
  *     picospec_round can keep the target rows' SEGMENT TABLE in it: the sum of exp((z - M)/T) over every 2 or 4 KB of
  *     every target row, which the statistics pass has at hand anyway.  With it the correction / bonus draw
  *     (picospec_sample_residual given the SAME workspace that picospec_verify filled for the same rows, or the draw
@@ -97,7 +102,8 @@ enum {
 
 enum { PICOSPEC_CALL_COMPRESS = 0, PICOSPEC_CALL_SAMPLE_DRAFT = 1, PICOSPEC_CALL_VERIFY = 2, PICOSPEC_CALL_SAMPLE_RESIDUAL = 3,
        PICOSPEC_CALL_COMPRESS_REJECTED = 4, PICOSPEC_CALL_RESAMPLE_SPARSE = 5, PICOSPEC_CALL_ROUND = 6,
-       PICOSPEC_CALL_VERIFY_SAMPLE = 7, PICOSPEC_CALL_ROW_STATS = 8, PICOSPEC_CALL_SAMPLE = 9, PICOSPEC_CALL_DISTILL = 10 };
+       PICOSPEC_CALL_VERIFY_SAMPLE = 7, PICOSPEC_CALL_ROW_STATS = 8, PICOSPEC_CALL_SAMPLE = 9, PICOSPEC_CALL_DISTILL = 10,
+       PICOSPEC_CALL_EMBED_GRAD = 11, PICOSPEC_CALL_CLIP_GRAD = 12 };
 enum { PICOSPEC_LIMIT_MAX_K = 0, PICOSPEC_LIMIT_MAX_V = 1 };
 
 /*
@@ -477,6 +483,85 @@ int picospec_distill(const void* logits, int dtype, int64_t ld, int32_t n_rows, 
 int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, float temperature,
                           const int32_t* idx, const float* prob, const int32_t* count, int32_t k, int tail, const float* weight,
                           const double* stats, void* grad, int64_t ld_grad, void* stream);
+
+/*
+ * Rows of logits adjusted for what a request asks, in front of any call that takes logits: penalties for tokens that its text holds already, biases of
+ * single tokens, a grammar's mask.  Rows are those of the other calls:
+ *   seq_off NULL            n_rows = B rows, one a sequence (decoding)
+ *   n_rows = n_draft + B    the target rows of a round: row seq_off[b] + b + t sees the first t drafted tokens of sequence b
+ *   n_rows = n_draft        the draft rows of a round: row seq_off[b] + t, likewise
+ * For a row of sequence b, a token is seen where it is in the sequence's history or among the drafted tokens in front of the row, and c is how often it is
+ * there behind the prompt (drafted tokens are).  In this order:
+ *   z <- z > 0 ? z / repetition : z * repetition   (seen tokens)
+ *   z <- z - frequency c - presence                (tokens with c > 0)
+ *   z <- z + bias                                  (tokens of the sequence's list)
+ *   z <- -inf                                      (tokens that the row's mask does not allow)
+ * formed in 64 bits and rounded to the rows' type; tokens that none of it touches keep their bits, NaN among them.
+ *   logits [n_rows, ld], out [n_rows, ld_out]: out may be the logits themselves (same pointer and stride; what does not change is not written then), else may not overlap them
+ *   draft_tok [n_draft]                                                                                      in
+ *   hist_tok [B, ld_hist], hist_len [B], prompt_len [B]: the first hist_len[b] tokens of row b (clamped to 0..hist_cap <= ld_hist) are the history, the first prompt_len[b] of them
+ *              its prompt (NULL: none).  Tokens outside [0, V) count for nothing.  hist_tok NULL: no history      in
+ *   repetition > 0, presence, frequency finite; *_rows [B], each nullable: a setting per sequence instead.  What the host would refuse counts as none (1, 0, 0)
+ *   bias_off [B + 1], bias_id, bias_value [n_bias], NULL together: the list of sequence b is bias_off[b] .. bias_off[b + 1] - 1; ids outside [0, V) are passed over, of
+ *              entries for the same token the last one counts                                                 in
+ *   mask [n_masks, ld_mask], ld_mask >= ceil(V / 32): bit x % 32 of word x / 32 allows token x.  mask_row [n_rows]: each row's mask, none for a row whose number is outside
+ *              [0, n_masks) (-1).  mask_row NULL: row r has mask r (n_masks >= n_rows).  A mask may leave nothing   in
+ */
+int picospec_adjust(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                    int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                    const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len, const int32_t* prompt_len,
+                    float repetition, float presence, float frequency,
+                    const float* repetition_rows, const float* presence_rows, const float* frequency_rows,
+                    const int32_t* bias_off, const int32_t* bias_id, const float* bias_value, int32_t n_bias,
+                    const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                    void* out, int64_t ld_out, void* stream);
+
+/*
+ * The gradient of picospec_adjust with respect to the logits: grad / repetition where the token is seen and its logit above 0, grad * repetition where it is seen
+ * otherwise, 0 where the mask does not allow it, grad elsewhere (bit for bit).
+ *   grad [n_rows, ld_grad] with respect to the adjusted rows, logits [n_rows, ld] as picospec_adjust took them (not the adjusted ones), in one type      in
+ *   out [n_rows, ld_out]: may be grad itself (same pointer and stride), else may overlap neither input
+ */
+int picospec_adjust_grad(const void* grad, int64_t ld_grad, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                         int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                         const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len,
+                         float repetition, const float* repetition_rows,
+                         const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                         void* out, int64_t ld_out, void* stream);
+
+/*
+ * Token embeddings, what a drafter reads its tokens by: out[i] = scale * table[tok[i]], rounded once (scale 1: the rows' bits); zeros where tok[i] is outside
+ * [0, V), as padding is.
+ *   table [V, ld], tok [n] in; out [n, ld_out] in the table's type, may not overlap the table; ld, ld_out >= d; V up to picospec_limit(MAX_V)
+ */
+int picospec_embed(const void* table, int dtype, int64_t ld, int32_t V, int32_t d, const int32_t* tok, int32_t n, float scale,
+                   void* out, int64_t ld_out, void* stream);
+
+/*
+ * Its gradient: table_grad[v] = scale * sum of grad[i] over tok[i] = v, summed in fp32 in an order that tok decides (a call gives the same bits every
+ * time) and rounded once; positions whose token is outside [0, V) go nowhere.
+ *   grad [n, ld] of dtype, tok [n] in, n up to 2^26
+ *   accumulate 0: every row of table_grad is written, zeros where a token does not occur; 1: the sums are added to what is there (in fp32, then rounded), other rows stay
+ *   table_grad [V, ld_table] of dtype_table, may not overlap grad                                    out
+ *   workspace: picospec_workspace_bytes(PICOSPEC_CALL_EMBED_GRAD, dtype, n, V, d) bytes on a 16-byte boundary, whatever they hold; needed (but for n = 0 with accumulate)
+ */
+int picospec_embed_grad(const void* grad, int dtype, int64_t ld, int32_t n, const int32_t* tok, int32_t V, int32_t d, float scale, int accumulate,
+                        void* table_grad, int dtype_table, int64_t ld_table, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The norm over all gradients of a model, and the gradients scaled to at most max_norm:
+ *   norm = sqrt(sum of g^2 over all tensors),  out = g * min(1, max_norm / (norm + 1e-6))
+ * Squares are summed in 64 bits in an order that the sizes decide; the factor and the products are formed in 64 bits, too, and rounded to the tensor's type.  With a norm of inf the factor is 0, with NaN NaN.
+ *   grads, numel, dtypes [n_tensors]     HOST arrays: device pointers to dense tensors of numel[i] elements, in any order of their elements; empty ones are passed over
+ *   out [n_tensors]                      HOST array of device pointers, or NULL: in place, where nothing is read again or written if the factor is 1.  out[i] may be grads[i];
+ *                                        otherwise no two of the tensors and outputs may share a byte
+ *   max_norm                             >= 0; inf: the norm alone (and a copy, if out is given)
+ *   norm                                 device, fp32 [1]                                                                             out
+ *   workspace: picospec_workspace_bytes(PICOSPEC_CALL_CLIP_GRAD, 0, n_tensors, 1, 0) bytes on a 16-byte boundary; needed
+ * The host arrays are read before the call returns: a captured call replays on the tensors that it was captured with.
+ */
+int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtypes,
+                       float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * host: memory-safety check of the streaming row loads.  For a row of V elements whose first byte lies

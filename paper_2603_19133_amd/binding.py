@@ -28,6 +28,7 @@ OK, EINVAL, EWORKSPACE, EDTYPE, EHIP, EUNSUPPORTED, ESCRATCH = 0, -1, -2, -3, -4
 FLAG_TOKEN_NOT_IN_SUPPORT, FLAG_NONFINITE, FLAG_RESIDUAL_EMPTY, FLAG_BAD_INPUT = 1, 2, 4, 8
 CALL_COMPRESS, CALL_SAMPLE_DRAFT, CALL_VERIFY, CALL_SAMPLE_RESIDUAL = 0, 1, 2, 3
 CALL_COMPRESS_REJECTED, CALL_RESAMPLE_SPARSE, CALL_ROUND, CALL_VERIFY_SAMPLE, CALL_ROW_STATS, CALL_SAMPLE, CALL_DISTILL = 4, 5, 6, 7, 8, 9, 10
+CALL_EMBED_GRAD, CALL_CLIP_GRAD = 11, 12
 LIMIT_MAX_K, LIMIT_MAX_V = 0, 1
 WIRE_FP32, WIRE_FP16, WIRE_BF16 = 0, 1, 2
 WIRE_BAD_HEADER, WIRE_BAD_BATCH, WIRE_CLAMPED, WIRE_TRUNCATED = 1, 2, 4, 8
@@ -36,6 +37,7 @@ EXPORTS = ("picospec_round", "picospec_verify_sample", "picospec_verify_sample_s
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
            "picospec_sample", "picospec_distill", "picospec_distill_grad",
+           "picospec_adjust", "picospec_adjust_grad", "picospec_embed", "picospec_embed_grad", "picospec_clip_grad",
            "picospec_downlink_bytes_max", "picospec_uplink_bytes", "picospec_max_load_byte", "picospec_check_device", "picospec_probe_clock",
            "picospec_workspace_bytes", "picospec_scratch_bytes", "picospec_one_launch_bytes", "picospec_limit", "picospec_strerror", "picospec_version")
 
@@ -83,6 +85,12 @@ lib.picospec_unpack_uplink.argtypes = [_p, _i64, _i32, _i32, _p, _p, _p, _p, _p]
 lib.picospec_sample.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _i32, _f, _f, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p]
 lib.picospec_distill.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _p, _p, _i64, _p, _sz, _p]
 lib.picospec_distill_grad.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p, _p, _i32, C.c_int, _p, _p, _p, _i64, _p]
+lib.picospec_adjust.argtypes = [_p, C.c_int, _i64, _i32, _i32, _i32, _i32, _p, _p, _p, _i64, _i32, _p, _p, _f, _f, _f, _p, _p, _p, _p, _p, _p, _i32,
+                                _p, _i64, _i32, _p, _p, _i64, _p]
+lib.picospec_adjust_grad.argtypes = [_p, _i64, _p, C.c_int, _i64, _i32, _i32, _i32, _i32, _p, _p, _p, _i64, _i32, _p, _f, _p, _p, _i64, _i32, _p, _p, _i64, _p]
+lib.picospec_embed.argtypes = [_p, C.c_int, _i64, _i32, _i32, _p, _i32, _f, _p, _i64, _p]
+lib.picospec_embed_grad.argtypes = [_p, C.c_int, _i64, _i32, _p, _i32, _i32, _f, C.c_int, _p, C.c_int, _i64, _p, _sz, _p]
+lib.picospec_clip_grad.argtypes = [_i32, _p, _p, _p, _p, _f, _p, _p, _sz, _p]
 lib.picospec_downlink_bytes_max.argtypes = [_i32, _i32, C.c_int]
 lib.picospec_downlink_bytes_max.restype = _i64
 lib.picospec_uplink_bytes.argtypes = [_i32, _i32, C.c_int]
@@ -106,7 +114,8 @@ lib.picospec_strerror.restype = C.c_char_p
 for _n in ("picospec_compress", "picospec_sample_draft", "picospec_verify", "picospec_sample_residual", "picospec_sample_residual_ws",
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse", "picospec_version",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
-           "picospec_verify_range", "picospec_round", "picospec_sample", "picospec_distill", "picospec_distill_grad"):
+           "picospec_verify_range", "picospec_round", "picospec_sample", "picospec_distill", "picospec_distill_grad",
+           "picospec_adjust", "picospec_adjust_grad", "picospec_embed", "picospec_embed_grad", "picospec_clip_grad"):
     getattr(lib, _n).restype = C.c_int
 
 
@@ -467,6 +476,66 @@ def distill_grad(logits: torch.Tensor, V: int, temperature: float, rec: Compress
         raise PicoSpecError(EINVAL)
     _check(_nat.distill_grad(logits, dt, ld, rows, V, temperature, rec.idx, rec.prob, rec.count, rec.k, tail, weight, stats, out, ld_g, _stream()))
     return out
+
+
+def _tensor_or_raise(r):
+    if r.__class__ is int:
+        raise PicoSpecError(r)
+    return r
+
+
+@dataclass
+class History:
+    tok: torch.Tensor                    # int32 [B, capacity]: each sequence's tokens from its first column on
+    length: torch.Tensor                 # int32 [B]: how many of them there are
+    prompt: torch.Tensor | None = None   # int32 [B]: how many of these are its prompt (None: none)
+
+
+@dataclass
+class Bias:
+    off: torch.Tensor     # int32 [B + 1]: sequence b's entries are off[b] .. off[b + 1] - 1
+    id: torch.Tensor      # int32 [entries]
+    value: torch.Tensor   # float32 [entries]
+
+
+_NO_HISTORY = (None, None, None)
+
+
+def adjust(logits: torch.Tensor, V: int, hist: History | None = None, repetition=1.0, presence=0.0, frequency=0.0, bias: Bias | None = None,
+           mask: torch.Tensor | None = None, mask_row: torch.Tensor | None = None, seq_off: torch.Tensor | None = None,
+           draft_tok: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """picospec_adjust of [rows, >=V] device logits -> [rows, V], or `out` (the logits themselves: in place).  One row a sequence, or with seq_off [B + 1] and draft_tok
+    [N] the N + B target rows or the N draft rows of a round.  repetition, presence and frequency are numbers or float32 device tensors with one per sequence; mask int32 [masks, >=V / 32]
+    holds 32 ids a word, mask_row int32 [rows] each row's mask (-1: none)."""
+    h = (hist.tok, hist.length, hist.prompt) if hist is not None else _NO_HISTORY
+    b = (bias.off, bias.id, bias.value) if bias is not None else _NO_HISTORY
+    return _tensor_or_raise(_nat.adjust(logits, V, *h, repetition, presence, frequency, *b, mask, mask_row, seq_off, draft_tok, None, out))
+
+
+def adjust_grad(grad: torch.Tensor, logits: torch.Tensor, V: int, hist: History | None = None, repetition=1.0,
+                mask: torch.Tensor | None = None, mask_row: torch.Tensor | None = None, seq_off: torch.Tensor | None = None,
+                draft_tok: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """picospec_adjust_grad: from the gradient with respect to adjust's rows that with respect to its logits, [rows, V] (what else adjust was given has no part in it).
+    training.adjust is the same for torch's autograd."""
+    h = (hist.tok, hist.length, None) if hist is not None else _NO_HISTORY
+    return _tensor_or_raise(_nat.adjust(logits, V, *h, repetition, 0.0, 0.0, None, None, None, mask, mask_row, seq_off, draft_tok, grad, out))
+
+
+def embed(table: torch.Tensor, tok: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None) -> torch.Tensor:
+    """picospec_embed: scale * table[tok] for int32 tokens of any shape -> [*tok.shape, d] (out: [tokens, d]); zeros for ids outside the table.
+    training.embed is the same for torch's autograd."""
+    return _tensor_or_raise(_nat.embed(table, tok, scale, out))
+
+
+def embed_grad(grad: torch.Tensor, tok: torch.Tensor, V: int, scale: float = 1.0, out: torch.Tensor | None = None, accumulate: bool = False) -> torch.Tensor:
+    """picospec_embed_grad: the gradient [V, d] of a table from that of its rows, [*tok.shape, d]; `out` may be of the other type, with `accumulate` the sums are added to it."""
+    return _tensor_or_raise(_nat.embed_grad(grad, tok, V, scale, int(accumulate), out))
+
+
+def clip_grad(grads, max_norm: float, out=None) -> torch.Tensor:
+    """picospec_clip_grad of a list of device tensors (fp32 or bf16, dense) -> their norm, float32 [1]; scaled in place, or into the tensors `out`.
+    training.clip_grad_norm takes a model's parameters."""
+    return _tensor_or_raise(_nat.clip_grad(grads, max_norm, out))
 
 
 def downlink_bytes_max(B: int, k: int, prob_format: int) -> int:

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "kernels.hpp"
 #include "rowspan.hpp"
@@ -582,6 +583,204 @@ int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_r
                                           grad, ld_grad, (hipStream_t)stream));
 }
 
+namespace {
+
+size_t esize(int dtype) { return dtype == PICOSPEC_F32 ? 4 : 2; }
+bool known_dtype(int dtype) { return dtype == PICOSPEC_F32 || dtype == PICOSPEC_BF16; }
+
+// The bytes of rows that lie `ld` elements apart, from the first one's first to the last one's last
+struct Span { uintptr_t begin; __int128 end; };
+Span span(const void* p, int64_t rows, int64_t ld, int64_t cols, size_t esz)
+{
+    return {(uintptr_t)p, rows > 0 && cols > 0 ? (__int128)(uintptr_t)p + ((__int128)(rows - 1) * ld + cols) * (__int128)esz : (__int128)(uintptr_t)p};
+}
+bool overlap(const Span& a, const Span& b) { return (__int128)a.begin < b.end && (__int128)b.begin < a.end; }
+
+// What picospec_adjust and its gradient have in common; src: the rows that are streamed
+int check_adjust(const void* src, int64_t ld_src, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V, int32_t B, int32_t n_draft,
+                 const int32_t* seq_off, const int32_t* draft_tok, const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len,
+                 float repetition, const float* repetition_rows, const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row, const void* out, int64_t ld_out)
+{
+    if (int rc = check_logits(logits, dtype, ld, n_rows, V, 1.f)) return rc;
+    if (B < 0 || n_draft < 0 || ld_src < V || ld_out < V) return PICOSPEC_EINVAL;
+    if (seq_off ? n_rows != n_draft && (int64_t)n_rows != (int64_t)n_draft + B : n_rows != B || n_draft != 0) return PICOSPEC_EINVAL;
+    if (n_rows == 0) return PICOSPEC_OK;
+    if (!src || !out || (uintptr_t)src % esize(dtype) || (uintptr_t)out % esize(dtype)) return PICOSPEC_EINVAL;
+    if (n_draft > 0 && !draft_tok) return PICOSPEC_EINVAL;
+    if (hist_tok && (!hist_len || hist_cap < 0 || ld_hist < hist_cap)) return PICOSPEC_EINVAL;
+    if (!repetition_rows && !finite_pos(repetition)) return PICOSPEC_EINVAL;
+    if (mask && (n_masks < 0 || ld_mask < ((int64_t)V + 31) / 32 || (!mask_row && n_masks < n_rows))) return PICOSPEC_EINVAL;
+    const Span to = span(out, n_rows, ld_out, V, esize(dtype));
+    if (!(out == src && ld_out == ld_src) && overlap(to, span(src, n_rows, ld_src, V, esize(dtype)))) return PICOSPEC_EINVAL;
+    if (logits != src && overlap(to, span(logits, n_rows, ld, V, esize(dtype)))) return PICOSPEC_EINVAL;
+    if ((int64_t)B * ((V + kAdjustChunk / 2 - 1) / (kAdjustChunk / 2)) * kAdjustThreads > UINT32_MAX) return PICOSPEC_EUNSUPPORTED;      // (threads of one launch)
+    return PICOSPEC_OK;
+}
+
+}  // namespace
+
+int picospec_adjust(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                    int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                    const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len, const int32_t* prompt_len,
+                    float repetition, float presence, float frequency,
+                    const float* repetition_rows, const float* presence_rows, const float* frequency_rows,
+                    const int32_t* bias_off, const int32_t* bias_id, const float* bias_value, int32_t n_bias,
+                    const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                    void* out, int64_t ld_out, void* stream)
+{
+    if (int rc = check_adjust(logits, ld, logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len,
+                              repetition, repetition_rows, mask, ld_mask, n_masks, mask_row, out, ld_out)) return rc;
+    if ((!presence_rows && !std::isfinite(presence)) || (!frequency_rows && !std::isfinite(frequency))) return PICOSPEC_EINVAL;
+    if (bias_off && (n_bias < 0 || (n_bias > 0 && (!bias_id || !bias_value)))) return PICOSPEC_EINVAL;
+    AdjustArgs a{};
+    a.src = a.logits = logits; a.ld_src = a.ld = ld; a.out = out; a.ld_out = ld_out; a.V = V;
+    a.seq_off = seq_off; a.draft_tok = draft_tok; a.n_draft = n_draft; a.bonus = n_rows != n_draft;
+    a.hist_tok = hist_tok; a.ld_hist = ld_hist; a.hist_cap = hist_cap; a.hist_len = hist_len; a.prompt_len = prompt_len;
+    a.repetition = repetition; a.presence = presence; a.frequency = frequency;
+    a.repetition_rows = repetition_rows; a.presence_rows = presence_rows; a.frequency_rows = frequency_rows;
+    a.bias_off = n_bias > 0 ? bias_off : nullptr; a.bias_id = bias_id; a.bias_value = bias_value; a.n_bias = n_bias;
+    a.mask = mask; a.ld_mask = ld_mask; a.n_masks = n_masks; a.mask_row = mask_row;
+    a.in_place = out == logits;
+    return hip_status(launch_adjust(a, dtype, B, n_rows, false, (hipStream_t)stream));
+}
+
+int picospec_adjust_grad(const void* grad, int64_t ld_grad, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                         int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                         const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len,
+                         float repetition, const float* repetition_rows,
+                         const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                         void* out, int64_t ld_out, void* stream)
+{
+    if (int rc = check_adjust(grad, ld_grad, logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len,
+                              repetition, repetition_rows, mask, ld_mask, n_masks, mask_row, out, ld_out)) return rc;
+    AdjustArgs a{};
+    a.src = grad; a.ld_src = ld_grad; a.logits = logits; a.ld = ld; a.out = out; a.ld_out = ld_out; a.V = V;
+    a.seq_off = seq_off; a.draft_tok = draft_tok; a.n_draft = n_draft; a.bonus = n_rows != n_draft;
+    a.hist_tok = hist_tok; a.ld_hist = ld_hist; a.hist_cap = hist_cap; a.hist_len = hist_len;
+    a.repetition = repetition; a.repetition_rows = repetition_rows;
+    a.mask = mask; a.ld_mask = ld_mask; a.n_masks = n_masks; a.mask_row = mask_row;
+    a.in_place = out == grad;
+    return hip_status(launch_adjust(a, dtype, B, n_rows, true, (hipStream_t)stream));
+}
+
+int picospec_embed(const void* table, int dtype, int64_t ld, int32_t V, int32_t d, const int32_t* tok, int32_t n, float scale,
+                   void* out, int64_t ld_out, void* stream)
+{
+    if (!known_dtype(dtype)) return PICOSPEC_EDTYPE;
+    if (V < 1 || d < 1 || n < 0 || ld < d || ld_out < d || !std::isfinite(scale)) return PICOSPEC_EINVAL;
+    if (V > kMaxV) return PICOSPEC_EUNSUPPORTED;
+    if (n == 0) return PICOSPEC_OK;
+    if (!table || !tok || !out || (uintptr_t)table % esize(dtype) || (uintptr_t)out % esize(dtype)) return PICOSPEC_EINVAL;
+    if (overlap(span(out, n, ld_out, d, esize(dtype)), span(table, V, ld, d, esize(dtype)))) return PICOSPEC_EINVAL;
+    return hip_status(launch_embed(table, dtype, ld, V, d, tok, n, scale, out, ld_out, (hipStream_t)stream));
+}
+
+int picospec_embed_grad(const void* grad, int dtype, int64_t ld, int32_t n, const int32_t* tok, int32_t V, int32_t d, float scale, int accumulate,
+                        void* table_grad, int dtype_table, int64_t ld_table, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!known_dtype(dtype) || !known_dtype(dtype_table)) return PICOSPEC_EDTYPE;
+    if (V < 1 || d < 1 || n < 0 || ld < d || ld_table < d || !std::isfinite(scale) || (accumulate != 0 && accumulate != 1)) return PICOSPEC_EINVAL;
+    if (V > kMaxV || n > kEmbedMostTokens) return PICOSPEC_EUNSUPPORTED;
+    if (!table_grad || (uintptr_t)table_grad % esize(dtype_table)) return PICOSPEC_EINVAL;
+    if (n > 0 && (!grad || !tok || (uintptr_t)grad % esize(dtype))) return PICOSPEC_EINVAL;
+    if (n > 0 && overlap(span(table_grad, V, ld_table, d, esize(dtype_table)), span(grad, n, ld, d, esize(dtype)))) return PICOSPEC_EINVAL;
+    if (n == 0 && accumulate) return PICOSPEC_OK;
+    if (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < embed_scratch(n, V, d).bytes) return PICOSPEC_EWORKSPACE;
+    EmbedGradArgs a{};
+    a.g = grad; a.ld = ld; a.d = d; a.out = table_grad; a.ld_out = ld_table; a.V = V; a.scale = scale; a.accumulate = accumulate;
+    return hip_status(launch_embed_grad(a, dtype, dtype_table, tok, n, workspace, (hipStream_t)stream));
+}
+
+namespace {
+
+struct Piece { uintptr_t begin, end; };
+
+// Whether two of the pieces share a byte.  Tensors mostly come in the order of their allocation or against it; others are put in order first (about 30 us for 1000).
+bool any_overlap(Piece* p, size_t n)
+{
+    auto by_begin = [](const Piece& a, const Piece& b) { return a.begin < b.begin; };
+    if (!std::is_sorted(p, p + n, by_begin)) std::sort(p, p + n, by_begin);
+    for (size_t i = 1; i < n; ++i)
+        if (p[i].begin < p[i - 1].end) return true;
+    return false;
+}
+
+}  // namespace
+
+int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtypes,
+                       float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (n_tensors < 0 || !(max_norm >= 0.f) || !norm || (uintptr_t)norm % 4) return PICOSPEC_EINVAL;
+    if (n_tensors > 0 && (!grads || !numel || !dtypes)) return PICOSPEC_EINVAL;
+    constexpr size_t kHere = 256;
+    Piece here[kHere], *pieces = here;
+    if ((size_t)n_tensors * 2 > kHere && !(pieces = static_cast<Piece*>(std::malloc((size_t)n_tensors * 2 * sizeof(Piece))))) return PICOSPEC_EINVAL;
+    size_t n_pieces = 0;
+    int rc = PICOSPEC_OK;
+    for (int i = 0; i < n_tensors && rc == PICOSPEC_OK; ++i) {
+        if (!known_dtype(dtypes[i])) { rc = PICOSPEC_EDTYPE; break; }
+        const size_t esz = esize(dtypes[i]);
+        if (numel[i] < 0 || numel[i] > (int64_t)1 << 42) { rc = PICOSPEC_EINVAL; break; }
+        if (numel[i] == 0) continue;
+        const uintptr_t g = (uintptr_t)grads[i], o = out ? (uintptr_t)out[i] : g;
+        if (!g || !o || g % esz || o % esz) { rc = PICOSPEC_EINVAL; break; }
+        pieces[n_pieces++] = {g, g + (size_t)numel[i] * esz};
+        if (o != g) pieces[n_pieces++] = {o, o + (size_t)numel[i] * esz};
+    }
+    if (rc == PICOSPEC_OK && any_overlap(pieces, n_pieces)) rc = PICOSPEC_EINVAL;
+    if (pieces != here) std::free(pieces);
+    if (rc != PICOSPEC_OK) return rc;
+    if (n_tensors > 0 && (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < clip_scratch_bytes(n_tensors))) return PICOSPEC_EWORKSPACE;
+
+    // f(tensors of a launch, its workgroups), for all tensors that hold anything
+    auto each_launch = [&](auto f) -> hipError_t {
+        ClipTensors c;
+        int64_t blocks = 0;
+        c.n = 0;
+        c.first[0] = 0;
+        auto go = [&] {
+            const hipError_t e = f(c, (int)std::min<int64_t>(blocks, kClipGroups));
+            c.n = 0;
+            blocks = 0;
+            return e;
+        };
+        for (int i = 0; i < n_tensors; ++i) {
+            if (numel[i] == 0) continue;
+            const int64_t more = (numel[i] + kClipBlock - 1) / kClipBlock;
+            if (c.n == kClipTensors || blocks + more > INT32_MAX)
+                if (hipError_t e = go()) return e;
+            c.grad[c.n] = grads[i];
+            c.out[c.n] = out ? out[i] : const_cast<void*>(grads[i]);
+            c.numel[c.n] = numel[i];
+            c.bf16[c.n] = dtypes[i] == PICOSPEC_BF16;
+            blocks += more;
+            c.first[++c.n] = (uint32_t)blocks;
+        }
+        return c.n ? go() : hipSuccess;
+    };
+    const hipStream_t s = (hipStream_t)stream;
+    double* const partial = (double*)workspace;
+    int partials = 0;
+    if (hipError_t e = each_launch([&](const ClipTensors& c, int groups) {
+            const hipError_t r = launch_clip_norm(c, partial + partials, groups, s);
+            partials += groups;
+            return r;
+        })) return hip_status(e);
+    bool named = false;                                           // (the first launch writes the norm)
+    if (!std::isinf(max_norm) || out) {
+        if (hipError_t e = each_launch([&](const ClipTensors& c, int groups) {
+                const hipError_t r = launch_clip_scale(c, partial, partials, max_norm, named ? nullptr : norm, groups, s);
+                named = true;
+                return r;
+            })) return hip_status(e);
+    }
+    if (named) return PICOSPEC_OK;
+    ClipTensors none;
+    none.n = 0;
+    none.first[0] = 0;
+    return hip_status(launch_clip_scale(none, partial, partials, max_norm, norm, 1, s));
+}
+
 size_t picospec_workspace_bytes(int which_call, int dtype, int32_t rows, int32_t V, int32_t k)
 {
     if (rows < 0 || V < 1 || V > kMaxV) return 0;
@@ -598,6 +797,9 @@ size_t picospec_workspace_bytes(int which_call, int dtype, int32_t rows, int32_t
         }
         case PICOSPEC_CALL_SAMPLE: return sample_scratch_bytes(dtype, rows, V);
         case PICOSPEC_CALL_DISTILL: return distill_scratch_bytes(dtype, rows, V);
+        // the calls that need theirs
+        case PICOSPEC_CALL_EMBED_GRAD: return k < 1 || rows > kEmbedMostTokens ? 0 : embed_scratch(rows, V, k).bytes;
+        case PICOSPEC_CALL_CLIP_GRAD: return clip_scratch_bytes(rows);
         default:
             return 0;                           // every other kernel keeps its intermediate state in LDS
     }

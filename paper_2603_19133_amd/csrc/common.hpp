@@ -329,6 +329,18 @@ __device__ __forceinline__ void unpack(const uint4& raw, float (&out)[Vec<BF16>:
     }
 }
 
+// Two fp32 values as a word of bf16, each rounded to nearest, ties to even.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    uint32_t r;
+    __builtin_memcpy(&r, &v, 4);
+    return r;
+}
+
+// 16 bytes at an address that is element-aligned only (global loads and stores take any alignment).
+typedef u32x4_t loose_t __attribute__((aligned(2)));
+
 // One logit by vocabulary id (random access).
 template <bool BF16>
 __device__ __forceinline__ float logit_at(const void* logits, int64_t ld, int64_t row, int x) {

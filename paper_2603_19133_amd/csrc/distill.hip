@@ -77,20 +77,8 @@ __device__ __forceinline__ double log2_of(float p)
     return (double)__builtin_amdgcn_frexp_expf(p) + (double)__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(p));
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    // (round to nearest, ties to even)
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 v = {(__bf16)a, (__bf16)b};
-    uint32_t r;
-    __builtin_memcpy(&r, &v, 4);
-    return r;
-}
-
 // 16 bytes to an address that is element-aligned only: the output rows need not lie like the input's (global stores take any alignment).  Non-temporal: the
 // gradient is not read here again, and the rows that are read twice keep their place in the caches (2048 rows of 128,256 fp32: 671 -> 544 us).
-typedef u32x4_t loose_t __attribute__((aligned(2)));
-
 template <bool BF16>
 __device__ __forceinline__ void store_vec(char* grad_row, const RowView& rv, int q, const float (&g)[Vec<BF16>::N])
 {

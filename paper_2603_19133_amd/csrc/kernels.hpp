@@ -471,4 +471,66 @@ hipError_t launch_distill_grad(const void* logits, int dtype, int64_t ld, int n_
                                const int32_t* idx, const float* prob, const int32_t* count, int k, int tail,
                                const double* stats, const float* weight, void* grad, int64_t ld_grad, hipStream_t stream);
 
+// ---- rows of logits with penalties, biases and masks (csrc/adjust.hip), and their gradient (src: the gradient of the adjusted rows)
+struct AdjustArgs {
+    const void* src; int64_t ld_src;
+    const void* logits; int64_t ld;
+    void* out; int64_t ld_out;
+    int V;
+    const int32_t *seq_off, *draft_tok; int n_draft, bonus;      // bonus: rows of a sequence behind its drafted tokens, 0 or 1
+    const int32_t *hist_tok; int64_t ld_hist; int hist_cap; const int32_t *hist_len, *prompt_len;
+    float repetition, presence, frequency;
+    const float *repetition_rows, *presence_rows, *frequency_rows;
+    const int32_t *bias_off, *bias_id; const float* bias_value; int n_bias;
+    const uint32_t* mask; int64_t ld_mask; int n_masks; const int32_t* mask_row;
+    int chunk, chunks, parts, in_place;
+};
+constexpr int kAdjustThreads = 256, kAdjustChunk = 8192;          // ids of the largest chunk
+hipError_t launch_adjust(AdjustArgs a, int dtype, int B, int64_t n_rows, bool gradient, hipStream_t stream);
+
+// ---- token embeddings (csrc/embed.hip)
+hipError_t launch_embed(const void* table, int dtype, int64_t ld, int V, int64_t d, const int32_t* tok, int64_t n, float scale, void* out, int64_t ld_out, hipStream_t stream);
+
+// The gradient's workspace: where each token's positions begin, the positions by token, the tokens of the pieces, the pieces' sums
+constexpr int kSortThreads = 1024, kSortLds = 64 * 1024, kPiece = 64;
+constexpr int64_t kEmbedMostTokens = 1 << 26;
+inline int embed_range(int V) { return std::min(std::max((V + 255) / 256, 1), kSortLds / (kSortThreads / 64 * 4)); }
+// A token's pieces: kPiece positions each, the last one those that are left as well.  Their slots begin at start / kPiece, and a token's last slot lies in front of the next one's first:
+// start / kPiece + len / kPiece <= (start + len) / kPiece.
+struct EmbedPieces { int slot, count; };
+__host__ __device__ inline EmbedPieces embed_pieces(int start, int len) { return {start / kPiece, len < 2 * kPiece ? 0 : len / kPiece}; }
+struct EmbedScratch { size_t order_at, slot_at, partial_at, bytes; int slots; int64_t d_pad; };
+inline EmbedScratch embed_scratch(int64_t n, int64_t V, int64_t d) {
+    EmbedScratch l;
+    l.slots = n < 2 * kPiece ? 0 : (int)(n / kPiece);
+    l.d_pad = (d + 7) / 8 * 8;
+    l.order_at = ((size_t)V + 1 + 63) / 64 * 256;
+    l.slot_at = l.order_at + ((size_t)n + 63) / 64 * 256;
+    l.partial_at = l.slot_at + ((size_t)l.slots + 63) / 64 * 256;
+    l.bytes = l.partial_at + (size_t)l.slots * l.d_pad * 4;
+    return l;
+}
+struct EmbedGradArgs {
+    const void* g; int64_t ld, d;
+    void* out; int64_t ld_out; int V;
+    float scale; int accumulate;
+    const int32_t *first, *order, *slot_tok; float* partial; int64_t d_pad;
+    int slots, slot_groups, share;
+};
+hipError_t launch_embed_grad(EmbedGradArgs a, int dtype, int out_dtype, const int32_t* tok, int n, void* workspace, hipStream_t stream);
+
+// ---- the norm over many tensors and their clipping (csrc/clip.hip): the tensors of one launch, as a kernel argument
+constexpr int kClipTensors = 128, kClipBlock = 16384, kClipGroups = 2048;        // tensors of a launch, elements that a workgroup takes at a time, workgroups of a launch
+struct ClipTensors {
+    const void* grad[kClipTensors];
+    void* out[kClipTensors];
+    int64_t numel[kClipTensors];
+    uint32_t first[kClipTensors + 1];                             // blocks in front of each tensor, and all of them
+    uint8_t bf16[kClipTensors];
+    int n;
+};
+inline size_t clip_scratch_bytes(int64_t n_tensors) { return (size_t)((n_tensors + kClipTensors - 1) / kClipTensors) * kClipGroups * 8; }
+hipError_t launch_clip_norm(const ClipTensors& c, double* partial, int groups, hipStream_t stream);
+hipError_t launch_clip_scale(const ClipTensors& c, const double* partial, int partials, float max_norm, float* norm, int groups, hipStream_t stream);
+
 }  // namespace picospec

@@ -5,12 +5,15 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <algorithm>
+#include <cmath>
 #include <stdexcept>
 
 #include "../../include/picospec.h"
@@ -361,6 +364,352 @@ PyObject* n_distill_loss(PyObject*, PyObject* const* v, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- adjusted logits, embeddings and clipped gradients.  These calls run on the current stream of their tensors' device, whichever device is current.
+
+using c10::hip::getCurrentHIPStream;
+
+at::Tensor optional_tensor(Args& a) {
+    PyObject* o = a.next();
+    if (o == Py_None) return at::Tensor();
+    if (!THPVariable_Check(o)) throw BadArgument("a tensor or None is expected");
+    return THPVariable_Unpack(o);
+}
+
+void refuse_unless(bool ok) { if (!ok) throw Refused{PICOSPEC_EINVAL}; }
+
+// rows of V columns and more in the type of `z` and on its device; returns the stride of a row
+int64_t rows_like(const at::Tensor& t, const at::Tensor& z, int64_t rows, int64_t V) {
+    refuse_unless(t.dim() == 2 && t.size(0) == rows && t.size(1) >= V && t.device() == z.device());
+    if (t.scalar_type() != z.scalar_type()) throw Refused{PICOSPEC_EDTYPE};
+    int64_t ld;
+    logits_code(t, ld);
+    return rows <= 1 ? std::max(ld, V) : ld;
+}
+
+template <class T> const T* data(const at::Tensor& t) { return t.defined() ? static_cast<const T*>(t.data_ptr()) : nullptr; }
+
+// a setting: a number for all sequences or a tensor with one for each
+struct Setting { float all; at::Tensor each; };
+Setting one_setting(Args& a) {
+    PyObject* o = a.next();
+    if (THPVariable_Check(o)) return {0.f, THPVariable_Unpack(o)};
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw BadArgument("");
+    return {(float)v, at::Tensor()};
+}
+
+// What a call adjusts its rows by, checked against them
+struct Adjustment {
+    at::Tensor hist_tok, length, prompt, bias_off, bias_id, bias_value, mask, mask_row, seq_off, draft_tok;
+    Setting repetition, presence, frequency;
+    int64_t B = 0, ld_hist = 0, hist_cap = 0, n_draft = 0, n_bias = 0, n_masks = 0, ld_mask = 0;
+
+    explicit Adjustment() = default;
+    explicit Adjustment(Args& a) {
+        hist_tok = optional_tensor(a); length = optional_tensor(a); prompt = optional_tensor(a);
+        repetition = one_setting(a); presence = one_setting(a); frequency = one_setting(a);
+        bias_off = optional_tensor(a); bias_id = optional_tensor(a); bias_value = optional_tensor(a);
+        mask = optional_tensor(a); mask_row = optional_tensor(a); seq_off = optional_tensor(a); draft_tok = optional_tensor(a);
+    }
+    void check(const at::Tensor& z, int64_t V) {
+        const int64_t rows = z.size(0);
+        auto list = [&](const at::Tensor& t, at::ScalarType type, int64_t n) { refuse_unless(t.defined() && t.dim() == 1 && (n < 0 || t.numel() == n) && dense(t, type, z)); };
+        refuse_unless(V >= 1 && V <= z.size(1) && rows <= INT32_MAX);
+        B = rows;
+        if (seq_off.defined()) {
+            list(seq_off, at::kInt, -1);
+            list(draft_tok, at::kInt, -1);
+            refuse_unless(seq_off.numel() >= 1 && draft_tok.numel() <= INT32_MAX);
+            B = seq_off.numel() - 1;
+            n_draft = draft_tok.numel();
+        } else {
+            refuse_unless(!draft_tok.defined());
+        }
+        if (hist_tok.defined()) {
+            refuse_unless(hist_tok.dim() == 2 && hist_tok.size(0) == B && hist_tok.scalar_type() == at::kInt && hist_tok.device() == z.device());
+            hist_cap = hist_tok.size(1);
+            ld_hist = B > 1 ? hist_tok.stride(0) : hist_cap;
+            refuse_unless(hist_cap <= INT32_MAX && (hist_cap <= 1 || hist_tok.stride(1) == 1));
+            list(length, at::kInt, B);
+            if (prompt.defined()) list(prompt, at::kInt, B);
+        }
+        for (const Setting* s : {&repetition, &presence, &frequency}) if (s->each.defined()) list(s->each, at::kFloat, B);
+        if (bias_off.defined()) {
+            list(bias_off, at::kInt, B + 1);
+            list(bias_id, at::kInt, -1);
+            list(bias_value, at::kFloat, bias_id.numel());
+            refuse_unless(bias_id.numel() <= INT32_MAX);
+            n_bias = bias_id.numel();
+        }
+        if (mask.defined()) {
+            refuse_unless(mask.dim() == 2 && mask.scalar_type() == at::kInt && mask.device() == z.device() && mask.size(0) <= INT32_MAX && mask.size(1) >= (V + 31) / 32 && (mask.size(1) == 1 || mask.stride(1) == 1));
+            n_masks = mask.size(0);
+            ld_mask = n_masks > 1 ? mask.stride(0) : mask.size(1);
+            if (mask_row.defined()) list(mask_row, at::kInt, rows);
+        } else {
+            refuse_unless(!mask_row.defined());
+        }
+    }
+    int forward(const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out) const {
+        return picospec_adjust(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
+                               data<int32_t>(hist_tok), ld_hist, (int32_t)hist_cap, data<int32_t>(length), data<int32_t>(prompt), repetition.all, presence.all, frequency.all,
+                               data<float>(repetition.each), data<float>(presence.each), data<float>(frequency.each), data<int32_t>(bias_off), data<int32_t>(bias_id), data<float>(bias_value), (int32_t)n_bias,
+                               data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, getCurrentHIPStream().stream());
+    }
+    int backward(const at::Tensor& g, int64_t ld_g, const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out) const {
+        return picospec_adjust_grad(g.data_ptr(), ld_g, z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
+                                    data<int32_t>(hist_tok), ld_hist, (int32_t)hist_cap, data<int32_t>(length), repetition.all, data<float>(repetition.each),
+                                    data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, getCurrentHIPStream().stream());
+    }
+};
+
+// A tensor that a call has written in place: what the tape has saved of it is not what it was
+void written(const at::Tensor& t) { if (!t.is_inference()) torch::autograd::impl::bump_version(t); }
+
+// Runs `call(args)`, which returns a new reference; a refusal is returned as the library's error code
+template <class F>
+PyObject* answer(PyObject* const* v, Py_ssize_t n, F call) {
+    HANDLE_TH_ERRORS
+    try {
+        Args a{v, n};
+        return call(a);
+    } catch (const Refused& r) {
+        return PyLong_FromLong(r.code);
+    } catch (const BadArgument& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, e.what());
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+void check_code(int rc) { if (rc != PICOSPEC_OK) throw Refused{rc}; }
+
+// adjust(logits, V, hist_tok, length, prompt, repetition, presence, frequency, bias_off, bias_id, bias_value, mask, mask_row, seq_off, draft_tok, grad, out) -> tensor or an error code; with a
+// gradient its own
+PyObject* n_adjust(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return answer(v, n, [](Args& a) {
+        const at::Tensor z = a.tensor();
+        const int64_t V = a.i64();
+        Adjustment by(a);
+        const at::Tensor grad = optional_tensor(a);
+        at::Tensor out = optional_tensor(a);
+        a.done();
+        const bool given = out.defined();
+        int64_t ld, ld_g = 0;
+        const int dt = logits_code(z, ld);
+        by.check(z, V);
+        const int64_t rows = z.size(0);
+        if (rows <= 1) ld = std::max(ld, V);
+        if (grad.defined()) ld_g = rows_like(grad, z, rows, V);
+        const c10::DeviceGuard guard(z.device());
+        if (!given) out = at::empty({rows, V}, z.options());
+        const int64_t ld_out = rows_like(out, z, rows, V);
+        check_code(grad.defined() ? by.backward(grad, ld_g, z, dt, ld, V, out, ld_out) : by.forward(z, dt, ld, V, out, ld_out));
+        if (given) written(out);
+        return THPVariable_Wrap(out);
+    });
+}
+
+struct AdjustFunction : torch::autograd::Function<AdjustFunction> {
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& z, Adjustment* by, int64_t V) {
+        int64_t ld;
+        const int dt = logits_code(z, ld);
+        by->check(z, V);
+        if (z.size(0) <= 1) ld = std::max(ld, V);
+        const c10::DeviceGuard guard(z.device());
+        at::Tensor out = at::empty({z.size(0), V}, z.options());
+        check_code(by->forward(z, dt, ld, V, out, V));
+        ctx->save_for_backward({z, by->hist_tok, by->length, by->repetition.each, by->mask, by->mask_row, by->seq_off, by->draft_tok});
+        ctx->saved_data["V"] = V;
+        ctx->saved_data["repetition"] = (double)by->repetition.all;
+        return out;
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        TORCH_CHECK(!at::GradMode::is_enabled(), "adjust is differentiable once");                 // (create_graph: the kernel is not on the tape)
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor& z = saved[0];
+        const int64_t V = ctx->saved_data["V"].toInt();
+        Adjustment by;
+        by.hist_tok = saved[1]; by.length = saved[2]; by.repetition = {(float)ctx->saved_data["repetition"].toDouble(), saved[3]};
+        by.mask = saved[4]; by.mask_row = saved[5]; by.seq_off = saved[6]; by.draft_tok = saved[7];
+        by.check(z, V);
+        int64_t ld;
+        const int dt = logits_code(z, ld);
+        if (z.size(0) <= 1) ld = std::max(ld, V);
+        const c10::DeviceGuard guard(z.device());
+        at::Tensor out = at::empty(z.sizes(), z.options());
+        if (z.size(1) > V) out.slice(1, V).zero_();                                                 // (columns behind the vocabulary are not read)
+        const at::Tensor g = grads[0].contiguous();                                                 // (of a sum: one value seen from every place)
+        const int rc = by.backward(g, V, z, dt, ld, V, out, z.size(1));
+        TORCH_CHECK(rc == PICOSPEC_OK, "picospec error ", rc, ": ", picospec_strerror(rc));
+        return {out, at::Tensor(), at::Tensor()};
+    }
+};
+
+// adjust_on_tape(logits, V, ... as adjust, draft_tok) -> tensor or an error code
+PyObject* n_adjust_on_tape(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return answer(v, n, [](Args& a) {
+        const at::Tensor z = a.tensor();
+        const int64_t V = a.i64();
+        Adjustment by(a);
+        a.done();
+        return THPVariable_Wrap(AdjustFunction::apply(z, &by, V));
+    });
+}
+
+struct Table { int dt; int64_t ld, V, d; };
+Table check_table(const at::Tensor& t) {
+    int64_t ld;
+    const int dt = logits_code(t, ld);
+    refuse_unless(t.size(0) >= 1 && t.size(0) <= INT32_MAX && t.size(1) >= 1 && t.size(1) <= INT32_MAX);
+    return {dt, t.size(0) == 1 ? std::max(ld, t.size(1)) : ld, t.size(0), t.size(1)};
+}
+
+at::Tensor embed(const at::Tensor& table, const at::Tensor& tok, float scale, at::Tensor out) {
+    const Table t = check_table(table);
+    refuse_unless(dense(tok, at::kInt, table) && tok.numel() <= INT32_MAX);
+    const int64_t n = tok.numel();
+    const c10::DeviceGuard guard(table.device());
+    int64_t ld_out = t.d;
+    if (out.defined()) {
+        refuse_unless(out.dim() == 2 && out.size(1) == t.d);
+        ld_out = rows_like(out, table, n, t.d);
+    } else {
+        auto sizes = tok.sizes().vec();
+        sizes.push_back(t.d);
+        out = at::empty(sizes, table.options());
+    }
+    check_code(picospec_embed(table.data_ptr(), t.dt, t.ld, (int32_t)t.V, (int32_t)t.d, data<int32_t>(tok), (int32_t)n, scale, out.data_ptr(), ld_out, getCurrentHIPStream().stream()));
+    return out;
+}
+
+at::Tensor embed_grad(at::Tensor g, const at::Tensor& tok, int64_t V, float scale, int accumulate, at::Tensor out) {
+    refuse_unless(g.is_cuda() && g.dim() == tok.dim() + 1 && g.sizes().slice(0, tok.dim()) == tok.sizes() && V >= 1 && V <= INT32_MAX);
+    const int64_t n = tok.numel(), d = g.size(-1);
+    refuse_unless(n <= INT32_MAX && d >= 1 && d <= INT32_MAX);
+    const c10::DeviceGuard guard(g.device());
+    if (g.dim() != 2) g = g.reshape({n, d});
+    refuse_unless(dense(tok, at::kInt, g));
+    int64_t ld;
+    const int dt = logits_code(g, ld);
+    if (n <= 1) ld = std::max(ld, d);
+    refuse_unless(out.defined() || !accumulate);
+    if (!out.defined()) out = at::empty({V, d}, g.options());
+    refuse_unless(out.dim() == 2 && out.size(0) == V && out.size(1) == d && out.device() == g.device());
+    const Table t = check_table(out);
+    const size_t bytes = picospec_workspace_bytes(PICOSPEC_CALL_EMBED_GRAD, dt, (int32_t)n, (int32_t)V, (int32_t)d);
+    const at::Tensor scratch = at::empty({(int64_t)std::max<size_t>(bytes, 16)}, g.options().dtype(at::kByte));
+    check_code(picospec_embed_grad(g.data_ptr(), dt, ld, (int32_t)n, data<int32_t>(tok), (int32_t)V, (int32_t)d, scale, accumulate, out.data_ptr(), t.dt, t.ld,
+                                   scratch.data_ptr(), (size_t)scratch.nbytes(), getCurrentHIPStream().stream()));
+    return out;
+}
+
+// embed(table, tok, scale, out) -> rows or an error code
+PyObject* n_embed(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return answer(v, n, [](Args& a) {
+        const at::Tensor table = a.tensor(), tok = a.tensor();
+        const float scale = a.f32();
+        const at::Tensor out = optional_tensor(a);
+        a.done();
+        const at::Tensor rows = embed(table, tok, scale, out);
+        if (out.defined()) written(out);
+        return THPVariable_Wrap(rows);
+    });
+}
+
+// embed_grad(grad, tok, V, scale, accumulate, out) -> the table's gradient or an error code
+PyObject* n_embed_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return answer(v, n, [](Args& a) {
+        const at::Tensor g = a.tensor(), tok = a.tensor();
+        const int64_t V = a.i64();
+        const float scale = a.f32();
+        const int accumulate = a.i32();
+        const at::Tensor out = optional_tensor(a);
+        a.done();
+        const at::Tensor sums = embed_grad(g, tok, V, scale, accumulate, out);
+        if (out.defined()) written(out);
+        return THPVariable_Wrap(sums);
+    });
+}
+
+struct EmbedFunction : torch::autograd::Function<EmbedFunction> {
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& table, const at::Tensor& tok, double scale) {
+        ctx->save_for_backward({tok});
+        ctx->saved_data["V"] = table.size(0);
+        ctx->saved_data["scale"] = scale;
+        return embed(table, tok, (float)scale, at::Tensor());
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        TORCH_CHECK(!at::GradMode::is_enabled(), "embed is differentiable once");                   // (create_graph: the kernel is not on the tape)
+        const auto saved = ctx->get_saved_variables();
+        try {
+            return {embed_grad(grads[0].contiguous(), saved[0], ctx->saved_data["V"].toInt(), (float)ctx->saved_data["scale"].toDouble(), 0, at::Tensor()), at::Tensor(), at::Tensor()};
+        } catch (const Refused& r) {
+            TORCH_CHECK(false, "picospec error ", r.code, ": ", picospec_strerror(r.code));
+        }
+    }
+};
+
+// embed_on_tape(table, tok, scale) -> rows or an error code
+PyObject* n_embed_on_tape(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return answer(v, n, [](Args& a) {
+        const at::Tensor table = a.tensor(), tok = a.tensor();
+        const double scale = a.f32();
+        a.done();
+        if (table.dim() != 2) throw Refused{PICOSPEC_EINVAL};
+        return THPVariable_Wrap(EmbedFunction::apply(table, tok, scale));
+    });
+}
+
+// clip_grad(grads, max_norm, out) -> norm [1] or an error code; lists or tuples of tensors, out None: in place
+PyObject* n_clip_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return answer(v, n, [](Args& a) {
+        PyObject* const grads = a.next();
+        const float max_norm = a.f32();
+        PyObject* const outs = a.next();
+        a.done();
+        auto sequence = [](PyObject* o) { if (!PyList_Check(o) && !PyTuple_Check(o)) throw BadArgument("a list or tuple of tensors is expected"); return PySequence_Fast_GET_SIZE(o); };
+        const Py_ssize_t count = sequence(grads);
+        refuse_unless(count <= INT32_MAX && (outs == Py_None || sequence(outs) == count));
+        auto at_place = [](PyObject* o, Py_ssize_t i) -> const at::Tensor& {
+            PyObject* t = PySequence_Fast_GET_ITEM(o, i);
+            if (!THPVariable_Check(t)) throw BadArgument("a list or tuple of tensors is expected");
+            return THPVariable_Unpack(t);
+        };
+        c10::SmallVector<const void*, 128> g;
+        c10::SmallVector<void*, 128> o;
+        c10::SmallVector<int64_t, 128> numel;
+        c10::SmallVector<int32_t, 128> dtypes;
+        at::Tensor like;
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            const at::Tensor& t = at_place(grads, i);
+            refuse_unless(t.layout() == at::kStrided && t.is_cuda() && (!like.defined() || t.device() == like.device()));
+            if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) throw Refused{PICOSPEC_EDTYPE};
+            refuse_unless(t.is_non_overlapping_and_dense());
+            if (!like.defined()) like = t;
+            g.push_back(t.data_ptr());
+            numel.push_back(t.numel());
+            dtypes.push_back(t.scalar_type() == at::kFloat ? PICOSPEC_F32 : PICOSPEC_BF16);
+            if (outs == Py_None) continue;
+            const at::Tensor& to = at_place(outs, i);
+            refuse_unless(to.layout() == at::kStrided && to.device() == t.device() && to.sizes() == t.sizes() && to.strides() == t.strides());
+            if (to.scalar_type() != t.scalar_type()) throw Refused{PICOSPEC_EDTYPE};
+            o.push_back(to.data_ptr());
+        }
+        const c10::OptionalDeviceGuard guard(like.defined() ? c10::optional<at::Device>(like.device()) : c10::nullopt);
+        const auto f32 = at::TensorOptions().dtype(at::kFloat).device(like.defined() ? like.device() : at::Device(at::kCUDA));
+        at::Tensor norm = at::empty({1}, f32);
+        const size_t bytes = picospec_workspace_bytes(PICOSPEC_CALL_CLIP_GRAD, 0, (int32_t)count, 1, 0);
+        const at::Tensor scratch = at::empty({(int64_t)std::max<size_t>(bytes, 16)}, f32.dtype(at::kByte));
+        check_code(picospec_clip_grad((int32_t)count, g.data(), outs == Py_None ? nullptr : o.data(), numel.data(), dtypes.data(), max_norm, norm.data_ptr<float>(),
+                                      scratch.data_ptr(), (size_t)scratch.nbytes(), getCurrentHIPStream().stream()));
+        for (Py_ssize_t i = 0; i < count && (outs != Py_None || !std::isinf(max_norm)); ++i) written(at_place(outs == Py_None ? grads : outs, i));
+        return THPVariable_Wrap(norm);
+    });
+}
+
 // rows2d(tensor) -> (dtype code, stride of a row, rows), or an error code of the library: a 2-d device tensor whose rows are
 // contiguous (the strides of a tensor without rows mean nothing)
 PyObject* n_rows2d(PyObject*, PyObject* o) {
@@ -498,7 +847,8 @@ PyMethodDef methods[] = {
     FAST("round", n_round), FAST("verify_sample", n_verify_sample), FAST("verify_sample_static", n_verify_sample_static),
     FAST("sample_residual", n_sample_residual<picospec_sample_residual>), FAST("sample_residual_ws", n_sample_residual<picospec_sample_residual_ws>), FAST("row_stats", n_row_stats), FAST("compress_rejected", n_compress_rejected),
     FAST("resample_sparse", n_resample_sparse), FAST("pack_downlink", n_pack_downlink), FAST("unpack_downlink", n_unpack_downlink),
-    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("sample", n_sample), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("distill_loss", n_distill_loss), FAST("distill_inputs", n_distill_inputs), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
+    FAST("pack_uplink", n_pack_uplink), FAST("unpack_uplink", n_unpack_uplink), FAST("sample", n_sample), FAST("distill", n_distill), FAST("distill_grad", n_distill_grad), FAST("distill_loss", n_distill_loss), FAST("distill_inputs", n_distill_inputs), FAST("adjust", n_adjust), FAST("adjust_on_tape", n_adjust_on_tape), FAST("embed", n_embed), FAST("embed_grad", n_embed_grad),
+    FAST("embed_on_tape", n_embed_on_tape), FAST("clip_grad", n_clip_grad), FAST("scratch_bytes", n_scratch_bytes), FAST("scratch", n_scratch), FAST("empty", n_empty),
     {"rows2d", (PyCFunction)n_rows2d, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,349 @@
+"""picospec_adjust and picospec_adjust_grad against the formulas in 64 bits, token by token.
+
+What the kernel does to a touched token is formed in 64 bits (a product with 1 / repetition, itself rounded, for the quotient) and rounded to fp32, bf16 rows from there once more: half a
+step of the rows' type (2^-24; 2^-8, and 2^-24 from the step between), and what 64 bits lose of the operands, a few 2^-53 of the largest.  Every other token keeps its bits."""
+import math
+import random
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8 * (1 + 2.0 ** -14)}
+BEYOND = {torch.float32: (2 - 2.0 ** -24) * 2.0 ** 127, torch.bfloat16: (2 - 2.0 ** -8) * 2.0 ** 127}       # (what rounds to infinity)
+
+
+@pytest.fixture(scope="module")
+def ps():
+    from paper_2603_19133_amd import binding
+    return binding
+
+
+def _pack(bits):
+    """int32 words of a bool matrix [masks, V]."""
+    m, V = bits.shape
+    words = (V + 31) // 32
+    full = torch.zeros((m, words * 32), dtype=torch.int64)
+    full[:, :V] = bits
+    w = (full.view(m, words, 32) << torch.arange(32)).sum(2)
+    return torch.where(w >= 2 ** 31, w - 2 ** 32, w).to(torch.int32)
+
+
+class Case:
+    """Inputs on the host and their results in 64 bits."""
+
+    def __init__(self, seed, V, dtype, gammas, target=True, cap=50, masks=0, mixed=True, bias=0, pad=0, values=None, lengths=None, token_range=None):
+        self.V, self.dtype, self.gammas, self.target = V, dtype, gammas, target
+        g = torch.Generator().manual_seed(seed)
+        r = random.Random(seed)
+        self.B = B = len(gammas)
+        self.decoding = all(x == 0 for x in gammas) and target
+        rows = sum(gammas) + (B if target else 0)
+        self.rows = rows
+        z = torch.randn((rows, V + pad), generator=g) * 4
+        if values is not None:
+            z.view(-1)[torch.randint(0, max(1, z.numel()), (z.numel() // 5 + 1,), generator=g)] = torch.tensor([r.choice(values) for _ in range(z.numel() // 5 + 1)])
+        self.z = z.to(dtype)[:, :V]
+        self.grad = (torch.randn((rows, V), generator=g) * 1e-3).to(dtype)
+        hi = token_range or V
+        self.hist = torch.randint(-2, hi + 1, (B, cap), generator=g, dtype=torch.int32)       # (some of them are no tokens)
+        self.length = torch.tensor(lengths or [r.randint(0, cap) for _ in range(B)], dtype=torch.int32)
+        self.prompt = torch.tensor([r.randint(0, max(0, int(n))) for n in self.length], dtype=torch.int32)
+        self.draft = torch.randint(0, hi, (sum(gammas),), generator=g, dtype=torch.int32)
+        f = lambda of: torch.tensor([of() for _ in range(B)], dtype=torch.float32)                                     # noqa: E731
+        if mixed:
+            self.rep, self.pres, self.freq = f(lambda: r.choice([1.0, r.uniform(0.5, 2.0)])), f(lambda: r.choice([0.0, r.uniform(-1, 2)])), f(lambda: r.choice([0.0, r.uniform(-1, 1)]))
+        else:
+            self.rep, self.pres, self.freq = 1.3, 0.7, 0.1
+        self.bias = None
+        if bias:
+            n = [r.randint(0, bias) for _ in range(B)]
+            ids = [r.randrange(-1, V + 1) for _ in range(sum(n))]
+            if sum(n) > 3:
+                ids[1] = ids[0]                                                      # (a token twice, in one list if the first has two)
+            self.bias = (torch.tensor([0] + [sum(n[:i + 1]) for i in range(B)], dtype=torch.int32), torch.tensor(ids, dtype=torch.int32), torch.randn(sum(n), generator=g) * 3)
+        self.bits = self.mask = self.mask_row = None
+        if masks:
+            self.bits = torch.rand((masks, V), generator=g) < torch.rand((masks, 1), generator=g)
+            self.bits[0] = False
+            self.mask = _pack(self.bits)
+            self.mask_row = torch.tensor([r.randint(-1, masks - 1) for _ in range(rows)], dtype=torch.int32)
+
+    def seen(self):
+        """(row, tokens seen, how often each was generated) of every row."""
+        at = row = 0
+        for b, gamma in enumerate(self.gammas):
+            n, p = min(max(int(self.length[b]), 0), self.hist.shape[1]), int(self.prompt[b])
+            for t in range(gamma + self.target):
+                made = torch.cat([self.hist[b, max(p, 0):n], self.draft[at:at + t]])
+                all_ = torch.cat([self.hist[b, :n], self.draft[at:at + t]])
+                ok = lambda x: x[(x >= 0) & (x < self.V)].long()                                                      # noqa: E731
+                yield b, row, torch.zeros(self.V, dtype=torch.bool).index_fill_(0, ok(all_), True), torch.bincount(ok(made), minlength=self.V).double()
+                row += 1
+            at += gamma
+
+    def of(self, v, b):
+        return float(v[b]) if isinstance(v, torch.Tensor) else float(torch.tensor(v, dtype=torch.float32))
+
+    def expect(self):
+        """(adjusted, its bound, what is not touched), [rows, V]."""
+        out, tol, same = self.z.double().clone(), torch.zeros((self.rows, self.V), dtype=torch.float64), torch.ones((self.rows, self.V), dtype=torch.bool)
+        for b, row, met, n in self.seen():
+            z, rep, pres, freq = self.z[row].double(), self.of(self.rep, b), self.of(self.pres, b), self.of(self.freq, b)
+            y = torch.where(met, torch.where(z > 0, z / rep, z * rep), z) - freq * n - pres * (n > 0)
+            bias = torch.zeros(self.V, dtype=torch.float64)
+            if self.bias is not None:
+                for i in range(int(self.bias[0][b]), int(self.bias[0][b + 1])):
+                    if 0 <= int(self.bias[1][i]) < self.V:
+                        bias[int(self.bias[1][i])] = float(self.bias[2][i])
+            active = rep != 1 or pres != 0 or freq != 0
+            same[row] = ~((met & active) | (bias != 0))
+            y = y + bias
+            y = torch.where(y.abs() >= BEYOND[self.dtype], torch.copysign(torch.tensor(math.inf, dtype=torch.float64), y), y)
+            out[row] = torch.where(same[row], z, y)
+            most = torch.nan_to_num(z, posinf=0.0, neginf=0.0, nan=0.0).abs() * max(rep, 1 / rep) + abs(freq) * n + abs(pres) + bias.abs()
+            tol[row] = HALF[self.dtype] * out[row].abs() * (1 + 2.0 ** -20) + 2.0 ** -50 * most
+            if self.bits is not None and int(self.mask_row[row]) >= 0:
+                away = ~self.bits[int(self.mask_row[row])]
+                out[row][away] = -math.inf
+                same[row] &= ~away
+        return out, tol, same
+
+    def expect_grad(self):
+        out, same = self.grad.double().clone(), torch.ones((self.rows, self.V), dtype=torch.bool)
+        for b, row, met, n in self.seen():
+            z, rep = self.z[row].double(), self.of(self.rep, b)
+            if rep != 1:
+                out[row] = torch.where(met, torch.where(z > 0, out[row] / rep, out[row] * rep), out[row])
+                same[row] = ~met
+            if self.bits is not None and int(self.mask_row[row]) >= 0:
+                away = ~self.bits[int(self.mask_row[row])]
+                out[row][away] = 0.0
+                same[row] &= ~away
+        return out, HALF[self.dtype] * out.abs() * (1 + 2.0 ** -20), same
+
+    def arguments(self, ps, dev, grad=False):
+        d = lambda t: t.to(dev) if isinstance(t, torch.Tensor) else t                                                   # noqa: E731
+        hist = ps.History(d(self.hist), d(self.length), d(self.prompt))
+        kw = dict(repetition=d(self.rep), mask=d(self.mask), mask_row=d(self.mask_row))
+        if not grad:
+            kw.update(presence=d(self.pres), frequency=d(self.freq), bias=ps.Bias(*map(d, self.bias)) if self.bias else None)
+        if not self.decoding:
+            off = torch.tensor([0] + [sum(self.gammas[:i + 1]) for i in range(self.B)], dtype=torch.int32)
+            kw.update(seq_off=d(off), draft_tok=d(self.draft))
+        return hist, kw
+
+    def device_rows(self, dev, rows, pad, fill=7.0):
+        """`rows` on the device, `pad` columns apart, the columns between filled."""
+        whole = torch.full((self.rows, self.V + pad), fill, dtype=self.dtype, device=dev)
+        whole[:, :self.V] = rows.to(dev)
+        return whole, whole[:, :self.V]
+
+
+def bits(t):
+    return t.contiguous().view(torch.int32 if t.dtype == torch.float32 else torch.int16)
+
+
+def same_bits(a, b):
+    return torch.equal(bits(a), bits(b))
+
+
+def hold(got, want, tol, same, before):
+    got, finite = got.cpu(), torch.isfinite(want)
+    assert torch.equal(bits(got)[same], bits(before)[same])
+    touched = ~same
+    assert torch.equal(torch.isnan(got)[touched], torch.isnan(want)[touched])
+    inf = touched & torch.isinf(want)
+    assert torch.equal(got.double()[inf], want[inf])
+    at = touched & finite
+    d = (got.double() - want).abs()[at]
+    assert bool((d <= tol[at]).all()), (d - tol[at]).max()
+
+
+ODD = [float("inf"), float("-inf"), float("nan"), 0.0, -0.0, -1e30, 3e38]
+
+CASES = {
+    "one": dict(seed=1, V=1, dtype=torch.float32, gammas=[0]),
+    "seven": dict(seed=2, V=7, dtype=torch.bfloat16, gammas=[0, 0, 0], masks=2, bias=4),
+    "words": dict(seed=3, V=33, dtype=torch.float32, gammas=[0] * 5, masks=3, bias=5, pad=1),
+    "round": dict(seed=4, V=1000, dtype=torch.bfloat16, gammas=[3, 0, 5, 1], masks=4, bias=20, pad=3),
+    "draft rows": dict(seed=5, V=1001, dtype=torch.float32, gammas=[3, 0, 5, 1], target=False, masks=4, bias=20),
+    "chunk": dict(seed=6, V=8191, dtype=torch.float32, gammas=[2, 2], masks=2, bias=30),
+    "chunks": dict(seed=7, V=8193, dtype=torch.bfloat16, gammas=[4], bias=30, cap=3000),
+    "no draft rows": dict(seed=8, V=300, dtype=torch.float32, gammas=[0, 0], target=False),
+    "few tokens often": dict(seed=9, V=20000, dtype=torch.bfloat16, gammas=[0, 16], cap=5000, token_range=5, lengths=[5000, 4999]),
+    "odd values": dict(seed=10, V=2000, dtype=torch.float32, gammas=[2, 3], masks=3, values=ODD, cap=1500),
+    "odd values bf16": dict(seed=11, V=2001, dtype=torch.bfloat16, gammas=[2, 3], masks=3, values=ODD, cap=1500),
+    "empty histories": dict(seed=12, V=4097, dtype=torch.float32, gammas=[0] * 4, lengths=[0, 0, 0, 0], masks=2),
+    "lengths off the buffer": dict(seed=13, V=500, dtype=torch.float32, gammas=[0] * 3, lengths=[-5, 1000, 2 ** 31 - 1]),
+    "numbers": dict(seed=14, V=50001, dtype=torch.bfloat16, gammas=[1] * 9, mixed=False, cap=700, masks=5, pad=2),
+    "many sequences": dict(seed=15, V=5000, dtype=torch.float32, gammas=[i % 4 for i in range(700)], cap=20, masks=9, bias=3),
+    "long drafts": dict(seed=16, V=3001, dtype=torch.bfloat16, gammas=[200, 1], token_range=40),
+}
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_adjust(gpu, ps, name):
+    print(f"[case] adjust {name}", flush=True)
+    kw = dict(CASES[name])
+    pad = kw.get("pad", 0)
+    c = Case(**kw)
+    _, z = c.device_rows(gpu, c.z, pad)
+    hist, args = c.arguments(ps, gpu)
+    want = c.expect()
+    out = ps.adjust(z, c.V, hist, **args)
+    assert out.shape == (c.rows, c.V) and out.dtype == c.dtype
+    hold(out, *want, c.z)
+    assert same_bits(ps.adjust(z, c.V, hist, **args), out)
+    # into rows of another stride, what lies between them untouched; and in place
+    whole, into = c.device_rows(gpu, torch.zeros_like(c.z), 5)
+    assert ps.adjust(z, c.V, hist, out=into, **args) is into or c.rows == 0
+    assert same_bits(into, out) and bool((whole[:, c.V:] == 7).all())
+    whole, into = c.device_rows(gpu, c.z, pad)
+    ps.adjust(into, c.V, hist, out=into, **args)
+    assert same_bits(into, out) and bool((whole[:, c.V:] == 7).all())
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_adjust_grad(gpu, ps, name):
+    print(f"[case] adjust_grad {name}", flush=True)
+    c = Case(**CASES[name])
+    _, z = c.device_rows(gpu, c.z, CASES[name].get("pad", 0))
+    hist, args = c.arguments(ps, gpu, grad=True)
+    want = c.expect_grad()
+    g = c.grad.to(gpu)
+    out = ps.adjust_grad(g, z, c.V, hist, **args)
+    hold(out, *want, c.grad)
+    whole, into = c.device_rows(gpu, c.grad, 3)
+    ps.adjust_grad(into, z, c.V, hist, out=into, **args)
+    assert same_bits(into, out) and bool((whole[:, c.V:] == 7).all())
+
+
+def test_long_rows_and_histories(gpu, ps):
+    print("[case] adjust long", flush=True)
+    for dtype in (torch.float32, torch.bfloat16):
+        c = Case(21, 151936, dtype, [4, 0], cap=100_000, masks=2, bias=100, lengths=[100_000, 70_001])
+        hist, args = c.arguments(ps, gpu)
+        hold(ps.adjust(c.z.to(gpu), c.V, hist, **args), *c.expect(), c.z)
+
+
+def test_nothing_to_adjust(gpu, ps):
+    print("[case] adjust nothing", flush=True)
+    z = torch.randn(3, 777, device=gpu)
+    assert same_bits(ps.adjust(z, 777), z) and same_bits(ps.adjust(z, 500), z[:, :500])
+    hist = ps.History(torch.zeros((3, 0), dtype=torch.int32, device=gpu), torch.zeros(3, dtype=torch.int32, device=gpu))
+    assert same_bits(ps.adjust(z, 777, hist, repetition=2.0), z)
+    assert ps.adjust(torch.empty(0, 777, device=gpu), 777).shape == (0, 777)
+
+
+def test_settings_that_a_host_would_refuse_count_as_none(gpu, ps):
+    print("[case] adjust settings", flush=True)
+    z = torch.randn(5, 100, device=gpu)
+    hist = ps.History(torch.arange(100, dtype=torch.int32, device=gpu).repeat(5, 1), torch.full((5,), 100, dtype=torch.int32, device=gpu))
+    t = lambda *v: torch.tensor(v, dtype=torch.float32, device=gpu)                                                       # noqa: E731
+    nan, inf = float("nan"), float("inf")
+    out = ps.adjust(z, 100, hist, repetition=t(0, -1, nan, inf, 1), presence=t(nan, inf, -inf, 0, 0), frequency=t(0, 0, nan, inf, -inf))
+    assert same_bits(out, z)
+
+
+def test_the_last_of_equal_biases_counts_wherever_they_stand(gpu, ps):
+    print("[case] adjust bias twice", flush=True)
+    n = 2000
+    ids = torch.randint(0, 9000, (n,), generator=torch.Generator().manual_seed(3), dtype=torch.int32) % 700
+    val = torch.arange(1, n + 1, dtype=torch.float32)
+    want = torch.zeros(9000)
+    for i in range(n):
+        want[int(ids[i])] = val[i]
+    bias = ps.Bias(torch.tensor([0, n], dtype=torch.int32, device=gpu), ids.to(gpu), val.to(gpu))
+    assert torch.equal(ps.adjust(torch.zeros(1, 9000, device=gpu), 9000, bias=bias).cpu()[0], want)
+
+
+def test_rows_behind_the_last_sequence_are_left_as_they_are(gpu, ps):
+    print("[case] adjust padded batch", flush=True)
+    # (offsets that end before the last row, as those of a batch padded for a graph do: sequences behind the end have no drafts)
+    z = torch.randn(6, 100, device=gpu)
+    out = torch.full((6, 100), 5.0, device=gpu)
+    off = torch.tensor([0, 2, 2], dtype=torch.int32, device=gpu)
+    draft = torch.tensor([1, 2, 3, 4], dtype=torch.int32, device=gpu)
+    ps.adjust(z, 100, presence=1.0, seq_off=off, draft_tok=draft, out=out)
+    assert bool((out[4:] == 5).all())
+    want = z.clone()
+    want[1, 1] -= 1
+    want[2, 1] -= 1
+    want[2, 2] -= 1
+    assert torch.allclose(out[:4], want[:4], rtol=0, atol=2.0 ** -22)
+
+
+def test_gradient_is_that_of_the_differences(gpu, ps):
+    print("[case] adjust differences", flush=True)
+    from paper_2603_19133_amd import training
+    c = Case(31, 400, torch.float32, [2, 1], cap=200, masks=2, bias=10)
+    hist, args = c.arguments(ps, gpu)
+    z0 = torch.where(c.z.abs() < 0.1, torch.tensor(0.5), c.z).to(gpu)                  # (away from 0, where the slope changes)
+    z = z0.clone().requires_grad_()
+    w = torch.randn(c.rows, c.V, device=gpu, generator=torch.Generator(device=gpu).manual_seed(1))
+    out = training.adjust(z, c.V, hist, **args)
+    torch.where(out.isinf(), 0.0, out * w).sum().backward()
+    h = 2.0 ** -5
+    up, down = ps.adjust(z0 + h, c.V, hist, **args), ps.adjust(z0 - h, c.V, hist, **args)
+    slope = torch.where(up.isinf(), 0.0, (up.double() - down.double()) / (2 * h)) * w
+    # each difference: two roundings of values below 64 (2^-24 of them each) and of z +- h (as much, times 2), over 2 h
+    assert bool(((z.grad.double() - slope).abs() <= (4 * 64 * 2.0 ** -24 * 2 / (2 * h) + 2.0 ** -22) * w.abs()).all())
+
+
+def test_on_the_tape(gpu, ps):
+    print("[case] adjust on the tape", flush=True)
+    from paper_2603_19133_amd import training
+    c = Case(32, 501, torch.bfloat16, [2, 4, 0], cap=60, masks=3)
+    hist, args = c.arguments(ps, gpu)
+    z = torch.zeros((c.rows, c.V + 6), dtype=c.dtype, device=gpu)
+    z[:, :c.V] = c.z.to(gpu)
+    z.requires_grad_()
+    out = training.adjust(z, c.V, hist, **args)
+    assert same_bits(out.detach(), ps.adjust(z.detach(), c.V, hist, **args))
+    out.backward(c.grad.to(gpu))
+    rep = {k: args[k] for k in ("repetition", "mask", "mask_row", "seq_off", "draft_tok") if k in args}
+    assert same_bits(z.grad[:, :c.V], ps.adjust_grad(c.grad.to(gpu), z.detach(), c.V, hist, **rep)) and bool((z.grad[:, c.V:] == 0).all())
+    # one value seen from every place; and a second derivative is refused
+    z.grad = None
+    training.adjust(z, c.V, hist, repetition=args["repetition"], seq_off=args["seq_off"], draft_tok=args["draft_tok"]).sum().backward()
+    assert z.grad.isfinite().all()
+    with pytest.raises(RuntimeError, match="differentiable once"):
+        torch.autograd.grad(training.adjust(z, c.V, hist, **args).float().sum(), z, create_graph=True)
+    # a history that moves on between the two calls is noticed
+    out = training.adjust(z, c.V, hist, **args)
+    hist.length.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.backward(c.grad.to(gpu))
+
+
+def test_refusals(gpu, ps):
+    print("[case] adjust refusals", flush=True)
+    z = torch.randn(3, 100, device=gpu)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device=gpu)                                                       # noqa: E731
+    hist = ps.History(torch.zeros((3, 9), dtype=torch.int32, device=gpu), i32(1, 2, 3))
+    words = torch.zeros((3, 4), dtype=torch.int32, device=gpu)
+    bad = [dict(V=101), dict(V=0), dict(hist=ps.History(hist.tok[:2], hist.length)), dict(hist=ps.History(hist.tok.long(), hist.length)), dict(hist=ps.History(hist.tok, hist.length.long())),
+           dict(hist=ps.History(hist.tok, hist.length[:2])), dict(hist=ps.History(hist.tok.cpu(), hist.length)), dict(hist=ps.History(hist.tok, hist.length, i32(1))),
+           dict(hist=ps.History(torch.zeros((9, 3), dtype=torch.int32, device=gpu).t(), hist.length)), dict(hist=ps.History(hist.tok[:1].expand(3, 9), hist.length)),
+           dict(repetition=torch.ones(2, device=gpu)), dict(repetition=torch.ones(3, device=gpu, dtype=torch.float64)), dict(repetition=torch.ones(3)), dict(repetition=0.0), dict(presence=float("nan")),
+           dict(mask=words[:2]), dict(mask=words[:, :3]), dict(mask=words.long()), dict(mask=words, mask_row=i32(0, 1)), dict(mask_row=i32(0, 1, 2)), dict(draft_tok=i32(1)),
+           dict(seq_off=i32(0, 1, 2), draft_tok=i32(1, 2)), dict(seq_off=i32(0, 1, 2).long(), draft_tok=i32(1)), dict(bias=ps.Bias(i32(0, 0, 0), i32(), torch.zeros(0, device=gpu))),
+           dict(bias=ps.Bias(i32(0, 0, 0, 1), i32(1), torch.zeros(2, device=gpu))), dict(out=torch.zeros(3, 99, device=gpu)), dict(out=torch.zeros(2, 100, device=gpu)), dict(out=torch.zeros(3, 100)),
+           dict(out=torch.zeros(100, 3, device=gpu).t())]
+    for kw in bad:
+        kw = dict(kw)
+        with pytest.raises(ps.PicoSpecError) as e:
+            ps.adjust(z, kw.pop("V", 100), **{"hist": hist, **kw})
+        assert e.value.code == ps.EINVAL, kw
+    for f in (lambda: ps.adjust(z.half(), 100), lambda: ps.adjust(z, 100, out=z.bfloat16()), lambda: ps.adjust_grad(z.bfloat16(), z, 100)):
+        with pytest.raises(ps.PicoSpecError) as e:
+            f()
+        assert e.value.code == ps.EDTYPE
+    flat = torch.randn(700, device=gpu)
+    a, b = flat[:300].view(3, 100), flat[50:350].view(3, 100)
+    with pytest.raises(ps.PicoSpecError):
+        ps.adjust(a, 100, out=b)
+    with pytest.raises(ps.PicoSpecError):
+        ps.adjust_grad(torch.randn(3, 100, device=gpu), a, 100, out=a)
