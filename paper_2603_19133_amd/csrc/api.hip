@@ -613,7 +613,7 @@ int check_adjust(const void* src, int64_t ld_src, const void* logits, int dtype,
     const Span to = span(out, n_rows, ld_out, V, esize(dtype));
     if (!(out == src && ld_out == ld_src) && overlap(to, span(src, n_rows, ld_src, V, esize(dtype)))) return PICOSPEC_EINVAL;
     if (logits != src && overlap(to, span(logits, n_rows, ld, V, esize(dtype)))) return PICOSPEC_EINVAL;
-    if ((int64_t)B * ((V + kAdjustChunk / 2 - 1) / (kAdjustChunk / 2)) * kAdjustThreads > UINT32_MAX) return PICOSPEC_EUNSUPPORTED;      // (threads of one launch)
+    if (adjust_threads_most(dtype, B, V) > UINT32_MAX) return PICOSPEC_EUNSUPPORTED;
     return PICOSPEC_OK;
 }
 
@@ -685,7 +685,8 @@ int picospec_embed_grad(const void* grad, int dtype, int64_t ld, int32_t n, cons
     if (n > 0 && (!grad || !tok || (uintptr_t)grad % esize(dtype))) return PICOSPEC_EINVAL;
     if (n > 0 && overlap(span(table_grad, V, ld_table, d, esize(dtype_table)), span(grad, n, ld, d, esize(dtype)))) return PICOSPEC_EINVAL;
     if (n == 0 && accumulate) return PICOSPEC_OK;
-    if (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < embed_scratch(n, V, d).bytes) return PICOSPEC_EWORKSPACE;
+    const size_t need = embed_scratch(n, V, d).bytes;
+    if (((uintptr_t)workspace & 15u) || (need > 0 && (!workspace || workspace_bytes < need))) return PICOSPEC_EWORKSPACE;
     EmbedGradArgs a{};
     a.g = grad; a.ld = ld; a.d = d; a.out = table_grad; a.ld_out = ld_table; a.V = V; a.scale = scale; a.accumulate = accumulate;
     return hip_status(launch_embed_grad(a, dtype, dtype_table, tok, n, workspace, (hipStream_t)stream));

@@ -483,30 +483,37 @@ struct AdjustArgs {
     const float *repetition_rows, *presence_rows, *frequency_rows;
     const int32_t *bias_off, *bias_id; const float* bias_value; int n_bias;
     const uint32_t* mask; int64_t ld_mask; int n_masks; const int32_t* mask_row;
-    int chunk, chunks, parts, in_place;
+    int chunks, parts, in_place;
 };
-constexpr int kAdjustThreads = 256, kAdjustChunk = 8192;          // ids of the largest chunk
+constexpr int kAdjustGroups = 2048;                               // workgroups (of 256 threads) that fill the chip
+// An upper bound of the threads of a launch: a thread has one vector or more; or the rows are shared out until there are kAdjustGroups workgroups, or in two
+inline int64_t adjust_threads_most(int dtype, int64_t B, int V) { const int ids = dtype == 1 ? 2048 : 1024; return std::max<int64_t>(2 * B * ((V + ids - 1) / ids), 2 * kAdjustGroups) * 256; }
 hipError_t launch_adjust(AdjustArgs a, int dtype, int B, int64_t n_rows, bool gradient, hipStream_t stream);
 
 // ---- token embeddings (csrc/embed.hip)
 hipError_t launch_embed(const void* table, int dtype, int64_t ld, int V, int64_t d, const int32_t* tok, int64_t n, float scale, void* out, int64_t ld_out, hipStream_t stream);
 
-// The gradient's workspace: where each token's positions begin, the positions by token, the tokens of the pieces, the pieces' sums
-constexpr int kSortThreads = 1024, kSortLds = 64 * 1024, kPiece = 64;
+// The gradient's workspace: where each token's positions begin and how many they are, positions and tokens in that order, the tokens of the pieces, words to arrive at, the pieces' sums.
+// Up to kFewTokens positions need none of it.
+constexpr int kSortThreads = 1024, kSortList = 256, kSortLds = 64 * 1024, kPiece = 32, kPiecesMost = 128, kFewTokens = 1024;
+constexpr int kTokensMost = 8, kTilesMost = 8;                    // tokens of a workgroup that writes zeros, workgroups that share a row
 constexpr int64_t kEmbedMostTokens = 1 << 26;
-inline int embed_range(int V) { return std::min(std::max((V + 255) / 256, 1), kSortLds / (kSortThreads / 64 * 4)); }
-// A token's pieces: kPiece positions each, the last one those that are left as well.  Their slots begin at start / kPiece, and a token's last slot lies in front of the next one's first:
+// Workgroups of the sort: 256, more where a workgroup's tokens would be more than its threads
+inline int embed_owners_log2(int V) { int l = 8; while (((V + (1 << l) - 1) >> l) > kSortLds / (kSortThreads / 64 * 4)) ++l; return l; }
+// A token's pieces, of kPiece positions or more.  Their slots begin at start / kPiece, and a token's last slot lies in front of the next one's first:
 // start / kPiece + len / kPiece <= (start + len) / kPiece.
 struct EmbedPieces { int slot, count; };
-__host__ __device__ inline EmbedPieces embed_pieces(int start, int len) { return {start / kPiece, len < 2 * kPiece ? 0 : len / kPiece}; }
-struct EmbedScratch { size_t order_at, slot_at, partial_at, bytes; int slots; int64_t d_pad; };
+__host__ __device__ inline EmbedPieces embed_pieces(int start, int len) { return {start / kPiece, len < 2 * kPiece ? 0 : len / kPiece < kPiecesMost ? len / kPiece : kPiecesMost}; }
+struct EmbedScratch { size_t order_at, slot_at, arrived_at, partial_at, bytes; int slots; int64_t d_pad; };
 inline EmbedScratch embed_scratch(int64_t n, int64_t V, int64_t d) {
-    EmbedScratch l;
-    l.slots = n < 2 * kPiece ? 0 : (int)(n / kPiece);
+    EmbedScratch l{};
+    if (n <= kFewTokens) return l;
+    l.slots = (int)(n / kPiece);
     l.d_pad = (d + 7) / 8 * 8;
-    l.order_at = ((size_t)V + 1 + 63) / 64 * 256;
-    l.slot_at = l.order_at + ((size_t)n + 63) / 64 * 256;
-    l.partial_at = l.slot_at + ((size_t)l.slots + 63) / 64 * 256;
+    l.order_at = ((size_t)V + 1 + 31) / 32 * 256;
+    l.slot_at = l.order_at + ((size_t)n + 31) / 32 * 256;
+    l.arrived_at = l.slot_at + ((size_t)l.slots + 63) / 64 * 256;
+    l.partial_at = l.arrived_at + ((size_t)l.slots * kTilesMost + 63) / 64 * 256;
     l.bytes = l.partial_at + (size_t)l.slots * l.d_pad * 4;
     return l;
 }
@@ -514,8 +521,8 @@ struct EmbedGradArgs {
     const void* g; int64_t ld, d;
     void* out; int64_t ld_out; int V;
     float scale; int accumulate;
-    const int32_t *first, *order, *slot_tok; float* partial; int64_t d_pad;
-    int slots, slot_groups, share;
+    const int2 *info, *order; const int32_t* slot_tok; uint32_t* arrived; float* partial; int64_t d_pad;
+    int slots, windows, tiles, share;
 };
 hipError_t launch_embed_grad(EmbedGradArgs a, int dtype, int out_dtype, const int32_t* tok, int n, void* workspace, hipStream_t stream);
 

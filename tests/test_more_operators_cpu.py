@@ -78,9 +78,11 @@ def test_embed_refuses_types_sizes_and_workspaces(B):
     assert _embed(B, V=(1 << 20) + 1) == B.EUNSUPPORTED and _embed_grad(B, V=(1 << 20) + 1) == B.EUNSUPPORTED and _embed_grad(B, n=(1 << 26) + 1, out=1 << 50) == B.EUNSUPPORTED
     assert _embed(B, n=0, tok=None, out=None, table=None) == B.OK
     assert _embed_grad(B, n=0, acc=1, tok=None, grad=None, ws=None, ws_bytes=0) == B.OK
-    need = B.workspace_bytes(B.CALL_EMBED_GRAD, B.F32, 4, 10, 8)
-    assert need >= 4 * (4 + 11)
-    assert _embed_grad(B, ws=None) == B.EWORKSPACE and _embed_grad(B, ws=FAKE + 8) == B.EWORKSPACE and _embed_grad(B, ws_bytes=need - 1) == B.EWORKSPACE
+    assert B.workspace_bytes(B.CALL_EMBED_GRAD, B.F32, 1024, 10, 8) == 0          # (few positions are looked up where they are)
+    need = B.workspace_bytes(B.CALL_EMBED_GRAD, B.F32, 1025, 10, 8)
+    assert need >= 4 * 1025 + 8 * 10 + 1025 // 64 * 8 * 4
+    many = dict(n=1025, out=1 << 50)
+    assert _embed_grad(B, ws=None, **many) == B.EWORKSPACE and _embed_grad(B, ws=FAKE + 8, **many) == B.EWORKSPACE and _embed_grad(B, ws_bytes=need - 1, **many) == B.EWORKSPACE
     # (a token's pieces have a row of sums each)
     assert B.workspace_bytes(B.CALL_EMBED_GRAD, B.BF16, 1 << 20, 1 << 20, 4096) >= (1 << 20) // 64 * 4096 * 4
     assert B.workspace_bytes(B.CALL_EMBED_GRAD, B.F32, 4, 10, 0) == 0
