@@ -281,7 +281,8 @@ hipError_t launch(const AdjustArgs& a, int B, int64_t n_rows, hipStream_t stream
     constexpr int N = Vec<BF16>::N;
     auto groups = [&](int ids) { return (int64_t)B * ((a.V + ids - 1) / ids); };
     if (a.hist_tok && a.hist_cap > 4 * (n_rows + B - 1) / B * (256 * 2 * N) && groups(8192) >= 512) return launch_one<BF16, GRAD, 512, 8192 / (512 * N)>(a, B, n_rows, stream);
-    if (!GRAD && groups(256 * 2 * N) >= 1024) return launch_one<BF16, GRAD, 256, 2>(a, B, n_rows, stream);
+    if constexpr (!GRAD)
+        if (groups(256 * 2 * N) >= 1024) return launch_one<BF16, GRAD, 256, 2>(a, B, n_rows, stream);
     return launch_one<BF16, GRAD, 256, 1>(a, B, n_rows, stream);
 }
 

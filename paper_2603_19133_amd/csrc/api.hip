@@ -717,6 +717,8 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
     Piece here[kHere], *pieces = here;
     if ((size_t)n_tensors * 2 > kHere && !(pieces = static_cast<Piece*>(std::malloc((size_t)n_tensors * 2 * sizeof(Piece))))) return PICOSPEC_EINVAL;
     size_t n_pieces = 0;
+    int64_t elements = 0, bytes = 0;
+    bool in_place = true;
     int rc = PICOSPEC_OK;
     for (int i = 0; i < n_tensors && rc == PICOSPEC_OK; ++i) {
         if (!known_dtype(dtypes[i])) { rc = PICOSPEC_EDTYPE; break; }
@@ -727,6 +729,9 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
         if (!g || !o || g % esz || o % esz) { rc = PICOSPEC_EINVAL; break; }
         pieces[n_pieces++] = {g, g + (size_t)numel[i] * esz};
         if (o != g) pieces[n_pieces++] = {o, o + (size_t)numel[i] * esz};
+        in_place &= o == g;
+        elements += numel[i];
+        bytes += numel[i] * (int64_t)esz;
     }
     if (rc == PICOSPEC_OK && any_overlap(pieces, n_pieces)) rc = PICOSPEC_EINVAL;
     if (pieces != here) std::free(pieces);
@@ -739,7 +744,12 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
         int64_t blocks = 0;
         c.n = 0;
         c.first[0] = 0;
+        c.block = clip_block(elements);
+        c.in_place = in_place;
         auto go = [&] {
+            // (the second pass begins where the first one ends)
+            const int64_t kept = bytes > 0 ? (int64_t)((double)kClipCached / (double)bytes * (double)elements) / c.block : 0;
+            c.stream = (uint32_t)std::max<int64_t>(blocks - kept, 0);
             const hipError_t e = f(c, (int)std::min<int64_t>(blocks, kClipGroups));
             c.n = 0;
             blocks = 0;
@@ -747,7 +757,7 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
         };
         for (int i = 0; i < n_tensors; ++i) {
             if (numel[i] == 0) continue;
-            const int64_t more = (numel[i] + kClipBlock - 1) / kClipBlock;
+            const int64_t more = (numel[i] + c.block - 1) / c.block;
             if (c.n == kClipTensors || blocks + more > INT32_MAX)
                 if (hipError_t e = go()) return e;
             c.grad[c.n] = grads[i];
@@ -776,9 +786,7 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
             })) return hip_status(e);
     }
     if (named) return PICOSPEC_OK;
-    ClipTensors none;
-    none.n = 0;
-    none.first[0] = 0;
+    ClipTensors none{};
     return hip_status(launch_clip_scale(none, partial, partials, max_norm, norm, 1, s));
 }
 

@@ -10,7 +10,7 @@ namespace picospec {
 
 namespace {
 
-constexpr int kCT = 256, kCW = kCT / kWave, kUnroll = 4;
+constexpr int kCT = 256, kCW = kCT / kWave;
 
 template <int N>
 __device__ __forceinline__ double squares(const float (&f)[N])
@@ -34,49 +34,53 @@ __device__ __forceinline__ double block_sum(double v)
     return s;
 }
 
-// The tensor that block `k` of the launch lies in (kClipBlock elements each, a tensor's last one shorter)
-__device__ __forceinline__ int tensor_of(const ClipTensors& c, int64_t k)
-{
-    int lo = 0, hi = c.n;                                         // c.first[lo] <= k < c.first[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if ((int64_t)c.first[mid] <= k) lo = mid; else hi = mid;
-    }
-    return lo;
-}
-
-// f(tensor, first element, end) for the blocks of this workgroup, ascending or descending
+// f(tensor, first element, end, block) for the blocks blockIdx.x, blockIdx.x + gridDim.x, .. of the launch's tensors (c.block elements each, a tensor's last one shorter), ascending or descending
 template <class F>
 __device__ __forceinline__ void each_block(const ClipTensors& c, bool down, F f)
 {
-    const int64_t blocks = c.first[c.n];
-    const int64_t trips = blocks > (int64_t)blockIdx.x ? (blocks - blockIdx.x + gridDim.x - 1) / gridDim.x : 0;
+    const int64_t blocks = c.first[c.n], here = blockIdx.x, step = gridDim.x;
+    if (here >= blocks) return;
+    const int64_t trips = (blocks - here + step - 1) / step;
+    int lo = 0, hi = c.n;                                         // c.first[lo] <= k < c.first[hi]
     for (int64_t i = 0; i < trips; ++i) {
-        const int64_t k = (int64_t)blockIdx.x + (down ? trips - 1 - i : i) * gridDim.x;
-        const int t = tensor_of(c, k);
-        const int64_t begin = (k - (int64_t)c.first[t]) * kClipBlock;
-        f(t, begin, min(begin + (int64_t)kClipBlock, c.numel[t]));
+        const int64_t k = here + (down ? trips - 1 - i : i) * step;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if ((int64_t)c.first[mid] <= k) lo = mid; else hi = mid;
+        }
+        while ((int64_t)c.first[lo + 1] <= k) ++lo;               // (from the block before on: a step or none, mostly)
+        while ((int64_t)c.first[lo] > k) --lo;
+        hi = lo + 1;
+        const int64_t begin = (k - (int64_t)c.first[lo]) * c.block;
+        f(lo, begin, min(begin + (int64_t)c.block, c.numel[lo]), k);
     }
 }
 
-template <bool BF16>
+template <bool BF16, bool STREAM>
 __device__ __forceinline__ double block_squares(const char* g, int64_t begin, int64_t end)
 {
-    constexpr int N = Vec<BF16>::N, STEP = kCT * N;
+    constexpr int N = Vec<BF16>::N, ESZ = BF16 ? 2 : 4, STEP = kCT * N, AHEAD = 4;
     double s = 0.0;
-    for (int64_t x = begin + (int64_t)threadIdx.x * N; x < end; x += kUnroll * STEP) {
-        uint4 raw[kUnroll];
+    int64_t x = begin + (int64_t)threadIdx.x * N;
+    for (int64_t whole = begin + AHEAD * STEP; whole <= end; whole += AHEAD * STEP, x += AHEAD * STEP) {
+        uint4 raw[AHEAD];
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j) {
-            raw[j] = make_uint4(0, 0, 0, 0);
-            if (x + j * STEP < end) raw[j] = load_row_vec<BF16>(g, x + j * STEP, end);
+        for (int j = 0; j < AHEAD; ++j) {
+            const loose_t* const p = reinterpret_cast<const loose_t*>(g + (x + j * STEP) * ESZ);
+            const u32x4_t v = STREAM ? __builtin_nontemporal_load(p) : *p;
+            raw[j] = make_uint4(v.x, v.y, v.z, v.w);
         }
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j) {
+        for (int j = 0; j < AHEAD; ++j) {
             float f[N];
             unpack<BF16>(raw[j], f);
             s += squares(f);
         }
+    }
+    for (; x < end; x += STEP) {
+        float f[N];
+        unpack<BF16>(load_row_vec<BF16>(g, x, end), f);
+        s += squares(f);
     }
     return s;
 }
@@ -84,36 +88,45 @@ __device__ __forceinline__ double block_squares(const char* g, int64_t begin, in
 __global__ __launch_bounds__(kCT) void clip_norm_kernel(const ClipTensors c, double* partial)
 {
     double s = 0.0;
-    each_block(c, false, [&](int t, int64_t begin, int64_t end) {
+    each_block(c, false, [&](int t, int64_t begin, int64_t end, int64_t k) {
         const char* const g = (const char*)c.grad[t];
-        s += c.bf16[t] ? block_squares<true>(g, begin, end) : block_squares<false>(g, begin, end);
+        if (k < (int64_t)c.stream) s += c.bf16[t] ? block_squares<true, true>(g, begin, end) : block_squares<false, true>(g, begin, end);
+        else s += c.bf16[t] ? block_squares<true, false>(g, begin, end) : block_squares<false, false>(g, begin, end);
     });
     s = block_sum(s);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
 template <bool BF16>
+__device__ __forceinline__ uint4 scaled(const uint4& raw, double by)
+{
+    if (by == 1.0) return raw;                                    // (the tensor's bits)
+    float f[Vec<BF16>::N];
+    unpack<BF16>(raw, f);
+#pragma unroll
+    for (int e = 0; e < Vec<BF16>::N; ++e) f[e] = (float)((double)f[e] * by);
+    return pack_vec<BF16>(f);
+}
+
+template <bool BF16>
 __device__ __forceinline__ void block_scale(const char* g, char* out, int64_t begin, int64_t end, double by)
 {
-    constexpr int N = Vec<BF16>::N, STEP = kCT * N;
-    for (int64_t x = begin + (int64_t)threadIdx.x * N; x < end; x += kUnroll * STEP) {
-        uint4 raw[kUnroll];
+    constexpr int N = Vec<BF16>::N, ESZ = BF16 ? 2 : 4, STEP = kCT * N, AHEAD = 4;
+    int64_t x = begin + (int64_t)threadIdx.x * N;
+    for (int64_t whole = begin + AHEAD * STEP; whole <= end; whole += AHEAD * STEP, x += AHEAD * STEP) {
+        uint4 raw[AHEAD];
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j)
-            if (x + j * STEP < end) raw[j] = load_row_vec<BF16>(g, x + j * STEP, end);
+        for (int j = 0; j < AHEAD; ++j) {
+            const u32x4_t v = *reinterpret_cast<const loose_t*>(g + (x + j * STEP) * ESZ);
+            raw[j] = make_uint4(v.x, v.y, v.z, v.w);
+        }
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j)
-            if (x + j * STEP < end) {
-                if (by != 1.0) {
-                    float f[N];
-                    unpack<BF16>(raw[j], f);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) f[e] = (float)((double)f[e] * by);
-                    raw[j] = pack_vec<BF16>(f);
-                }
-                store_row_vec<BF16>(out, x + j * STEP, end, raw[j]);
-            }
+        for (int j = 0; j < AHEAD; ++j) {
+            const uint4 r = scaled<BF16>(raw[j], by);
+            __builtin_nontemporal_store(u32x4_t{r.x, r.y, r.z, r.w}, reinterpret_cast<loose_t*>(out + (x + j * STEP) * ESZ));
+        }
     }
+    for (; x < end; x += STEP) store_row_vec<BF16>(out, x, end, scaled<BF16>(load_row_vec<BF16>(g, x, end), by));
 }
 
 __global__ __launch_bounds__(kCT) void clip_scale_kernel(const ClipTensors c, const double* partial, int partials, float max_norm, float* norm_out)
@@ -123,10 +136,10 @@ __global__ __launch_bounds__(kCT) void clip_scale_kernel(const ClipTensors c, co
     const double norm = sqrt(block_sum(s)), by64 = (double)max_norm / (norm + 1e-6);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const double by = by64 >= 1.0 ? 1.0 : by64;                   // (a norm of NaN: NaN; in 64 bits: the factor of a norm beyond fp32's range is below its normal numbers)
-    each_block(c, true, [&](int t, int64_t begin, int64_t end) {
+    if (by == 1.0 && c.in_place) return;
+    each_block(c, true, [&](int t, int64_t begin, int64_t end, int64_t) {
         const char* const g = (const char*)c.grad[t];
         char* const out = (char*)c.out[t];
-        if (by == 1.0 && out == g) return;
         if (c.bf16[t]) block_scale<true>(g, out, begin, end, by);
         else block_scale<false>(g, out, begin, end, by);
     });

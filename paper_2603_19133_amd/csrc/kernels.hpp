@@ -527,15 +527,23 @@ struct EmbedGradArgs {
 hipError_t launch_embed_grad(EmbedGradArgs a, int dtype, int out_dtype, const int32_t* tok, int n, void* workspace, hipStream_t stream);
 
 // ---- the norm over many tensors and their clipping (csrc/clip.hip): the tensors of one launch, as a kernel argument
-constexpr int kClipTensors = 128, kClipBlock = 16384, kClipGroups = 2048;        // tensors of a launch, elements that a workgroup takes at a time, workgroups of a launch
+constexpr int kClipTensors = 128, kClipGroups = 2048;             // tensors and workgroups of a launch
 struct ClipTensors {
     const void* grad[kClipTensors];
     void* out[kClipTensors];
     int64_t numel[kClipTensors];
     uint32_t first[kClipTensors + 1];                             // blocks in front of each tensor, and all of them
     uint8_t bf16[kClipTensors];
-    int n;
+    int n, block;                                                 // block: elements that a workgroup takes at a time
+    uint32_t stream;                                              // blocks whose loads for the norm pass by the caches: those that the second pass would not find there
+    int in_place;                                                 // whether every output is its tensor
 };
+// Elements that a workgroup takes at a time: the same number of blocks for each, of up to 16,384 elements
+inline int clip_block(int64_t elements) {
+    const int64_t trips = (elements + kClipGroups * 16384ll - 1) / (kClipGroups * 16384ll);
+    return (int)std::max<int64_t>((elements + kClipGroups * trips * 1024 - 1) / std::max<int64_t>(kClipGroups * trips * 1024, 1) * 1024, 1024);
+}
+constexpr int64_t kClipCached = 192ll << 20;                      // bytes that the second pass still finds in the caches
 inline size_t clip_scratch_bytes(int64_t n_tensors) { return (size_t)((n_tensors + kClipTensors - 1) / kClipTensors) * kClipGroups * 8; }
 hipError_t launch_clip_norm(const ClipTensors& c, double* partial, int groups, hipStream_t stream);
 hipError_t launch_clip_scale(const ClipTensors& c, const double* partial, int partials, float max_norm, float* norm, int groups, hipStream_t stream);
