@@ -272,10 +272,10 @@ hipError_t launch_one(AdjustArgs a, int B, int64_t n_rows, hipStream_t stream)
     const size_t lds = (size_t)IDS * (4 + (BF16 ? 2 : 4) + (!GRAD && a.bias_off ? 4 : 0));
     a.chunks = (a.V + IDS - 1) / IDS;
     const int64_t groups = (int64_t)B * a.chunks, mean = (n_rows + B - 1) / B;
-    // A sequence's rows shared out, each share counting the history again: where there are fewer than kAdjustGroups workgroups (us, one share / two / four: 8 sequences of 9 rows of 128,256 fp32
+    // A sequence's rows shared out, each share counting the history again: where there are fewer than kAdjustGroups workgroups of 256 threads (us, one share / two / four: 8 sequences of 9 rows of 128,256 fp32
     // 14.2 / 12.5 / 14.2, gradients of 32 sequences of 9.5 rows of 32,000 fp32 27 / 20.5 / 20.4), and where rows are so many that the sequences' ends are far apart (256 of 9.5 rows of 151,936 bf16 309 / 300 / 323;
     // of 5 rows of 75,000 fp32 177 / 182 / 208)
-    a.parts = (int)std::min<int64_t>(mean, std::max<int64_t>((kAdjustGroups + groups - 1) / groups, mean >= 8 ? 2 : 1));
+    a.parts = (int)std::min<int64_t>(mean, std::max<int64_t>((kAdjustGroups * 256 / T + groups - 1) / groups, mean >= 8 ? 2 : 1));
     static DeviceFlags done;
     int dev;
     if (lds > 64 * 1024)
@@ -285,7 +285,9 @@ hipError_t launch_one(AdjustArgs a, int B, int64_t n_rows, hipStream_t stream)
 }
 
 // Which way, us:
-//   512 threads, 8192 ids   histories that are long beside the rows (each chunk reads the history): 512 single rows of 151,936 fp32, up to 32,768 tokens 193, with 2048 ids 252
+//   512 threads             histories that are longer than what a sequence has of rows in a chunk (each chunk reads the history).  8192 ids where these are workgroups enough: 512 single rows of
+//                           151,936 fp32, up to 32,768 tokens 193, with 2048 ids 252; 64 of bf16 23 (26, with one vector 28).  Else one vector: a row of 151,936 bf16 with 32,768 tokens 8.8 (8192 ids 10.6, 256
+//                           threads 11.8), 9 rows of it with 100,000 20 (23, 30)
 //   256 threads, 2 vectors  512 single rows of 151,936 bf16 87 (with one vector 124, 8192 ids 92), 64 of 128,256 fp32 17.6 (20, 19)
 //   256 threads, 1 vector   gradients (128 sequences of 5.5 rows of 128,256 bf16 82, with two vectors 95) and what would leave compute units without work (64 of 6.5 rows of 50,001 bf16 27.7 / 30.1)
 template <bool BF16, bool GRAD>
@@ -293,7 +295,8 @@ hipError_t launch(const AdjustArgs& a, int B, int64_t n_rows, hipStream_t stream
 {
     constexpr int N = Vec<BF16>::N;
     auto groups = [&](int ids) { return (int64_t)B * ((a.V + ids - 1) / ids); };
-    if (a.hist_tok && a.hist_cap > 4 * (n_rows + B - 1) / B * (256 * 2 * N) && groups(8192) >= 512) return launch_one<BF16, GRAD, 512, 8192 / (512 * N)>(a, B, n_rows, stream);
+    if (a.hist_tok && a.hist_cap > (n_rows + B - 1) / B * (256 * 2 * N))
+        return groups(8192) >= 1024 ? launch_one<BF16, GRAD, 512, 8192 / (512 * N)>(a, B, n_rows, stream) : launch_one<BF16, GRAD, 512, 1>(a, B, n_rows, stream);
     if constexpr (!GRAD)
         if (groups(256 * 2 * N) >= 1024) return launch_one<BF16, GRAD, 256, 2>(a, B, n_rows, stream);
     return launch_one<BF16, GRAD, 256, 1>(a, B, n_rows, stream);
