@@ -2,9 +2,12 @@
 
 The calls as a program uses them, in turn:
 
+  training.embed       the models' tokens, with the table's gradient
+  binding.adjust       the roll-out's rows with a penalty for what each sequence holds already
   binding.sample       rolls out tokens from the target (temperature, top-p) and drafts from the drafter
   binding.compress     Top-K records of the target's rows: all that a trainer keeps of the target
   training.distill_loss  the drafter's divergence from the records and the expected acceptance, through torch's autograd
+  training.clip_grad_norm  the drafter's gradients, scaled to a norm of at most 1
   binding.round        compress, verification and draw of a speculative round, before and after the training
 
 Both models are a table of bigram logits of low rank (no downloads): the target's is fixed, the drafter starts at random.
@@ -22,7 +25,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2603_19133_amd import binding as ps  # noqa: E402
-from paper_2603_19133_amd.training import distill_loss  # noqa: E402
+from paper_2603_19133_amd.training import clip_grad_norm, distill_loss, embed  # noqa: E402
 
 V, T, K, GAMMA = 4096, 0.8, 64, 4
 
@@ -34,7 +37,7 @@ class Bigram(torch.nn.Module):
         self.out = torch.nn.Parameter(torch.randn(rank, V, generator=generator, device="cuda") * scale / rank ** 0.5)
 
     def forward(self, tok: torch.Tensor) -> torch.Tensor:
-        return self.emb[tok.long()] @ self.out
+        return embed(self.emb, tok) @ self.out
 
 
 @torch.no_grad()
@@ -64,6 +67,7 @@ def main(steps: int = 150, batch: int = 512, seed: int = 0, verbose: bool = True
     start = torch.randint(0, V, (256,), generator=g, device="cuda", dtype=torch.int32)
     before = accepted(target, drafter, start, g)
     tok = torch.randint(0, V, (batch,), generator=g, device="cuda", dtype=torch.int32)
+    hist = ps.History(torch.zeros((batch, steps + 1), dtype=torch.int32, device="cuda"), torch.zeros(batch, dtype=torch.int32, device="cuda"))
     first = last = None
     for step in range(steps):
         logits = target(tok)
@@ -71,12 +75,16 @@ def main(steps: int = 150, batch: int = 512, seed: int = 0, verbose: bool = True
         loss, accept = distill_loss(drafter(tok), rec, V, T, tail=1)
         opt.zero_grad(set_to_none=True)
         loss.mean().backward()
+        clip_grad_norm(drafter.parameters(), 1.0)
         opt.step()
         last = loss.mean().item(), accept.mean().item()
         first = first or last
         if verbose and (step % 25 == 0 or step == steps - 1):
             print(f"step {step:4d}  loss {last[0]:.4f}  expected acceptance {last[1]:.4f}", flush=True)
-        # the next tokens of the roll-out, a nucleus draw from the target
+        # the next tokens of the roll-out, a nucleus draw from the target that seldom says the same again
+        hist.tok[:, step] = tok
+        hist.length += 1
+        logits = ps.adjust(logits, V, hist, repetition=1.1)
         tok = ps.sample(logits, V, torch.rand(batch, generator=g, device="cuda"), temperature=T, top_p=0.95).tok
     after = accepted(target, drafter, start, g)
     if verbose:
