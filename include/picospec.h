@@ -543,7 +543,8 @@ int picospec_embed(const void* table, int dtype, int64_t ld, int32_t V, int32_t 
  *   grad [n, ld] of dtype, tok [n] in, n up to 2^26
  *   accumulate 0: every row of table_grad is written, zeros where a token does not occur; 1: the sums are added to what is there (in fp32, then rounded), other rows stay
  *   table_grad [V, ld_table] of dtype_table, may not overlap grad                                    out
- *   workspace: picospec_workspace_bytes(PICOSPEC_CALL_EMBED_GRAD, dtype, n, V, d) bytes on a 16-byte boundary, whatever they hold; needed where that is more than 0 (n > 1024)
+ *   workspace: picospec_workspace_bytes(PICOSPEC_CALL_EMBED_GRAD, dtype, n, V, d) bytes on a 16-byte boundary, whatever they hold; needed where that is more than 0 (n > 1024).
+ *              Calls that overlap in time must not share it
  */
 int picospec_embed_grad(const void* grad, int dtype, int64_t ld, int32_t n, const int32_t* tok, int32_t V, int32_t d, float scale, int accumulate,
                         void* table_grad, int dtype_table, int64_t ld_table, void* workspace, size_t workspace_bytes, void* stream);
@@ -557,7 +558,8 @@ int picospec_embed_grad(const void* grad, int dtype, int64_t ld, int32_t n, cons
  *                                        otherwise no two of the tensors and outputs may share a byte
  *   max_norm                             >= 0; inf: the norm alone (and a copy, if out is given)
  *   norm                                 device, fp32 [1]                                                                             out
- *   workspace: picospec_workspace_bytes(PICOSPEC_CALL_CLIP_GRAD, 0, n_tensors, 1, 0) bytes on a 16-byte boundary; needed
+ *   workspace: picospec_workspace_bytes(PICOSPEC_CALL_CLIP_GRAD, 0, n_tensors, 1, 0) bytes on a 16-byte boundary, whatever they hold; needed.  Calls that overlap in time must not
+ *              share it
  * The host arrays are read before the call returns: a captured call replays on the tensors that it was captured with.
  */
 int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtypes,

@@ -612,7 +612,7 @@ int check_adjust(const void* src, int64_t ld_src, const void* logits, int dtype,
     if (mask && (n_masks < 0 || ld_mask < ((int64_t)V + 31) / 32 || (!mask_row && n_masks < n_rows))) return PICOSPEC_EINVAL;
     const Span to = span(out, n_rows, ld_out, V, esize(dtype));
     if (!(out == src && ld_out == ld_src) && overlap(to, span(src, n_rows, ld_src, V, esize(dtype)))) return PICOSPEC_EINVAL;
-    if (logits != src && overlap(to, span(logits, n_rows, ld, V, esize(dtype)))) return PICOSPEC_EINVAL;
+    if (!(logits == src && ld == ld_src) && overlap(to, span(logits, n_rows, ld, V, esize(dtype)))) return PICOSPEC_EINVAL;
     if (adjust_threads_most(dtype, B, V) > UINT32_MAX) return PICOSPEC_EUNSUPPORTED;
     return PICOSPEC_OK;
 }
@@ -723,7 +723,7 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
     for (int i = 0; i < n_tensors && rc == PICOSPEC_OK; ++i) {
         if (!known_dtype(dtypes[i])) { rc = PICOSPEC_EDTYPE; break; }
         const size_t esz = esize(dtypes[i]);
-        if (numel[i] < 0 || numel[i] > (int64_t)1 << 42) { rc = PICOSPEC_EINVAL; break; }
+        if (numel[i] < 0 || numel[i] > kClipMost - elements) { rc = PICOSPEC_EINVAL; break; }
         if (numel[i] == 0) continue;
         const uintptr_t g = (uintptr_t)grads[i], o = out ? (uintptr_t)out[i] : g;
         if (!g || !o || g % esz || o % esz) { rc = PICOSPEC_EINVAL; break; }
@@ -740,7 +740,7 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
 
     // f(tensors of a launch, its workgroups), for all tensors that hold anything
     auto each_launch = [&](auto f) -> hipError_t {
-        ClipTensors c;
+        ClipTensors c;                                            // (its arrays are read as far as they are filled)
         int64_t blocks = 0;
         c.n = 0;
         c.first[0] = 0;
@@ -758,7 +758,7 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
         for (int i = 0; i < n_tensors; ++i) {
             if (numel[i] == 0) continue;
             const int64_t more = (numel[i] + c.block - 1) / c.block;
-            if (c.n == kClipTensors || blocks + more > INT32_MAX)
+            if (c.n == kClipTensors)
                 if (hipError_t e = go()) return e;
             c.grad[c.n] = grads[i];
             c.out[c.n] = out ? out[i] : const_cast<void*>(grads[i]);

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kCT) void clip_scale_kernel(const ClipTensors c, co
     for (int i = threadIdx.x; i < partials; i += kCT) s += partial[i];
     const double norm = sqrt(block_sum(s)), by64 = (double)max_norm / (norm + 1e-6);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-    const double by = by64 >= 1.0 ? 1.0 : by64;                   // (a norm of NaN: NaN; in 64 bits: the factor of a norm beyond fp32's range is below its normal numbers)
+    const double by = by64 >= 1.0 || max_norm == __builtin_huge_valf() ? 1.0 : by64;        // (a norm of NaN: NaN; in 64 bits: the factor of a norm beyond fp32's range is below its normal numbers)
     if (by == 1.0 && c.in_place) return;
     each_block(c, true, [&](int t, int64_t begin, int64_t end, int64_t) {
         const char* const g = (const char*)c.grad[t];

@@ -543,6 +543,7 @@ inline int clip_block(int64_t elements) {
     const int64_t trips = (elements + kClipGroups * 16384ll - 1) / (kClipGroups * 16384ll);
     return (int)std::max<int64_t>((elements + kClipGroups * trips * 1024 - 1) / std::max<int64_t>(kClipGroups * trips * 1024, 1) * 1024, 1024);
 }
+constexpr int64_t kClipMost = 1ll << 44;                          // elements of a call: blocks of 16,384 are counted in 32 bits
 constexpr int64_t kClipCached = 192ll << 20;                      // bytes that the second pass still finds in the caches
 inline size_t clip_scratch_bytes(int64_t n_tensors) { return (size_t)((n_tensors + kClipTensors - 1) / kClipTensors) * kClipGroups * 8; }
 hipError_t launch_clip_norm(const ClipTensors& c, double* partial, int groups, hipStream_t stream);

@@ -446,6 +446,7 @@ struct Adjustment {
             n_masks = mask.size(0);
             ld_mask = n_masks > 1 ? mask.stride(0) : mask.size(1);
             if (mask_row.defined()) list(mask_row, at::kInt, rows);
+            else refuse_unless(n_masks >= rows);
         } else {
             refuse_unless(!mask_row.defined());
         }

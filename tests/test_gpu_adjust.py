@@ -228,6 +228,35 @@ def test_long_rows_and_histories(gpu, ps):
         hold(ps.adjust(c.z.to(gpu), c.V, hist, **args), *c.expect(), c.z)
 
 
+def test_more_than_32_bits_of_elements(gpu, ps):
+    print("[case] adjust large offsets", flush=True)
+    B, V = 15000, 150001
+    z = torch.zeros((B, V), dtype=torch.bfloat16, device=gpu)
+    some = [0, 7158, 14318, B - 1]                                # (the border of 2^31 elements lies in row 14,316)
+    rows = torch.randn(4, V, device=gpu).bfloat16()
+    z[some] = rows
+    # histories a thousand million tokens apart
+    far = torch.zeros((1 << 31) + 4000, dtype=torch.int32, device=gpu)
+    hist = far.as_strided((3, 1000), ((1 << 30) + 1, 1))
+    hist.copy_(torch.randint(0, V, (3, 1000), device=gpu, dtype=torch.int32))
+    h = ps.History(hist, torch.full((3,), 1000, dtype=torch.int32, device=gpu))
+    few = torch.randn(3, V, device=gpu)
+    out = ps.adjust(few, V, h, presence=1.0)
+    met = torch.zeros(3, V, dtype=torch.bool, device=gpu).scatter_(1, hist.long(), True)
+    assert torch.equal(out, torch.where(met, (few.double() - 1.0).float(), few))
+    del far, hist, h
+    tok = torch.arange(B, dtype=torch.int32, device=gpu).view(B, 1)
+    ps.adjust(z, V, ps.History(tok, torch.ones(B, dtype=torch.int32, device=gpu)), presence=2.0, out=z)
+    for r, row in zip(some, rows):
+        want = row.clone()
+        want[r] = (row[r].double() - 2.0).bfloat16()
+        assert torch.equal(z[r], want)
+    assert int((z == -2.0).sum()) >= B - 4 - int((rows == -2.0).sum())
+    g = torch.ones((B, V), dtype=torch.bfloat16, device=gpu)
+    ps.adjust_grad(g, z, V, ps.History(tok, torch.ones(B, dtype=torch.int32, device=gpu)), repetition=2.0, out=g)
+    assert int((g != 1.0).sum()) == B and bool((g[torch.arange(B, device=gpu), torch.arange(B, device=gpu)] != 1.0).all())
+
+
 def test_nothing_to_adjust(gpu, ps):
     print("[case] adjust nothing", flush=True)
     z = torch.randn(3, 777, device=gpu)
@@ -328,7 +357,7 @@ def test_refusals(gpu, ps):
            dict(hist=ps.History(hist.tok, hist.length[:2])), dict(hist=ps.History(hist.tok.cpu(), hist.length)), dict(hist=ps.History(hist.tok, hist.length, i32(1))),
            dict(hist=ps.History(torch.zeros((9, 3), dtype=torch.int32, device=gpu).t(), hist.length)), dict(hist=ps.History(hist.tok[:1].expand(3, 9), hist.length)),
            dict(repetition=torch.ones(2, device=gpu)), dict(repetition=torch.ones(3, device=gpu, dtype=torch.float64)), dict(repetition=torch.ones(3)), dict(repetition=0.0), dict(presence=float("nan")),
-           dict(mask=words[:2]), dict(mask=words[:, :3]), dict(mask=words.long()), dict(mask=words, mask_row=i32(0, 1)), dict(mask_row=i32(0, 1, 2)), dict(draft_tok=i32(1)),
+           dict(mask=words[:2]), dict(mask=words[:0]), dict(mask=words[:, :3]), dict(mask=words.long()), dict(mask=words, mask_row=i32(0, 1)), dict(mask_row=i32(0, 1, 2)), dict(draft_tok=i32(1)),
            dict(seq_off=i32(0, 1, 2), draft_tok=i32(1, 2)), dict(seq_off=i32(0, 1, 2).long(), draft_tok=i32(1)), dict(bias=ps.Bias(i32(0, 0, 0), i32(), torch.zeros(0, device=gpu))),
            dict(bias=ps.Bias(i32(0, 0, 0, 1), i32(1), torch.zeros(2, device=gpu))), dict(out=torch.zeros(3, 99, device=gpu)), dict(out=torch.zeros(2, 100, device=gpu)), dict(out=torch.zeros(3, 100)),
            dict(out=torch.zeros(100, 3, device=gpu).t())]

@@ -104,6 +104,26 @@ def test_large_and_small_values(gpu, ps):
         assert all(x == then or (math.isnan(then) and math.isnan(x)) for x in h.tolist() + g.tolist()[:7]) and math.isnan(g[7].item())
 
 
+def test_without_a_limit_nothing_is_scaled(gpu, ps):
+    print("[case] clip without a limit", flush=True)
+    g, to = torch.randn(5000, device=gpu), torch.zeros(5000, device=gpu)
+    g[3] = float("inf")
+    assert ps.clip_grad([g], float("inf"), [to]).item() == float("inf") and torch.equal(g, to)
+
+
+def test_more_than_32_bits_of_elements(gpu, ps):
+    print("[case] clip large offsets", flush=True)
+    n = (1 << 31) + 5000
+    g = torch.full((n,), 2.0 ** -10, dtype=torch.bfloat16, device=gpu)
+    h = torch.ones(7, device=gpu)
+    want = math.sqrt(n * 2.0 ** -20 + 7)
+    assert abs(ps.clip_grad([g, h], 2.0 ** -10).item() - want) <= want * 2.0 ** -24 * (1 + 2.0 ** -10)
+    ref = 2.0 ** -20 / (want + 1e-6)
+    for part in (g[:9], g[n // 2:n // 2 + 9], g[-9:]):
+        assert bool(((part.double() - ref).abs() <= OFF[torch.bfloat16] * ref).all())
+    assert bool((g == g[0]).all())
+
+
 def test_the_same_bits_every_time(gpu, ps):
     print("[case] clip twice", flush=True)
     grads = _grads(gpu, SHAPES["odd"] + SHAPES["large"])

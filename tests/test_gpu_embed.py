@@ -1,7 +1,7 @@
 """picospec_embed and picospec_embed_grad against the sums in 64 bits.
 
-The gradient's sums are formed in fp32, at most 2 * 64 - 1 rows behind each other in a piece and the pieces of a token behind each other, so a sum of k rows is off by at most
-(min(k, 127) + k / 64) 2^-24 of the sum of absolute values; the factor rounds once more, the result to the table's type once (an added table: the sum with it, too)."""
+The gradient's sums are formed in fp32: k rows behind each other, or (k of 64 and more, tokens of more than 1024 positions in all) in pieces of 32 and up to k / 128 rows, at most 128 of them, or
+in up to 32 parts.  So a sum of k rows is off by less than (min(k, 127) + k / 64) 2^-24 of the sum of absolute values; the factor rounds once more, the result to the table's type once (an added table: the sum with it, too)."""
 import pytest
 import torch
 
@@ -112,6 +112,44 @@ def test_embed_grad(gpu, ps, n, V, d, how, dtype, out_dtype):
     out = ps.embed_grad(grad, tok, V, scale, out=old.clone(), accumulate=True)
     assert bool(((out.double() - s).abs() <= bound).all())
     assert torch.equal(out[(k == 0)[:, 0]], old[(k == 0)[:, 0]])
+
+
+def test_more_than_32_bits_of_elements(gpu, ps):
+    print("[case] embed large offsets", flush=True)
+    V, d = 1 << 20, 2100
+    table = torch.zeros((V, d), dtype=torch.bfloat16, device=gpu)
+    ids = torch.tensor([0, V - 1, V // 2, V - 2, -1, V, 1], dtype=torch.int32, device=gpu)
+    rows = torch.randn(7, d, device=gpu).bfloat16()
+    there = torch.tensor([0, 1, 2, 3, 6], device=gpu)
+    table[ids[there].long()] = rows[there]
+    want = rows.clone()
+    want[4:6] = 0
+    assert torch.equal(ps.embed(table, ids), want)
+    for n in (7, 3000):                                       # (few positions, and many)
+        tok = torch.full((n,), -1, dtype=torch.int32, device=gpu)
+        tok[-7:] = ids
+        g = torch.zeros((n, d), dtype=torch.bfloat16, device=gpu)
+        g[-7:] = rows
+        table.fill_(5.0)
+        ps.embed_grad(g, tok, V, out=table)
+        assert torch.equal(table[ids[there].long()], rows[there]) and int((table != 0).any(1).sum()) == 5
+    wide = torch.randn((1100000, 2000), device=gpu).bfloat16()          # (and of rows)
+    tok = torch.full((wide.shape[0],), 3, dtype=torch.int32, device=gpu)
+    tok[:-2] = -1
+    got = ps.embed_grad(wide, tok, 9, out=torch.empty((9, 2000), device=gpu))
+    assert torch.equal(got[3], wide[-2].float() + wide[-1].float()) and int((got != 0).any(1).sum()) == 1
+
+
+@pytest.mark.parametrize("V", [255, 256, 257, 262144, 262145, 1 << 20])
+def test_vocabularies_around_the_sorts_shares(gpu, ps, V):
+    print(f"[case] embed_grad V {V}", flush=True)
+    g = torch.Generator(device=gpu).manual_seed(V)
+    tok = torch.randint(0, V, (3000,), device=gpu, generator=g, dtype=torch.int32)
+    tok[::3] = V - 1
+    grad = torch.randn((3000, 9), device=gpu, generator=g)
+    s, bound, k = _expect(grad, tok, V, 1.0)
+    out = ps.embed_grad(grad, tok, V)
+    assert bool(((out.double() - s).abs() <= bound + HALF[torch.float32] * (s.abs() + bound)).all()) and bool((out[(k == 0)[:, 0]] == 0).all())
 
 
 def test_embed_grad_of_nothing(gpu, ps):

@@ -38,7 +38,8 @@ def test_adjust_refuses(B, kw):
     assert _adjust(B, **kw) == B.EINVAL
 
 
-@pytest.mark.parametrize("kw", BAD_ROWS + [dict(grad=None), dict(ld_g=99), dict(out=FAKE * 2), dict(out=FAKE + 4), dict(out=FAKE, ld_out=101)])
+@pytest.mark.parametrize("kw", BAD_ROWS + [dict(grad=None), dict(ld_g=99), dict(out=FAKE * 2), dict(out=FAKE + 4), dict(out=FAKE, ld_out=101),
+                                           dict(grad=FAKE, logits=FAKE, ld=120, out=FAKE)])
 def test_adjust_grad_refuses(B, kw):
     assert _adjust_grad(B, **kw) == B.EINVAL
 
@@ -95,7 +96,7 @@ def _clip(B, ptrs=(FAKE, FAKE + 4096), numel=(8, 8), dtypes=(0, 1), outs=None, m
     return B.lib.picospec_clip_grad(k if n is None else n, p, o, (C.c_int64 * k)(*numel), (C.c_int32 * k)(*dtypes), max_norm, norm, ws, ws_bytes, None)
 
 
-@pytest.mark.parametrize("kw", [dict(n=-1), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(norm=None), dict(norm=FAR + 2), dict(numel=(8, -1)), dict(ptrs=(FAKE, None)),
+@pytest.mark.parametrize("kw", [dict(n=-1), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(norm=None), dict(norm=FAR + 2), dict(numel=(8, -1)), dict(numel=(8, 1 << 45)), dict(ptrs=(FAKE, None)),
                                 dict(ptrs=(FAKE + 2, FAKE + 4096)), dict(ptrs=(FAKE, FAKE)), dict(ptrs=(FAKE, FAKE + 31), dtypes=(0, 1)), dict(ptrs=(FAKE + 28, FAKE), dtypes=(0, 0)),
                                 dict(outs=(FAKE, None)), dict(outs=(FAKE + 4, FAKE + 4096)), dict(outs=(FAR, FAR + 16)), dict(outs=(FAKE + 4096, FAKE))])
 def test_clip_refuses(B, kw):
