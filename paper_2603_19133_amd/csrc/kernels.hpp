@@ -496,7 +496,7 @@ hipError_t launch_embed(const void* table, int dtype, int64_t ld, int V, int64_t
 // The gradient's workspace: where each token's positions begin and how many they are, positions and tokens in that order, the tokens of the pieces, words to arrive at, the pieces' sums.
 // Up to kFewTokens positions need none of it.
 constexpr int kSortThreads = 1024, kSortList = 256, kSortLds = 64 * 1024, kPiece = 32, kPiecesMost = 128, kFewTokens = 1024;
-constexpr int kTokensMost = 8, kTilesMost = 8;                    // tokens of a workgroup that writes zeros, workgroups that share a row
+constexpr int kTokensMost = 64, kTilesMost = 8;                   // tokens of a workgroup that writes zeros, workgroups that share a row
 constexpr int64_t kEmbedMostTokens = 1 << 26;
 // Workgroups of the sort: 256, more where a workgroup's tokens would be more than its threads
 inline int embed_owners_log2(int V) { int l = 8; while (((V + (1 << l) - 1) >> l) > kSortLds / (kSortThreads / 64 * 4)) ++l; return l; }
