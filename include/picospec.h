@@ -87,7 +87,7 @@ enum {
     PICOSPEC_EWORKSPACE = -2,  /* a workspace was given that is smaller than picospec_workspace_bytes() says, or misaligned */
     PICOSPEC_EDTYPE = -3,      /* dtype is neither PICOSPEC_F32 nor PICOSPEC_BF16 */
     PICOSPEC_EHIP = -4,        /* a HIP runtime call (launch, attribute) failed */
-    PICOSPEC_EUNSUPPORTED = -5,/* k or V beyond the limits reported by picospec_limit() */
+    PICOSPEC_EUNSUPPORTED = -5,/* k or V beyond the limits reported by picospec_limit(), or a call larger than a launch can be */
     PICOSPEC_ESCRATCH = -6     /* picospec_verify_sample_static: the rows' segment table exceeds the library's fixed array */
 };
 

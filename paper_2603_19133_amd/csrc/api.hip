@@ -605,6 +605,7 @@ int check_adjust(const void* src, int64_t ld_src, const void* logits, int dtype,
     if (B < 0 || n_draft < 0 || ld_src < V || ld_out < V) return PICOSPEC_EINVAL;
     if (seq_off ? n_rows != n_draft && (int64_t)n_rows != (int64_t)n_draft + B : n_rows != B || n_draft != 0) return PICOSPEC_EINVAL;
     if (n_rows == 0) return PICOSPEC_OK;
+    if (B == 0) return PICOSPEC_EINVAL;                           // (drafted rows of no sequence)
     if (!src || !out || (uintptr_t)src % esize(dtype) || (uintptr_t)out % esize(dtype)) return PICOSPEC_EINVAL;
     if (n_draft > 0 && !draft_tok) return PICOSPEC_EINVAL;
     if (hist_tok && (!hist_len || hist_cap < 0 || ld_hist < hist_cap)) return PICOSPEC_EINVAL;
@@ -832,6 +833,7 @@ size_t picospec_scratch_bytes(int which_call, int dtype, int32_t n_draft, int32_
             return (round_seg_table_bytes(dtype, rows, V) + 15) / 16 * 16 + split_scratch_bytes(dtype, n_draft, V, k);
         }
         case PICOSPEC_CALL_SAMPLE: return sample_scratch_bytes(dtype, n_draft, V);
+        case PICOSPEC_CALL_EMBED_GRAD: case PICOSPEC_CALL_CLIP_GRAD: return picospec_workspace_bytes(which_call, dtype, n_draft, V, k);
         case PICOSPEC_CALL_DISTILL: return distill_scratch_bytes(dtype, n_draft, V);
         default: return 0;
     }
@@ -892,7 +894,7 @@ const char* picospec_strerror(int code)
         case PICOSPEC_EWORKSPACE: return "workspace smaller than picospec_workspace_bytes() or not on a 16-byte boundary";
         case PICOSPEC_EDTYPE: return "dtype must be PICOSPEC_F32 or PICOSPEC_BF16";
         case PICOSPEC_EHIP: return "HIP runtime call failed";
-        case PICOSPEC_EUNSUPPORTED: return "k or V exceeds picospec_limit()";
+        case PICOSPEC_EUNSUPPORTED: return "k or V exceeds picospec_limit(), or a call is larger than a launch can be";
         case PICOSPEC_ESCRATCH: return "the target rows' segment table exceeds the fixed array of picospec_verify_sample_static (picospec_static_scratch_bytes())";
         default: return "unknown picospec error code";
     }

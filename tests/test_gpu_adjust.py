@@ -179,6 +179,10 @@ CASES = {
     "lengths off the buffer": dict(seed=13, V=500, dtype=torch.float32, gammas=[0] * 3, lengths=[-5, 1000, 2 ** 31 - 1]),
     "numbers": dict(seed=14, V=50001, dtype=torch.bfloat16, gammas=[1] * 9, mixed=False, cap=700, masks=5, pad=2),
     "many sequences": dict(seed=15, V=5000, dtype=torch.float32, gammas=[i % 4 for i in range(700)], cap=20, masks=9, bias=3),
+    "many bf16": dict(seed=17, V=20001, dtype=torch.bfloat16, gammas=[0] * 300, cap=30, masks=9, bias=3, pad=1),
+    "shared out": dict(seed=18, V=33000, dtype=torch.bfloat16, gammas=[9, 12, 5, 16, 0, 9] * 14, cap=300, masks=9, token_range=3000),
+    "long histories": dict(seed=19, V=140001, dtype=torch.float32, gammas=[0] * 60, cap=2500, masks=3, bias=40),
+    "long histories bf16": dict(seed=20, V=140001, dtype=torch.bfloat16, gammas=[0] * 60, cap=4500, masks=3, bias=40, pad=3),
     "long drafts": dict(seed=16, V=3001, dtype=torch.bfloat16, gammas=[200, 1], token_range=40),
 }
 

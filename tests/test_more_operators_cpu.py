@@ -27,7 +27,7 @@ def _adjust_grad(B, grad=FAKE, ld_g=100, logits=FAKE * 2, dtype=0, ld=100, rows=
 
 
 BAD_ROWS = [dict(rows=-1), dict(V=0), dict(ld=99), dict(ld_out=99), dict(logits=None), dict(out=None), dict(out=FAR + 2), dict(seqs=3), dict(seqs=-1), dict(n_draft=1),
-            dict(seq_off=FAKE, n_draft=3), dict(seq_off=FAKE, n_draft=2, seqs=1), dict(seq_off=FAKE, n_draft=-1, seqs=1),
+            dict(seq_off=FAKE, n_draft=3), dict(seq_off=FAKE, n_draft=2, seqs=1), dict(seq_off=FAKE, n_draft=-1, seqs=1), dict(seq_off=FAKE, n_draft=2, seqs=0, draft=FAKE),
             dict(length=None), dict(cap=9), dict(cap=-1), dict(rep=0.0), dict(rep=float("nan")), dict(rep=float("inf")), dict(rep=-1.0),
             dict(mask=FAKE, ld_mask=3), dict(mask=FAKE, masks=1), dict(mask=FAKE, masks=-1, mask_row=FAKE)]
 
@@ -87,6 +87,7 @@ def test_embed_refuses_types_sizes_and_workspaces(B):
     # (a token's pieces have a row of sums each)
     assert B.workspace_bytes(B.CALL_EMBED_GRAD, B.BF16, 1 << 20, 1 << 20, 4096) >= (1 << 20) // 64 * 4096 * 4
     assert B.workspace_bytes(B.CALL_EMBED_GRAD, B.F32, 4, 10, 0) == 0
+    assert B.scratch_bytes(B.CALL_EMBED_GRAD, B.F32, 1025, 0, 10, 8) == need
 
 
 def _clip(B, ptrs=(FAKE, FAKE + 4096), numel=(8, 8), dtypes=(0, 1), outs=None, max_norm=1.0, norm=FAR, ws=FAKE, ws_bytes=1 << 20, n=None):
