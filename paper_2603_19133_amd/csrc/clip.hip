@@ -35,8 +35,8 @@ __device__ __forceinline__ double block_sum(double v)
 }
 
 // f(tensor, first element, end, block) for the blocks blockIdx.x, blockIdx.x + gridDim.x, .. of the launch's tensors (c.block elements each, a tensor's last one shorter), ascending or descending
-template <class F>
-__device__ __forceinline__ void each_block(const ClipTensors& c, bool down, F f)
+template <int MOST, class F>
+__device__ __forceinline__ void each_block(const ClipList<MOST>& c, bool down, F f)
 {
     const int64_t blocks = c.first[c.n], here = blockIdx.x, step = gridDim.x;
     if (here >= blocks) return;
@@ -85,7 +85,8 @@ __device__ __forceinline__ double block_squares(const char* g, int64_t begin, in
     return s;
 }
 
-__global__ __launch_bounds__(kCT) void clip_norm_kernel(const ClipTensors c, double* partial)
+template <int MOST>
+__global__ __launch_bounds__(kCT) void clip_norm_kernel(const ClipList<MOST> c, double* partial)
 {
     double s = 0.0;
     each_block(c, false, [&](int t, int64_t begin, int64_t end, int64_t k) {
@@ -129,7 +130,8 @@ __device__ __forceinline__ void block_scale(const char* g, char* out, int64_t be
     for (; x < end; x += STEP) store_row_vec<BF16>(out, x, end, scaled<BF16>(load_row_vec<BF16>(g, x, end), by));
 }
 
-__global__ __launch_bounds__(kCT) void clip_scale_kernel(const ClipTensors c, const double* partial, int partials, float max_norm, float* norm_out)
+template <int MOST>
+__global__ __launch_bounds__(kCT) void clip_scale_kernel(const ClipList<MOST> c, const double* partial, int partials, float max_norm, float* norm_out)
 {
     double s = 0.0;
     for (int i = threadIdx.x; i < partials; i += kCT) s += partial[i];
@@ -145,18 +147,35 @@ __global__ __launch_bounds__(kCT) void clip_scale_kernel(const ClipTensors c, co
     });
 }
 
+// f(list) with a short list where that holds the tensors: the host pays half a microsecond for a kilobyte of arguments (two tensors 12.7 us a call with the long one, 9.1 so; lists of 64 gained nothing)
+template <class F>
+hipError_t with_list(const ClipTensors& c, F f)
+{
+    if (c.n <= kClipFew) {
+        ClipList<kClipFew> few;                                   // (read as far as it is filled)
+        std::copy_n(c.grad, c.n, few.grad);
+        std::copy_n(c.out, c.n, few.out);
+        std::copy_n(c.numel, c.n, few.numel);
+        std::copy_n(c.first, c.n + 1, few.first);
+        std::copy_n(c.bf16, c.n, few.bf16);
+        few.n = c.n; few.block = c.block; few.stream = c.stream; few.in_place = c.in_place;
+        f(few);
+    } else {
+        f(c);
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_clip_norm(const ClipTensors& c, double* partial, int groups, hipStream_t stream)
 {
-    hipLaunchKernelGGL(clip_norm_kernel, dim3((unsigned)groups), dim3(kCT), 0, stream, c, partial);
-    return hipGetLastError();
+    return with_list(c, [&](const auto& list) { clip_norm_kernel<<<dim3((unsigned)groups), dim3(kCT), 0, stream>>>(list, partial); });
 }
 
 hipError_t launch_clip_scale(const ClipTensors& c, const double* partial, int partials, float max_norm, float* norm, int groups, hipStream_t stream)
 {
-    hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)groups), dim3(kCT), 0, stream, c, partial, partials, max_norm, norm);
-    return hipGetLastError();
+    return with_list(c, [&](const auto& list) { clip_scale_kernel<<<dim3((unsigned)groups), dim3(kCT), 0, stream>>>(list, partial, partials, max_norm, norm); });
 }
 
 }  // namespace picospec

@@ -527,17 +527,19 @@ struct EmbedGradArgs {
 hipError_t launch_embed_grad(EmbedGradArgs a, int dtype, int out_dtype, const int32_t* tok, int n, void* workspace, hipStream_t stream);
 
 // ---- the norm over many tensors and their clipping (csrc/clip.hip): the tensors of one launch, as a kernel argument
-constexpr int kClipTensors = 128, kClipGroups = 2048;             // tensors and workgroups of a launch
-struct ClipTensors {
-    const void* grad[kClipTensors];
-    void* out[kClipTensors];
-    int64_t numel[kClipTensors];
-    uint32_t first[kClipTensors + 1];                             // blocks in front of each tensor, and all of them
-    uint8_t bf16[kClipTensors];
+constexpr int kClipTensors = 128, kClipFew = 16, kClipGroups = 2048;       // tensors of a launch (of a short list), workgroups
+template <int MOST>
+struct ClipList {
+    const void* grad[MOST];
+    void* out[MOST];
+    int64_t numel[MOST];
+    uint32_t first[MOST + 1];                                     // blocks in front of each tensor, and all of them
+    uint8_t bf16[MOST];
     int n, block;                                                 // block: elements that a workgroup takes at a time
     uint32_t stream;                                              // blocks whose loads for the norm pass by the caches: those that the second pass would not find there
     int in_place;                                                 // whether every output is its tensor
 };
+using ClipTensors = ClipList<kClipTensors>;
 // Elements that a workgroup takes at a time: the same number of blocks for each, of up to 16,384 elements
 inline int clip_block(int64_t elements) {
     const int64_t trips = (elements + kClipGroups * 16384ll - 1) / (kClipGroups * 16384ll);
