@@ -42,7 +42,7 @@ class Case:
         rows = sum(gammas) + (B if target else 0)
         self.rows = rows
         z = torch.randn((rows, V + pad), generator=g) * 4
-        if values is not None:
+        if values is not None and z.numel():
             z.view(-1)[torch.randint(0, max(1, z.numel()), (z.numel() // 5 + 1,), generator=g)] = torch.tensor([r.choice(values) for _ in range(z.numel() // 5 + 1)])
         self.z = z.to(dtype)[:, :V]
         self.grad = (torch.randn((rows, V), generator=g) * 1e-3).to(dtype)
