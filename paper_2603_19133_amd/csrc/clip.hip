@@ -77,9 +77,18 @@ __device__ __forceinline__ double block_squares(const char* g, int64_t begin, in
             s += squares(f);
         }
     }
-    for (; x < end; x += STEP) {
+    // (what is left together, too: 203 million bf16, 7 vectors a thread and block, 87 us with 3 of them behind each other, 81)
+    if (x >= end) return s;
+    uint4 raw[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+        raw[j] = make_uint4(0, 0, 0, 0);
+        if (x + j * STEP < end) raw[j] = load_row_vec<BF16>(g, x + j * STEP, end);
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
         float f[N];
-        unpack<BF16>(load_row_vec<BF16>(g, x, end), f);
+        unpack<BF16>(raw[j], f);
         s += squares(f);
     }
     return s;
@@ -127,7 +136,14 @@ __device__ __forceinline__ void block_scale(const char* g, char* out, int64_t be
             __builtin_nontemporal_store(u32x4_t{r.x, r.y, r.z, r.w}, reinterpret_cast<loose_t*>(out + (x + j * STEP) * ESZ));
         }
     }
-    for (; x < end; x += STEP) store_row_vec<BF16>(out, x, end, scaled<BF16>(load_row_vec<BF16>(g, x, end), by));
+    if (x >= end) return;
+    uint4 raw[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+        if (x + j * STEP < end) raw[j] = load_row_vec<BF16>(g, x + j * STEP, end);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+        if (x + j * STEP < end) store_row_vec<BF16, true>(out, x + j * STEP, end, scaled<BF16>(raw[j], by));
 }
 
 template <int MOST>
