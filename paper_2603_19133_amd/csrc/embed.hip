@@ -232,6 +232,28 @@ __device__ __forceinline__ void write_sums(char* row, int64_t x, int64_t d, floa
     }
 }
 
+// Zeros for the rows row0 .. row0 + rows - 1 (up to 64) of the table but those with a bit in `kept`, by the workgroup; rows that lie without gaps as one stretch
+template <bool OUT16>
+__device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, int64_t row0, int rows, unsigned long long kept)
+{
+    constexpr int M = Vec<OUT16>::N, ESZ = OUT16 ? 2 : 4;
+    const int tid = threadIdx.x;
+    for (int r = 0; r < rows;) {
+        if (kept >> r & 1ull) { ++r; continue; }
+        const unsigned long long next = kept >> r;
+        const int end = a.ld_out != a.d ? r + 1 : min(rows, next ? r + (int)__builtin_ctzll(next) : rows);
+        char* const to = (char*)a.out + (row0 + r) * a.ld_out * ESZ;
+        const int64_t total = (end - r) * a.d;
+        const int head = (int)min<int64_t>((16 - ((uintptr_t)to & 15)) % 16 / ESZ, total);
+        if (tid < head) {
+            if constexpr (OUT16) reinterpret_cast<uint16_t*>(to)[tid] = 0;
+            else reinterpret_cast<float*>(to)[tid] = 0.f;
+        }
+        for (int64_t x = head + (int64_t)tid * M; x < total; x += (int64_t)kRowThreads * M) store_row_vec<OUT16>(to, x, total, make_uint4(0, 0, 0, 0));
+        r = end;
+    }
+}
+
 // The table's rows.  The workgroups in front take the pieces of the tokens that occur most, one each, and the last piece of a token to be done adds its pieces up; those behind them the
 // other tokens that occur, by their positions; the rest writes zeros.  In this order: rows that are read beside a stream of writes come at the rate of a copy, the zeros alone
 // at that of a fill.
@@ -334,7 +356,19 @@ __global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(const EmbedGradA
         return;
     }
     // zeros for the tokens that do not occur
-    const int before = (a.slots + a.windows) * a.tiles, groups = (int)gridDim.x - before, group = (int)blockIdx.x - before, tokens = (a.V - group + groups - 1) / groups;
+    const int before = (a.slots + a.windows) * a.tiles, groups = (int)gridDim.x - before, group = (int)blockIdx.x - before;
+    if (a.together) {
+        const int rows = (a.V + groups - 1) / groups, row0 = group * rows, here = min(rows, a.V - row0);
+        __shared__ unsigned long long kept;
+        if (tid < kWave) {
+            const unsigned long long some = __ballot(tid < here && a.info[row0 + tid].y != 0);
+            if (tid == 0) kept = some;
+        }
+        __syncthreads();
+        zero_rows<OUT16>(a, row0, here, kept);
+        return;
+    }
+    const int tokens = (a.V - group + groups - 1) / groups;
     if (tid < tokens) info[tid] = a.info[group + tid * groups];
     __syncthreads();
     for (int k = sub; k < tokens; k += per) {
@@ -356,10 +390,13 @@ __global__ __launch_bounds__(kRowThreads) void embed_few_kernel(const EmbedGradA
     const int tid = threadIdx.x, per = kRowThreads >> a.share, sub = tid >> a.share;
     const int64_t x0 = (int64_t)(tid & ((1 << a.share) - 1)) * N, step = (int64_t)N << a.share;
     const int group = blockIdx.x, groups = 1 << groups_log2, tokens = (a.V - group + groups - 1) >> groups_log2;
-    if (tid == 0) how_many = 0;
+    const int rows_here = (a.V + (int)gridDim.x - 1) / (int)gridDim.x, row0 = group * rows_here;      // a.together: the rows that it zeroes
+    __shared__ unsigned long long kept;
+    if (tid == 0) { how_many = 0; kept = 0ull; }
     __syncthreads();
     for (int i = tid; i < n; i += kRowThreads) {
         const int t = tok[i];
+        if (a.together && (unsigned)t - (unsigned)row0 < (unsigned)rows_here) atomicOr(&kept, 1ull << (t - row0));
         if ((unsigned)t < (unsigned)a.V && (t & (groups - 1)) == group) found[atomicAdd(&how_many, 1)] = (uint32_t)(t >> groups_log2) << 16 | (uint32_t)i;
     }
     __syncthreads();
@@ -404,7 +441,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_few_kernel(const EmbedGradA
     }
     for (int k = sub; k < tokens; k += per) {
         const int p0 = first[k], p1 = first[k + 1];
-        if ((a.accumulate && p0 == p1) || (per > 1 && p1 - p0 > kFewRows)) continue;
+        if (((a.accumulate || a.together) && p0 == p1) || (per > 1 && p1 - p0 > kFewRows)) continue;
         char* const row = (char*)a.out + (int64_t)(group + (k << groups_log2)) * a.ld_out * (OUT16 ? 2 : 4);
         for (int64_t x = x0; x < a.d; x += step) {
             float sum[N] = {};
@@ -412,6 +449,7 @@ __global__ __launch_bounds__(kRowThreads) void embed_few_kernel(const EmbedGradA
             write_sums<OUT16, N>(row, x, a.d, sum, a.scale, a.accumulate);
         }
     }
+    if (a.together && !a.accumulate) zero_rows<OUT16>(a, row0, min(rows_here, a.V - row0), kept);
 }
 
 // Workgroups that write the table's rows: 20 KB each, but 8 to kTokensMost rows, and no fewer than 2048 of them (116,340 rows of 320 fp32, 149 MB, 8 rows each 32 us, 16 27.8; of 512 33.8, 34.3, of 4 KB
@@ -422,6 +460,11 @@ template <bool OUT16> int row_groups(const EmbedGradArgs& a)
     return std::max((a.V + rows - 1) / rows, std::min(a.V, 2048));
 }
 
+// Whether a workgroup zeroes rows that stand together, as one stretch where they lie without gaps, rather than every so many-th row.  us, apart / together: rows whose ends share a line with the
+// next one's, which another workgroup writes (126,730 x 1124 fp32 135 / 108, 120,000 x 333 bf16 31 / 22), or leave lanes without work (116,340 x 320 fp32 30 / 25); but stretches that
+// begin whole pages apart meet in the same channels of the memory (100,000 x 4096 bf16 146 / 157, x 2048 72 / 79).
+template <bool OUT16> int together(const EmbedGradArgs& a) { return a.ld_out * (OUT16 ? 2 : 4) % 4096 != 0; }
+
 template <bool BF16, bool OUT16>
 hipError_t launch_sums(EmbedGradArgs a, int n, hipStream_t stream)
 {
@@ -430,6 +473,7 @@ hipError_t launch_sums(EmbedGradArgs a, int n, hipStream_t stream)
     a.windows = ((n + kPiece - 1) / kPiece + per - 1) / per;
     a.tiles = (int)std::min<int64_t>((a.d + kRowThreads * Vec<BF16>::N - 1) / (kRowThreads * Vec<BF16>::N), kTilesMost);
     const int groups = a.accumulate ? 0 : row_groups<OUT16>(a);
+    a.together = together<OUT16>(a);
     hipLaunchKernelGGL((embed_sum_kernel<BF16, OUT16>), dim3((unsigned)((a.slots + a.windows) * a.tiles + groups)), dim3(kRowThreads), 0, stream, a);
     return hipGetLastError();
 }
@@ -438,6 +482,7 @@ template <bool BF16, bool OUT16>
 hipError_t launch_few(EmbedGradArgs a, const int32_t* tok, int n, hipStream_t stream)
 {
     a.share = row_threads_log2<BF16>(a.d);
+    a.together = together<OUT16>(a);
     int log2 = 0;
     while ((1 << log2) < row_groups<OUT16>(a)) ++log2;
     const dim3 grid((unsigned)std::min(1 << log2, a.V));

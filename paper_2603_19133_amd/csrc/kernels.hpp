@@ -522,7 +522,7 @@ struct EmbedGradArgs {
     void* out; int64_t ld_out; int V;
     float scale; int accumulate;
     const int2 *info, *order; const int32_t* slot_tok; uint32_t* arrived; float* partial; int64_t d_pad;
-    int slots, windows, tiles, share;
+    int slots, windows, tiles, share, together;
 };
 hipError_t launch_embed_grad(EmbedGradArgs a, int dtype, int out_dtype, const int32_t* tok, int n, void* workspace, hipStream_t stream);
 
