@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kRowThreads = 256;                                  // of a workgroup that moves rows
 constexpr int kFewRows = 8;                                       // of a token, that one group of threads adds up
+constexpr int kChain = 32;                                        // rows of a token in a chain of additions, where all of them may be one thread's
 
 // true in the last of `total` workgroups that arrive at a word that was 0 at the kernel's start.  What they hand over went by put_shared (see there).
 __device__ __forceinline__ bool arrived_last(uint32_t* word, unsigned total)
@@ -168,13 +169,16 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
     }
 }
 
-// sum += rows at(p0) .. at(p1 - 1), elements x .. x + N - 1, eight rows under way at a time.  FAR: the places lie in memory, and the next eight are read beside the rows (32,768 rows for one token
-// 196 -> 156 us; where they lie in LDS the registers cost more)
+// sum = rows at(p0) .. at(p1 - 1), elements x .. x + N - 1, added up, eight rows under way at a time (sum: zeros).  FAR: the places lie in memory, and the next eight are read beside the rows (32,768 rows for one token
+// 196 -> 156 us; where they lie in LDS the registers cost more).  Where they lie in LDS the rows may be all of a token's, up to kFewTokens: every kChain of them are added up
+// apart, so that no element goes through more than 2 kChain additions (rows behind each other in one chain were off by as many roundings as there are rows).
 template <bool BF16, bool FAR, class At>
 __device__ __forceinline__ void add_rows(const char* g, int64_t ld, int64_t d, At at, int p0, int p1, int64_t x, float (&sum)[Vec<BF16>::N])
 {
     constexpr int N = Vec<BF16>::N, ESZ = BF16 ? 2 : 4, AHEAD = 8;
+    static_assert(kChain % AHEAD == 0 && kChain * kChain >= kFewTokens, "a chain of chains");
     int i[AHEAD];
+    float chains[N] = {};
     auto places = [&](int p) {
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) i[j] = p + j < p1 ? at(p + j) : 0;
@@ -196,6 +200,14 @@ __device__ __forceinline__ void add_rows(const char* g, int64_t ld, int64_t d, A
 #pragma unroll
             for (int e = 0; e < N; ++e) sum[e] += f[e];
         }
+        if (!FAR && (p - p0) % kChain == kChain - AHEAD) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) { chains[e] += sum[e]; sum[e] = 0.f; }
+        }
+    }
+    if (!FAR && p1 - p0 > kChain - AHEAD) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += chains[e];
     }
 }
 
