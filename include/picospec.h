@@ -496,7 +496,8 @@ int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_r
  *   z <- z - frequency c - presence                (tokens with c > 0)
  *   z <- z + bias                                  (tokens of the sequence's list)
  *   z <- -inf                                      (tokens that the row's mask does not allow)
- * formed in 64 bits and rounded to the rows' type; tokens that none of it touches keep their bits, NaN among them.
+ * formed in 64 bits and rounded to the rows' type; tokens that none of it touches keep their bits, NaN among them.  seq_off ascends; rows that no sequence has, because it begins above 0 or ends
+ * before n_draft (a batch that is padded), are left as they are.
  *   logits [n_rows, ld], out [n_rows, ld_out]: out may be the logits themselves (same pointer and stride; what does not change is not written then), else may not overlap them
  *   draft_tok [n_draft]                                                                                      in
  *   hist_tok [B, ld_hist], hist_len [B], prompt_len [B]: the first hist_len[b] tokens of row b (clamped to 0..hist_cap <= ld_hist) are the history, the first prompt_len[b] of them
@@ -528,6 +529,25 @@ int picospec_adjust_grad(const void* grad, int64_t ld_grad, const void* logits, 
                          float repetition, const float* repetition_rows,
                          const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
                          void* out, int64_t ld_out, void* stream);
+
+/*
+ * The same two calls for an `out` whose memory holds nothing yet: rows that no sequence has (in front of seq_off[0], behind the last sequence) are zeros in it.  picospec_adjust and
+ * picospec_adjust_grad leave such rows as they are.  out may not be the rows that are read.
+ */
+int picospec_adjust_whole(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                          int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                          const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len, const int32_t* prompt_len,
+                          float repetition, float presence, float frequency,
+                          const float* repetition_rows, const float* presence_rows, const float* frequency_rows,
+                          const int32_t* bias_off, const int32_t* bias_id, const float* bias_value, int32_t n_bias,
+                          const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                          void* out, int64_t ld_out, void* stream);
+int picospec_adjust_grad_whole(const void* grad, int64_t ld_grad, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                               int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                               const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len,
+                               float repetition, const float* repetition_rows,
+                               const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                               void* out, int64_t ld_out, void* stream);
 
 /*
  * Token embeddings, what a drafter reads its tokens by: out[i] = scale * table[tok[i]], rounded once (scale 1: the rows' bits); zeros where tok[i] is outside

@@ -38,7 +38,7 @@ EXPORTS = ("picospec_round", "picospec_verify_sample", "picospec_verify_sample_s
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
            "picospec_sample", "picospec_distill", "picospec_distill_grad",
-           "picospec_adjust", "picospec_adjust_grad", "picospec_embed", "picospec_embed_grad", "picospec_clip_grad",
+           "picospec_adjust", "picospec_adjust_grad", "picospec_adjust_whole", "picospec_adjust_grad_whole", "picospec_embed", "picospec_embed_grad", "picospec_clip_grad",
            "picospec_downlink_bytes_max", "picospec_uplink_bytes", "picospec_max_load_byte", "picospec_check_device", "picospec_probe_clock",
            "picospec_workspace_bytes", "picospec_scratch_bytes", "picospec_one_launch_bytes", "picospec_limit", "picospec_strerror", "picospec_version")
 
@@ -89,6 +89,7 @@ lib.picospec_distill_grad.argtypes = [_p, C.c_int, _i64, _i32, _i32, _f, _p, _p,
 lib.picospec_adjust.argtypes = [_p, C.c_int, _i64, _i32, _i32, _i32, _i32, _p, _p, _p, _i64, _i32, _p, _p, _f, _f, _f, _p, _p, _p, _p, _p, _p, _i32,
                                 _p, _i64, _i32, _p, _p, _i64, _p]
 lib.picospec_adjust_grad.argtypes = [_p, _i64, _p, C.c_int, _i64, _i32, _i32, _i32, _i32, _p, _p, _p, _i64, _i32, _p, _f, _p, _p, _i64, _i32, _p, _p, _i64, _p]
+lib.picospec_adjust_whole.argtypes, lib.picospec_adjust_grad_whole.argtypes = lib.picospec_adjust.argtypes, lib.picospec_adjust_grad.argtypes
 lib.picospec_embed.argtypes = [_p, C.c_int, _i64, _i32, _i32, _p, _i32, _f, _p, _i64, _p]
 lib.picospec_embed_grad.argtypes = [_p, C.c_int, _i64, _i32, _p, _i32, _i32, _f, C.c_int, _p, C.c_int, _i64, _p, _sz, _p]
 lib.picospec_clip_grad.argtypes = [_i32, _p, _p, _p, _p, _f, _p, _p, _sz, _p]
@@ -116,7 +117,7 @@ for _n in ("picospec_compress", "picospec_sample_draft", "picospec_verify", "pic
            "picospec_row_stats", "picospec_row_stats_ws", "picospec_compress_rejected", "picospec_resample_sparse", "picospec_version",
            "picospec_pack_downlink", "picospec_unpack_downlink", "picospec_pack_uplink", "picospec_unpack_uplink",
            "picospec_verify_range", "picospec_round", "picospec_sample", "picospec_distill", "picospec_distill_grad",
-           "picospec_adjust", "picospec_adjust_grad", "picospec_embed", "picospec_embed_grad", "picospec_clip_grad"):
+           "picospec_adjust", "picospec_adjust_grad", "picospec_adjust_whole", "picospec_adjust_grad_whole", "picospec_embed", "picospec_embed_grad", "picospec_clip_grad"):
     getattr(lib, _n).restype = C.c_int
 
 
@@ -507,7 +508,8 @@ def adjust(logits: torch.Tensor, V: int, hist: History | None = None, repetition
            draft_tok: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """picospec_adjust of [rows, >=V] device logits -> [rows, V], or `out` (the logits themselves: in place).  One row a sequence, or with seq_off [B + 1] and draft_tok
     [N] the N + B target rows or the N draft rows of a round.  repetition, presence and frequency are numbers or float32 device tensors with one per sequence; mask int32 [masks, >=V / 32]
-    holds 32 ids a word, mask_row int32 [rows] each row's mask (-1: none)."""
+    holds 32 ids a word, mask_row int32 [rows] each row's mask (-1: none).  Rows that no sequence has (offsets that begin above 0 or end before N) are left as they are in
+    `out`, and zeros without it."""
     h = (hist.tok, hist.length, hist.prompt) if hist is not None else _NO_HISTORY
     b = (bias.off, bias.id, bias.value) if bias is not None else _NO_HISTORY
     return _tensor_or_raise(_nat.adjust(logits, V, *h, repetition, presence, frequency, *b, mask, mask_row, seq_off, draft_tok, None, out))
@@ -516,7 +518,8 @@ def adjust(logits: torch.Tensor, V: int, hist: History | None = None, repetition
 def adjust_grad(grad: torch.Tensor, logits: torch.Tensor, V: int, hist: History | None = None, repetition=1.0,
                 mask: torch.Tensor | None = None, mask_row: torch.Tensor | None = None, seq_off: torch.Tensor | None = None,
                 draft_tok: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
-    """picospec_adjust_grad: from the gradient with respect to adjust's rows that with respect to its logits, [rows, V] (what else adjust was given has no part in it).
+    """picospec_adjust_grad: from the gradient with respect to adjust's rows that with respect to its logits, [rows, V] (what else adjust was given has no part in it);
+    rows that no sequence has as in adjust.
     training.adjust is the same for torch's autograd."""
     h = (hist.tok, hist.length, None) if hist is not None else _NO_HISTORY
     return _tensor_or_raise(_nat.adjust(logits, V, *h, repetition, 0.0, 0.0, None, None, None, mask, mask_row, seq_off, draft_tok, grad, out))

@@ -21,11 +21,16 @@ constexpr uint32_t kSeenBit = 1u, kOnce = 2u;
 // -inf, as stored
 template <bool BF16> constexpr uint32_t kMaskedBits = BF16 ? 0xFF80u : 0xFF800000u;
 
-__device__ __forceinline__ float setting(const float* rows, int b, float all) { return rows ? rows[b] : all; }
+// A word that the kernel does not write and that a whole wave reads, by a scalar load (behind stores that may lie in front of it the compiler takes a vector load, and a sequence has ten such words:
+// 5 to 10 % of a call)
+template <class T>
+__device__ __forceinline__ T input(const T* p) { return *(const __attribute__((address_space(4))) T*)p; }
+
+__device__ __forceinline__ float setting(const float* rows, int b, float all) { return rows ? input(rows + b) : all; }
 
 // T threads with VPT vectors of a row each
 template <bool BF16, bool GRAD, int T, int VPT>
-__global__ __launch_bounds__(T) void adjust_kernel(const AdjustArgs a)
+__device__ __forceinline__ void adjust_rows(const AdjustArgs& a)
 {
     constexpr int N = Vec<BF16>::N, ESZ = BF16 ? 2 : 4, IDS = T * VPT * N;
     constexpr unsigned WHOLE = (1u << N) - 1u;
@@ -39,8 +44,8 @@ __global__ __launch_bounds__(T) void adjust_kernel(const AdjustArgs a)
     // the sequence's rows of this part, and the drafted tokens in front of them (what the offsets say beyond the arrays is not followed)
     int off = 0, gamma = 0;
     if (a.seq_off) {
-        off = min(max(a.seq_off[b], 0), a.n_draft);
-        gamma = min(max(a.seq_off[b + 1], off), a.n_draft) - off;
+        off = min(max(input(a.seq_off + b), 0), a.n_draft);
+        gamma = min(max(input(a.seq_off + b + 1), off), a.n_draft) - off;
     }
     const int n = a.seq_off ? gamma + a.bonus : 1, each = (n + a.parts - 1) / a.parts, t0 = part * each, t1 = min(t0 + each, n);
     const int64_t row0 = a.seq_off ? (int64_t)off + (a.bonus ? b : 0) : b;
@@ -53,14 +58,14 @@ __global__ __launch_bounds__(T) void adjust_kernel(const AdjustArgs a)
     const bool counted = rep != 1.f || pres != 0.f || freq != 0.f;
     int bias0 = 0, bias1 = 0;
     if (!GRAD && a.bias_off) {
-        bias0 = min(max(a.bias_off[b], 0), a.n_bias);
-        bias1 = min(max(a.bias_off[b + 1], bias0), a.n_bias);
+        bias0 = min(max(input(a.bias_off + b), 0), a.n_bias);
+        bias1 = min(max(input(a.bias_off + b + 1), bias0), a.n_bias);
     }
     const bool biased = bias1 > bias0;
     int length = 0, prompt = 0;
     if (a.hist_tok) {
-        length = min(max(a.hist_len[b], 0), a.hist_cap);
-        prompt = a.prompt_len ? a.prompt_len[b] : 0;
+        length = min(max(input(a.hist_len + b), 0), a.hist_cap);
+        prompt = a.prompt_len ? input(a.prompt_len + b) : 0;
     }
     if (!counted) length = 0;
 
@@ -88,7 +93,7 @@ __global__ __launch_bounds__(T) void adjust_kernel(const AdjustArgs a)
 #pragma unroll
         for (int j = 0; j < VPT; ++j) allowed[j] = WHOLE;
         if (!a.mask || t >= t1) return;
-        const int m = a.mask_row ? a.mask_row[row0 + t] : (int)(row0 + t);
+        const int m = a.mask_row ? input(a.mask_row + row0 + t) : (int)(row0 + t);
         if ((unsigned)m >= (unsigned)a.n_masks) return;
         const unsigned char* const mask = reinterpret_cast<const unsigned char*>(a.mask + (int64_t)m * a.ld_mask) + lo / 8;
 #pragma unroll
@@ -265,22 +270,48 @@ __global__ __launch_bounds__(T) void adjust_kernel(const AdjustArgs a)
     }
 }
 
+// Zeros in the rows that no sequence has, in front of the first one and behind the last, by workgroup `at` of a.idle: a few for every chunk of the vocabulary
+template <bool BF16, int T, int IDS>
+__device__ __forceinline__ void zero_rest(const AdjustArgs& a, int at)
+{
+    constexpr int N = Vec<BF16>::N, ESZ = BF16 ? 2 : 4;
+    const int lo = at % a.chunks * IDS, ids = min(IDS, a.V - lo);
+    const int64_t front = min(max(a.seq_off[0], 0), a.n_draft), back = (int64_t)min(max(a.seq_off[a.B], 0), a.n_draft) + (a.bonus ? a.B : 0), outside = front + a.n_rows - back;
+    for (int64_t i = at / a.chunks; i < outside; i += a.idle / a.chunks) {
+        char* const row = (char*)a.out + ((i < front ? i : back + i - front) * a.ld_out + lo) * ESZ;
+        for (int x = (int)threadIdx.x * N; x < ids; x += T * N) store_row_vec<BF16>(row, x, ids, make_uint4(0, 0, 0, 0));
+    }
+}
+
+// The workgroups behind those of the sequences are for the rows of none (there are none, mostly, and a workgroup that finds that out costs nothing there)
+template <bool BF16, bool GRAD, int T, int VPT>
+__global__ __launch_bounds__(T) void adjust_kernel(const AdjustArgs a)
+{
+    if (blockIdx.x < a.busy) adjust_rows<BF16, GRAD, T, VPT>(a);
+    else zero_rest<BF16, T, T * VPT * Vec<BF16>::N>(a, (int)(blockIdx.x - a.busy));
+}
+
 template <bool BF16, bool GRAD, int T, int VPT>
 hipError_t launch_one(AdjustArgs a, int B, int64_t n_rows, hipStream_t stream)
 {
     constexpr int IDS = T * VPT * Vec<BF16>::N;
     const size_t lds = (size_t)IDS * (4 + (BF16 ? 2 : 4) + (!GRAD && a.bias_off ? 4 : 0));
     a.chunks = (a.V + IDS - 1) / IDS;
+    a.B = B;
+    a.n_rows = (int)n_rows;
     const int64_t groups = (int64_t)B * a.chunks, mean = (n_rows + B - 1) / B;
     // A sequence's rows shared out, each share counting the history again: where there are fewer than kAdjustGroups workgroups of 256 threads (us, one share / two / four: 8 sequences of 9 rows of 128,256 fp32
     // 14.2 / 12.5 / 14.2, gradients of 32 sequences of 9.5 rows of 32,000 fp32 27 / 20.5 / 20.4), and where rows are so many that the sequences' ends are far apart (256 of 9.5 rows of 151,936 bf16 309 / 300 / 323;
     // of 5 rows of 75,000 fp32 177 / 182 / 208)
     a.parts = (int)std::min<int64_t>(mean, std::max<int64_t>((kAdjustGroups * 256 / T + groups - 1) / groups, mean >= 8 ? 2 : 1));
+    a.busy = (uint32_t)(groups * a.parts);
+    // (one workgroup for every chunk and 32 rows, up to 256: a batch that is mostly padding has a share of the chip to write it, and a small one not more of them than it has others)
+    a.idle = a.whole && a.seq_off ? a.chunks * (int)std::min<int64_t>(std::max(256 / a.chunks, 1), (n_rows + 31) / 32) : 0;
     static DeviceFlags done;
     int dev;
     if (lds > 64 * 1024)
         if (hipError_t e = raise_lds_limit_once((const void*)adjust_kernel<BF16, GRAD, T, VPT>, 160 * 1024, done, dev)) return e;
-    hipLaunchKernelGGL((adjust_kernel<BF16, GRAD, T, VPT>), dim3((unsigned)(groups * a.parts)), dim3(T), lds, stream, a);
+    hipLaunchKernelGGL((adjust_kernel<BF16, GRAD, T, VPT>), dim3(a.busy + (unsigned)a.idle), dim3(T), lds, stream, a);
     return hipGetLastError();
 }
 

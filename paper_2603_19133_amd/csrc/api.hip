@@ -620,17 +620,20 @@ int check_adjust(const void* src, int64_t ld_src, const void* logits, int dtype,
 
 }  // namespace
 
-int picospec_adjust(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
-                    int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
-                    const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len, const int32_t* prompt_len,
-                    float repetition, float presence, float frequency,
-                    const float* repetition_rows, const float* presence_rows, const float* frequency_rows,
-                    const int32_t* bias_off, const int32_t* bias_id, const float* bias_value, int32_t n_bias,
-                    const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
-                    void* out, int64_t ld_out, void* stream)
+namespace {
+
+int adjust(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+           int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+           const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len, const int32_t* prompt_len,
+           float repetition, float presence, float frequency,
+           const float* repetition_rows, const float* presence_rows, const float* frequency_rows,
+           const int32_t* bias_off, const int32_t* bias_id, const float* bias_value, int32_t n_bias,
+           const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+           void* out, int64_t ld_out, int whole, void* stream)
 {
     if (int rc = check_adjust(logits, ld, logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len,
                               repetition, repetition_rows, mask, ld_mask, n_masks, mask_row, out, ld_out)) return rc;
+    if (whole && n_rows > 0 && out == logits) return PICOSPEC_EINVAL;
     if ((!presence_rows && !std::isfinite(presence)) || (!frequency_rows && !std::isfinite(frequency))) return PICOSPEC_EINVAL;
     if (bias_off && (n_bias < 0 || (n_bias > 0 && (!bias_id || !bias_value)))) return PICOSPEC_EINVAL;
     AdjustArgs a{};
@@ -642,7 +645,59 @@ int picospec_adjust(const void* logits, int dtype, int64_t ld, int32_t n_rows, i
     a.bias_off = n_bias > 0 ? bias_off : nullptr; a.bias_id = bias_id; a.bias_value = bias_value; a.n_bias = n_bias;
     a.mask = mask; a.ld_mask = ld_mask; a.n_masks = n_masks; a.mask_row = mask_row;
     a.in_place = out == logits;
+    a.whole = whole;
     return hip_status(launch_adjust(a, dtype, B, n_rows, false, (hipStream_t)stream));
+}
+
+int adjust_grad(const void* grad, int64_t ld_grad, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len,
+                float repetition, const float* repetition_rows,
+                const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                void* out, int64_t ld_out, int whole, void* stream)
+{
+    if (int rc = check_adjust(grad, ld_grad, logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len,
+                              repetition, repetition_rows, mask, ld_mask, n_masks, mask_row, out, ld_out)) return rc;
+    if (whole && n_rows > 0 && out == grad) return PICOSPEC_EINVAL;
+    AdjustArgs a{};
+    a.src = grad; a.ld_src = ld_grad; a.logits = logits; a.ld = ld; a.out = out; a.ld_out = ld_out; a.V = V;
+    a.seq_off = seq_off; a.draft_tok = draft_tok; a.n_draft = n_draft; a.bonus = n_rows != n_draft;
+    a.hist_tok = hist_tok; a.ld_hist = ld_hist; a.hist_cap = hist_cap; a.hist_len = hist_len;
+    a.repetition = repetition; a.repetition_rows = repetition_rows;
+    a.mask = mask; a.ld_mask = ld_mask; a.n_masks = n_masks; a.mask_row = mask_row;
+    a.in_place = out == grad;
+    a.whole = whole;
+    return hip_status(launch_adjust(a, dtype, B, n_rows, true, (hipStream_t)stream));
+}
+
+}  // namespace
+
+int picospec_adjust(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                    int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                    const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len, const int32_t* prompt_len,
+                    float repetition, float presence, float frequency,
+                    const float* repetition_rows, const float* presence_rows, const float* frequency_rows,
+                    const int32_t* bias_off, const int32_t* bias_id, const float* bias_value, int32_t n_bias,
+                    const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                    void* out, int64_t ld_out, void* stream)
+{
+    return adjust(logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len, prompt_len, repetition,
+                  presence, frequency, repetition_rows, presence_rows, frequency_rows, bias_off, bias_id, bias_value, n_bias, mask, ld_mask, n_masks,
+                  mask_row, out, ld_out, 0, stream);
+}
+
+int picospec_adjust_whole(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                          int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                          const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len, const int32_t* prompt_len,
+                          float repetition, float presence, float frequency,
+                          const float* repetition_rows, const float* presence_rows, const float* frequency_rows,
+                          const int32_t* bias_off, const int32_t* bias_id, const float* bias_value, int32_t n_bias,
+                          const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                          void* out, int64_t ld_out, void* stream)
+{
+    return adjust(logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len, prompt_len, repetition,
+                  presence, frequency, repetition_rows, presence_rows, frequency_rows, bias_off, bias_id, bias_value, n_bias, mask, ld_mask, n_masks,
+                  mask_row, out, ld_out, 1, stream);
 }
 
 int picospec_adjust_grad(const void* grad, int64_t ld_grad, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
@@ -652,16 +707,19 @@ int picospec_adjust_grad(const void* grad, int64_t ld_grad, const void* logits, 
                          const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
                          void* out, int64_t ld_out, void* stream)
 {
-    if (int rc = check_adjust(grad, ld_grad, logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len,
-                              repetition, repetition_rows, mask, ld_mask, n_masks, mask_row, out, ld_out)) return rc;
-    AdjustArgs a{};
-    a.src = grad; a.ld_src = ld_grad; a.logits = logits; a.ld = ld; a.out = out; a.ld_out = ld_out; a.V = V;
-    a.seq_off = seq_off; a.draft_tok = draft_tok; a.n_draft = n_draft; a.bonus = n_rows != n_draft;
-    a.hist_tok = hist_tok; a.ld_hist = ld_hist; a.hist_cap = hist_cap; a.hist_len = hist_len;
-    a.repetition = repetition; a.repetition_rows = repetition_rows;
-    a.mask = mask; a.ld_mask = ld_mask; a.n_masks = n_masks; a.mask_row = mask_row;
-    a.in_place = out == grad;
-    return hip_status(launch_adjust(a, dtype, B, n_rows, true, (hipStream_t)stream));
+    return adjust_grad(grad, ld_grad, logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len,
+                       repetition, repetition_rows, mask, ld_mask, n_masks, mask_row, out, ld_out, 0, stream);
+}
+
+int picospec_adjust_grad_whole(const void* grad, int64_t ld_grad, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
+                               int32_t B, int32_t n_draft, const int32_t* seq_off, const int32_t* draft_tok,
+                               const int32_t* hist_tok, int64_t ld_hist, int32_t hist_cap, const int32_t* hist_len,
+                               float repetition, const float* repetition_rows,
+                               const uint32_t* mask, int64_t ld_mask, int32_t n_masks, const int32_t* mask_row,
+                               void* out, int64_t ld_out, void* stream)
+{
+    return adjust_grad(grad, ld_grad, logits, dtype, ld, n_rows, V, B, n_draft, seq_off, draft_tok, hist_tok, ld_hist, hist_cap, hist_len,
+                       repetition, repetition_rows, mask, ld_mask, n_masks, mask_row, out, ld_out, 1, stream);
 }
 
 int picospec_embed(const void* table, int dtype, int64_t ld, int32_t V, int32_t d, const int32_t* tok, int32_t n, float scale,

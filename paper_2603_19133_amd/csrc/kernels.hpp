@@ -484,6 +484,8 @@ struct AdjustArgs {
     const int32_t *bias_off, *bias_id; const float* bias_value; int n_bias;
     const uint32_t* mask; int64_t ld_mask; int n_masks; const int32_t* mask_row;
     int chunks, parts, in_place;
+    int whole, B, n_rows, idle;                                   // whole: zeros in rows that no sequence has, by `idle` workgroups behind the `busy` ones
+    uint32_t busy;
 };
 constexpr int kAdjustGroups = 2048;                               // workgroups (of 256 threads) that fill the chip
 // An upper bound of the threads of a launch: a thread has one vector or more; or the rows are shared out until there are kAdjustGroups workgroups, or in two

@@ -451,14 +451,15 @@ struct Adjustment {
             refuse_unless(!mask_row.defined());
         }
     }
-    int forward(const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out) const {
-        return picospec_adjust(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
+    // whole: `out` is new, and rows that no sequence has are zeros in it
+    int forward(const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out, bool whole) const {
+        return (whole ? picospec_adjust_whole : picospec_adjust)(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
                                data<int32_t>(hist_tok), ld_hist, (int32_t)hist_cap, data<int32_t>(length), data<int32_t>(prompt), repetition.all, presence.all, frequency.all,
                                data<float>(repetition.each), data<float>(presence.each), data<float>(frequency.each), data<int32_t>(bias_off), data<int32_t>(bias_id), data<float>(bias_value), (int32_t)n_bias,
                                data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, getCurrentHIPStream().stream());
     }
-    int backward(const at::Tensor& g, int64_t ld_g, const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out) const {
-        return picospec_adjust_grad(g.data_ptr(), ld_g, z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
+    int backward(const at::Tensor& g, int64_t ld_g, const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out, bool whole) const {
+        return (whole ? picospec_adjust_grad_whole : picospec_adjust_grad)(g.data_ptr(), ld_g, z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
                                     data<int32_t>(hist_tok), ld_hist, (int32_t)hist_cap, data<int32_t>(length), repetition.all, data<float>(repetition.each),
                                     data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, getCurrentHIPStream().stream());
     }
@@ -505,7 +506,7 @@ PyObject* n_adjust(PyObject*, PyObject* const* v, Py_ssize_t n) {
         const c10::DeviceGuard guard(z.device());
         if (!given) out = at::empty({rows, V}, z.options());
         const int64_t ld_out = rows_like(out, z, rows, V);
-        check_code(grad.defined() ? by.backward(grad, ld_g, z, dt, ld, V, out, ld_out) : by.forward(z, dt, ld, V, out, ld_out));
+        check_code(grad.defined() ? by.backward(grad, ld_g, z, dt, ld, V, out, ld_out, !given) : by.forward(z, dt, ld, V, out, ld_out, !given));
         if (given) written(out);
         return THPVariable_Wrap(out);
     });
@@ -519,7 +520,7 @@ struct AdjustFunction : torch::autograd::Function<AdjustFunction> {
         if (z.size(0) <= 1) ld = std::max(ld, V);
         const c10::DeviceGuard guard(z.device());
         at::Tensor out = at::empty({z.size(0), V}, z.options());
-        check_code(by->forward(z, dt, ld, V, out, V));
+        check_code(by->forward(z, dt, ld, V, out, V, true));
         ctx->save_for_backward({z, by->hist_tok, by->length, by->repetition.each, by->mask, by->mask_row, by->seq_off, by->draft_tok});
         ctx->saved_data["V"] = V;
         ctx->saved_data["repetition"] = (double)by->repetition.all;
@@ -542,7 +543,7 @@ struct AdjustFunction : torch::autograd::Function<AdjustFunction> {
         at::Tensor out = at::empty(z.sizes(), z.options());
         if (z.size(1) > V) out.slice(1, V).zero_();                                                 // (columns behind the vocabulary are not read)
         const at::Tensor g = grads[0].contiguous();                                                 // (of a sum: one value seen from every place)
-        const int rc = by.backward(g, V, z, dt, ld, V, out, z.size(1));
+        const int rc = by.backward(g, V, z, dt, ld, V, out, z.size(1), true);
         TORCH_CHECK(rc == PICOSPEC_OK, "picospec error ", rc, ": ", picospec_strerror(rc));
         return {out, at::Tensor(), at::Tensor()};
     }
