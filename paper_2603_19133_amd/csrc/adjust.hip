@@ -292,21 +292,10 @@ __global__ __launch_bounds__(T) void adjust_kernel(const AdjustArgs a)
 }
 
 template <bool BF16, bool GRAD, int T, int VPT>
-hipError_t launch_one(AdjustArgs a, int B, int64_t n_rows, hipStream_t stream)
+hipError_t launch_one(const AdjustArgs& a, hipStream_t stream)
 {
     constexpr int IDS = T * VPT * Vec<BF16>::N;
     const size_t lds = (size_t)IDS * (4 + (BF16 ? 2 : 4) + (!GRAD && a.bias_off ? 4 : 0));
-    a.chunks = (a.V + IDS - 1) / IDS;
-    a.B = B;
-    a.n_rows = (int)n_rows;
-    const int64_t groups = (int64_t)B * a.chunks, mean = (n_rows + B - 1) / B;
-    // A sequence's rows shared out, each share counting the history again: where there are fewer than kAdjustGroups workgroups of 256 threads (us, one share / two / four: 8 sequences of 9 rows of 128,256 fp32
-    // 14.2 / 12.5 / 14.2, gradients of 32 sequences of 9.5 rows of 32,000 fp32 27 / 20.5 / 20.4), and where rows are so many that the sequences' ends are far apart (256 of 9.5 rows of 151,936 bf16 309 / 300 / 323;
-    // of 5 rows of 75,000 fp32 177 / 182 / 208)
-    a.parts = (int)std::min<int64_t>(mean, std::max<int64_t>((kAdjustGroups * 256 / T + groups - 1) / groups, mean >= 8 ? 2 : 1));
-    a.busy = (uint32_t)(groups * a.parts);
-    // (one workgroup for every chunk and 32 rows, up to 256: a batch that is mostly padding has a share of the chip to write it, and a small one not more of them than it has others)
-    a.idle = a.whole && a.seq_off ? a.chunks * (int)std::min<int64_t>(std::max(256 / a.chunks, 1), (n_rows + 31) / 32) : 0;
     static DeviceFlags done;
     int dev;
     if (lds > 64 * 1024)
@@ -315,31 +304,54 @@ hipError_t launch_one(AdjustArgs a, int B, int64_t n_rows, hipStream_t stream)
     return hipGetLastError();
 }
 
+template <bool BF16, bool GRAD>
+hipError_t launch(const AdjustArgs& a, const AdjustPlan& plan, hipStream_t stream)
+{
+    constexpr int MOST = 8192 / (512 * Vec<BF16>::N);
+    if (plan.T == 512) return plan.vectors == MOST ? launch_one<BF16, GRAD, 512, MOST>(a, stream) : launch_one<BF16, GRAD, 512, 1>(a, stream);
+    if constexpr (!GRAD)
+        if (plan.vectors == 2) return launch_one<BF16, GRAD, 256, 2>(a, stream);
+    return launch_one<BF16, GRAD, 256, 1>(a, stream);
+}
+
+}  // namespace
+
 // Which way, us:
 //   512 threads             histories that are longer than what a sequence has of rows in a chunk (each chunk reads the history).  8192 ids where these are workgroups enough: 512 single rows of
 //                           151,936 fp32, up to 32,768 tokens 193, with 2048 ids 252; 64 of bf16 23 (26, with one vector 28).  Else one vector: a row of 151,936 bf16 with 32,768 tokens 8.8 (8192 ids 10.6, 256
 //                           threads 11.8), 9 rows of it with 100,000 20 (23, 30)
 //   256 threads, 2 vectors  512 single rows of 151,936 bf16 87 (with one vector 124, 8192 ids 92), 64 of 128,256 fp32 17.6 (20, 19)
 //   256 threads, 1 vector   gradients (128 sequences of 5.5 rows of 128,256 bf16 82, with two vectors 95) and what would leave compute units without work (64 of 6.5 rows of 50,001 bf16 27.7 / 30.1)
-template <bool BF16, bool GRAD>
-hipError_t launch(const AdjustArgs& a, int B, int64_t n_rows, hipStream_t stream)
+AdjustPlan adjust_plan(const AdjustArgs& a, int dtype, int B, int64_t n_rows, bool gradient)
 {
-    constexpr int N = Vec<BF16>::N;
-    auto groups = [&](int ids) { return (int64_t)B * ((a.V + ids - 1) / ids); };
-    if (a.hist_tok && a.hist_cap > (n_rows + B - 1) / B * (256 * 2 * N))
-        return groups(8192) >= 1024 ? launch_one<BF16, GRAD, 512, 8192 / (512 * N)>(a, B, n_rows, stream) : launch_one<BF16, GRAD, 512, 1>(a, B, n_rows, stream);
-    if constexpr (!GRAD)
-        if (groups(256 * 2 * N) >= 1024) return launch_one<BF16, GRAD, 256, 2>(a, B, n_rows, stream);
-    return launch_one<BF16, GRAD, 256, 1>(a, B, n_rows, stream);
+    const int N = dtype == 1 ? Vec<true>::N : Vec<false>::N;
+    const int64_t mean = (n_rows + B - 1) / B;
+    auto chunks = [&](int ids) { return (a.V + ids - 1) / ids; };
+    AdjustPlan p{256, 1};
+    if (a.hist_tok && a.hist_cap > mean * (256 * 2 * N)) {
+        p.T = 512;
+        if ((int64_t)B * chunks(8192) >= 1024) p.vectors = 8192 / (512 * N);
+    } else if (!gradient && (int64_t)B * chunks(256 * 2 * N) >= 1024) {
+        p.vectors = 2;
+    }
+    p.chunks = chunks(p.T * p.vectors * N);
+    // A sequence's rows shared out, each share counting the history again: where there are fewer than kAdjustGroups workgroups of 256 threads (us, one share / two / four: 8 sequences of 9 rows of 128,256 fp32
+    // 14.2 / 12.5 / 14.2, gradients of 32 sequences of 9.5 rows of 32,000 fp32 27 / 20.5 / 20.4), and where rows are so many that the sequences' ends are far apart (256 of 9.5 rows of 151,936 bf16 309 / 300 / 323;
+    // of 5 rows of 75,000 fp32 177 / 182 / 208)
+    const int64_t groups = (int64_t)B * p.chunks;
+    p.parts = (int)std::min<int64_t>(mean, std::max<int64_t>((kAdjustGroups * 256 / p.T + groups - 1) / groups, mean >= 8 ? 2 : 1));
+    p.busy = groups * p.parts;
+    // (one workgroup for every chunk and 32 rows, up to 256: a batch that is mostly padding has a share of the chip to write it, and a small one not more of them than it has others)
+    p.idle = a.whole && a.seq_off ? p.chunks * (int)std::min<int64_t>(std::max(256 / p.chunks, 1), (n_rows + 31) / 32) : 0;
+    p.fits = (p.busy + p.idle) * p.T <= (int64_t)UINT32_MAX;
+    return p;
 }
 
-}  // namespace
-
-hipError_t launch_adjust(AdjustArgs a, int dtype, int B, int64_t n_rows, bool gradient, hipStream_t stream)
+hipError_t launch_adjust(AdjustArgs a, const AdjustPlan& plan, int dtype, int B, int64_t n_rows, bool gradient, hipStream_t stream)
 {
-    if (n_rows == 0) return hipSuccess;
-    if (gradient) return dtype == 1 ? launch<true, true>(a, B, n_rows, stream) : launch<false, true>(a, B, n_rows, stream);
-    return dtype == 1 ? launch<true, false>(a, B, n_rows, stream) : launch<false, false>(a, B, n_rows, stream);
+    a.chunks = plan.chunks; a.parts = plan.parts; a.idle = plan.idle; a.busy = (uint32_t)plan.busy; a.B = B; a.n_rows = (int)n_rows;
+    if (gradient) return dtype == 1 ? launch<true, true>(a, plan, stream) : launch<false, true>(a, plan, stream);
+    return dtype == 1 ? launch<true, false>(a, plan, stream) : launch<false, false>(a, plan, stream);
 }
 
 }  // namespace picospec

@@ -614,8 +614,15 @@ int check_adjust(const void* src, int64_t ld_src, const void* logits, int dtype,
     const Span to = span(out, n_rows, ld_out, V, esize(dtype));
     if (!(out == src && ld_out == ld_src) && overlap(to, span(src, n_rows, ld_src, V, esize(dtype)))) return PICOSPEC_EINVAL;
     if (!(logits == src && ld == ld_src) && overlap(to, span(logits, n_rows, ld, V, esize(dtype)))) return PICOSPEC_EINVAL;
-    if (adjust_threads_most(dtype, B, V) > UINT32_MAX) return PICOSPEC_EUNSUPPORTED;
     return PICOSPEC_OK;
+}
+
+int run_adjust(const AdjustArgs& a, int dtype, int B, int n_rows, bool gradient, void* stream)
+{
+    if (n_rows == 0) return PICOSPEC_OK;
+    const AdjustPlan plan = adjust_plan(a, dtype, B, n_rows, gradient);
+    if (!plan.fits) return PICOSPEC_EUNSUPPORTED;
+    return hip_status(launch_adjust(a, plan, dtype, B, n_rows, gradient, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -646,7 +653,7 @@ int adjust(const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
     a.mask = mask; a.ld_mask = ld_mask; a.n_masks = n_masks; a.mask_row = mask_row;
     a.in_place = out == logits;
     a.whole = whole;
-    return hip_status(launch_adjust(a, dtype, B, n_rows, false, (hipStream_t)stream));
+    return run_adjust(a, dtype, B, n_rows, false, stream);
 }
 
 int adjust_grad(const void* grad, int64_t ld_grad, const void* logits, int dtype, int64_t ld, int32_t n_rows, int32_t V,
@@ -667,7 +674,7 @@ int adjust_grad(const void* grad, int64_t ld_grad, const void* logits, int dtype
     a.mask = mask; a.ld_mask = ld_mask; a.n_masks = n_masks; a.mask_row = mask_row;
     a.in_place = out == grad;
     a.whole = whole;
-    return hip_status(launch_adjust(a, dtype, B, n_rows, true, (hipStream_t)stream));
+    return run_adjust(a, dtype, B, n_rows, true, stream);
 }
 
 }  // namespace

@@ -488,9 +488,10 @@ struct AdjustArgs {
     uint32_t busy;
 };
 constexpr int kAdjustGroups = 2048;                               // workgroups (of 256 threads) that fill the chip
-// An upper bound of the threads of a launch: a thread has one vector or more; or the rows are shared out until there are kAdjustGroups workgroups, or in two
-inline int64_t adjust_threads_most(int dtype, int64_t B, int V) { const int ids = dtype == 1 ? 2048 : 1024; return std::max<int64_t>(2 * B * ((V + ids - 1) / ids), 2 * kAdjustGroups) * 256; }
-hipError_t launch_adjust(AdjustArgs a, int dtype, int B, int64_t n_rows, bool gradient, hipStream_t stream);
+// How a call is launched: workgroups of T threads with `vectors` vectors of a row each, for `chunks` chunks of the vocabulary and a sequence's rows shared out in `parts`; `idle` more for rows of no sequence
+struct AdjustPlan { int T, vectors, chunks, parts, idle; int64_t busy; bool fits; };
+AdjustPlan adjust_plan(const AdjustArgs& a, int dtype, int B, int64_t n_rows, bool gradient);
+hipError_t launch_adjust(AdjustArgs a, const AdjustPlan& plan, int dtype, int B, int64_t n_rows, bool gradient, hipStream_t stream);
 
 // ---- token embeddings (csrc/embed.hip)
 hipError_t launch_embed(const void* table, int dtype, int64_t ld, int V, int64_t d, const int32_t* tok, int64_t n, float scale, void* out, int64_t ld_out, hipStream_t stream);
