@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 #include <stdexcept>
+#include <string>
 
 #include "../../include/picospec.h"
 
@@ -266,7 +267,11 @@ PyObject* n_distill_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
 // ---- the distillation loss on torch's tape, in native code: the engine runs the backward call in a thread of its own, which would have to wait for the
 // interpreter twice (forward and backward of a small batch, on the host: 37 us with a Python function, of which torch takes 25 for any operator)
 
-struct Refused { int code; };
+// A call that the library would refuse, or has refused.  Where no call of the binding answers it with its code - a backward call, in a thread of the engine's - it is an error like any other.
+struct Refused : std::runtime_error {
+    int code;
+    explicit Refused(int code) : std::runtime_error("picospec error " + std::to_string(code) + ": " + picospec_strerror(code)), code(code) {}
+};
 
 int logits_code(const at::Tensor& t, int64_t& ld) {        // dtype code or error of rows2d
     if (t.dim() != 2 || !t.is_cuda()) throw Refused{PICOSPEC_EINVAL};
@@ -543,8 +548,7 @@ struct AdjustFunction : torch::autograd::Function<AdjustFunction> {
         at::Tensor out = at::empty(z.sizes(), z.options());
         if (z.size(1) > V) out.slice(1, V).zero_();                                                 // (columns behind the vocabulary are not read)
         const at::Tensor g = grads[0].contiguous();                                                 // (of a sum: one value seen from every place)
-        const int rc = by.backward(g, V, z, dt, ld, V, out, z.size(1), true);
-        TORCH_CHECK(rc == PICOSPEC_OK, "picospec error ", rc, ": ", picospec_strerror(rc));
+        check_code(by.backward(g, V, z, dt, ld, V, out, z.size(1), true));
         return {out, at::Tensor(), at::Tensor()};
     }
 };
@@ -646,11 +650,7 @@ struct EmbedFunction : torch::autograd::Function<EmbedFunction> {
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
         TORCH_CHECK(!at::GradMode::is_enabled(), "embed is differentiable once");                   // (create_graph: the kernel is not on the tape)
         const auto saved = ctx->get_saved_variables();
-        try {
-            return {embed_grad(grads[0].contiguous(), saved[0], ctx->saved_data["V"].toInt(), (float)ctx->saved_data["scale"].toDouble(), 0, at::Tensor()), at::Tensor(), at::Tensor()};
-        } catch (const Refused& r) {
-            TORCH_CHECK(false, "picospec error ", r.code, ": ", picospec_strerror(r.code));
-        }
+        return {embed_grad(grads[0].contiguous(), saved[0], ctx->saved_data["V"].toInt(), (float)ctx->saved_data["scale"].toDouble(), 0, at::Tensor()), at::Tensor(), at::Tensor()};
     }
 };
 
