@@ -328,9 +328,13 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
         const double T = ctx->saved_data["T"].toDouble();
         int64_t ld;
         const int dt = logits_code(z, ld);
+        const at::Tensor weight = grads[0].contiguous();                                            // (of a sum or mean over the rows: one value seen from every row)
+        // (what a hook gives back for the saved tensors need not be what they were)
+        check_record(z, idx, prob, count, k);
+        if (V > z.size(1) || stats.dim() != 2 || stats.size(0) != z.size(0) || stats.size(1) != 4 || !dense(stats, at::kDouble, z)) throw Refused{PICOSPEC_EINVAL};
+        if (weight.numel() != z.size(0) || !dense(weight, at::kFloat, z)) throw Refused{PICOSPEC_EINVAL};
         at::Tensor grad = at::empty(z.sizes(), z.options());
         if (z.size(1) > V) grad.slice(1, V).zero_();                                                // (columns behind the vocabulary are not read)
-        const at::Tensor weight = grads[0].contiguous();                                            // (of a sum or mean over the rows: one value seen from every row)
         const int rc = picospec_distill_grad(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
                                              (int)tail, weight.data_ptr<float>(), stats.data_ptr<double>(), grad.data_ptr(), z.size(1), c10::hip::getCurrentHIPStream().stream());
         TORCH_CHECK(rc == PICOSPEC_OK, "picospec error ", rc, ": ", picospec_strerror(rc));
@@ -548,6 +552,7 @@ struct AdjustFunction : torch::autograd::Function<AdjustFunction> {
         at::Tensor out = at::empty(z.sizes(), z.options());
         if (z.size(1) > V) out.slice(1, V).zero_();                                                 // (columns behind the vocabulary are not read)
         const at::Tensor g = grads[0].contiguous();                                                 // (of a sum: one value seen from every place)
+        rows_like(g, z, z.size(0), V);                                                              // (what a hook gives back for the logits need not have the rows that they had)
         check_code(by.backward(g, V, z, dt, ld, V, out, z.size(1), true));
         return {out, at::Tensor(), at::Tensor()};
     }

@@ -45,3 +45,23 @@ def _refused(leaf, call, unpack):
 def test_other_forms(gpu, calls, name, form):
     print(f"[case] saved tensors {name} {form}", flush=True)
     _refused(*calls[name], FORMS[form])
+
+
+SIZES = {
+    "all of fewer rows": lambda t: t[:-1],
+    "all of more rows": lambda t: torch.cat([t, t[:1]]),
+    "logits of fewer rows": lambda t: t[:-1] if t.dtype == torch.float32 and t.dim() == 2 and t.shape[1] == 300 else t,
+    "logits of more rows": lambda t: torch.cat([t, t[:1]]) if t.dtype == torch.float32 and t.dim() == 2 and t.shape[1] == 300 else t,
+    "logits of fewer columns": lambda t: t[:, :-1].contiguous() if t.dtype == torch.float32 and t.dim() == 2 and t.shape[1] == 300 else t,
+    "whole numbers on the host": lambda t: t.cpu() if t.dtype == torch.int32 else t,
+    "fewer whole numbers": lambda t: t[:-1] if t.dtype == torch.int32 else t,
+    "wide numbers on the host": lambda t: t.cpu() if t.dtype == torch.float64 else t,
+    "fewer wide numbers": lambda t: t[:-1] if t.dtype == torch.float64 else t,
+}
+
+
+@pytest.mark.parametrize("name,size", [(n, s) for n in ("adjust", "adjust round", "embed", "distill_loss") for s in SIZES
+                                       if not (s.startswith("logits") and n == "embed") and not ("wide" in s and n != "distill_loss")])       # (what a call saves)
+def test_other_sizes(gpu, calls, name, size):
+    print(f"[case] saved tensors {name} {size}", flush=True)
+    _refused(*calls[name], SIZES[size])
