@@ -10,7 +10,8 @@ pool keeps it for the replays.
 Outputs that a call allocates by itself (the wire messages', sample_draft's, row_stats') share one allocation as far as they are
 small (64 KB each): one that is kept keeps the other small ones of its call, torch.save writes them with it, and an in-place resize_
 beyond its size runs into them; clone() it for any of these.  Larger outputs stand alone.
-adjust, embed, clip_grad and their gradients run on the current stream of their tensors' device, also where another device is current.
+adjust, embed, clip_grad and their gradients run on the current stream of their tensors' device, also where another device is current.  They record nothing for torch's
+autograd (training has what does), so their `out` may not require a gradient while it records.
 There is no fallback: if the library has not been built (``python -m paper_2603_19133_amd.build``) importing this module raises.
 """
 from __future__ import annotations

@@ -474,6 +474,9 @@ struct Adjustment {
     }
 };
 
+// A tensor that a call is to write must not be part of what the tape records: it does not learn of the call, and a gradient that is taken later would leave it out
+void refuse_recorded(const at::Tensor& out) { refuse_unless(!(out.defined() && out.requires_grad() && at::GradMode::is_enabled())); }
+
 // A tensor that a call has written in place: what the tape has saved of it is not what it was
 void written(const at::Tensor& t) { if (!t.is_inference()) torch::autograd::impl::bump_version(t); }
 
@@ -505,6 +508,7 @@ PyObject* n_adjust(PyObject*, PyObject* const* v, Py_ssize_t n) {
         const at::Tensor grad = optional_tensor(a);
         at::Tensor out = optional_tensor(a);
         a.done();
+        refuse_recorded(out);
         const bool given = out.defined();
         int64_t ld, ld_g = 0;
         const int dt = logits_code(z, ld);
@@ -623,6 +627,7 @@ PyObject* n_embed(PyObject*, PyObject* const* v, Py_ssize_t n) {
         const float scale = a.f32();
         const at::Tensor out = optional_tensor(a);
         a.done();
+        refuse_recorded(out);
         const at::Tensor rows = embed(table, tok, scale, out);
         if (out.defined()) written(out);
         return THPVariable_Wrap(rows);
@@ -638,6 +643,7 @@ PyObject* n_embed_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
         const int accumulate = a.i32();
         const at::Tensor out = optional_tensor(a);
         a.done();
+        refuse_recorded(out);
         const at::Tensor sums = embed_grad(g, tok, V, scale, accumulate, out);
         if (out.defined()) written(out);
         return THPVariable_Wrap(sums);
@@ -701,6 +707,7 @@ PyObject* n_clip_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
             dtypes.push_back(t.scalar_type() == at::kFloat ? PICOSPEC_F32 : PICOSPEC_BF16);
             if (outs == Py_None) continue;
             const at::Tensor& to = at_place(outs, i);
+            refuse_recorded(to);
             refuse_unless(to.layout() == at::kStrided && to.device() == t.device() && to.sizes() == t.sizes() && to.strides() == t.strides());
             if (to.scalar_type() != t.scalar_type()) throw Refused{PICOSPEC_EDTYPE};
             o.push_back(to.data_ptr());
