@@ -474,8 +474,8 @@ struct Adjustment {
     }
 };
 
-// A tensor that a call is to write must not be part of what the tape records: it does not learn of the call, and a gradient that is taken later would leave it out
-void refuse_recorded(const at::Tensor& out) { refuse_unless(!(out.defined() && out.requires_grad() && at::GradMode::is_enabled())); }
+// A tensor that a call is to write, or reads without a gradient for it, must not be part of what the tape records: a gradient that is taken later would leave the call out
+void refuse_recorded(const at::Tensor& t) { refuse_unless(!(t.defined() && t.requires_grad() && at::GradMode::is_enabled())); }
 
 // A tensor that a call has written in place: what the tape has saved of it is not what it was
 void written(const at::Tensor& t) { if (!t.is_inference()) torch::autograd::impl::bump_version(t); }
@@ -569,6 +569,7 @@ PyObject* n_adjust_on_tape(PyObject*, PyObject* const* v, Py_ssize_t n) {
         const int64_t V = a.i64();
         Adjustment by(a);
         a.done();
+        for (const at::Tensor* t : {&by.repetition.each, &by.presence.each, &by.frequency.each, &by.bias_value}) refuse_recorded(*t);      // (they would have no gradient)
         return THPVariable_Wrap(AdjustFunction::apply(z, &by, V));
     });
 }

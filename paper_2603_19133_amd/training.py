@@ -33,7 +33,7 @@ def embed(table: torch.Tensor, tok: torch.Tensor, scale: float = 1.0) -> torch.T
 def adjust(logits: torch.Tensor, V: int, hist: "_ps.History | None" = None, repetition=1.0, presence=0.0, frequency=0.0, bias: "_ps.Bias | None" = None,
            mask: torch.Tensor | None = None, mask_row: torch.Tensor | None = None, seq_off: torch.Tensor | None = None,
            draft_tok: torch.Tensor | None = None) -> torch.Tensor:
-    """binding.adjust, differentiable in the logits; rows that no sequence has are zeros and have a gradient of 0."""
+    """binding.adjust, differentiable in the logits (settings and biases may not require a gradient); rows that no sequence has are zeros and have a gradient of 0."""
     h = (hist.tok, hist.length, hist.prompt) if hist is not None else (None, None, None)
     b = (bias.off, bias.id, bias.value) if bias is not None else (None, None, None)
     r = _ps._nat.adjust_on_tape(logits, V, *h, repetition, presence, frequency, *b, mask, mask_row, seq_off, draft_tok)

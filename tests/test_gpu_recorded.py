@@ -43,3 +43,22 @@ def test_an_output_that_is_recorded(gpu, ps):
     y = (x * 1.0)
     ps.clip_grad([y], 1e-3)
     assert float(y.detach().norm()) <= 1.01e-3
+
+
+def test_settings_that_are_recorded(gpu, ps):
+    """training.adjust has a gradient for the logits alone."""
+    print("[case] recorded settings", flush=True)
+    from paper_2603_19133_amd import training
+    V = 50
+    z = torch.randn((3, V), device=gpu, requires_grad=True)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device=gpu)                                                       # noqa: E731
+    hist = ps.History(i32(1, 2, 3).view(3, 1), i32(1, 1, 1))
+    learnt = torch.full((3,), 1.5, device=gpu, requires_grad=True)
+    for kw in (dict(repetition=learnt), dict(presence=learnt), dict(frequency=learnt), dict(bias=ps.Bias(i32(0, 1, 2, 3), i32(4, 5, 6), learnt))):
+        _refuses(ps, lambda: training.adjust(z, V, hist, **kw))
+        with torch.no_grad():
+            want = training.adjust(z, V, hist, **kw)
+        for k, v in kw.items():
+            kw[k] = ps.Bias(v.off, v.id, v.value.detach()) if k == "bias" else v.detach()
+        out = training.adjust(z, V, hist, **kw)
+        assert out.requires_grad and torch.equal(out.detach(), want)
