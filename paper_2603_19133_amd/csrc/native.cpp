@@ -424,6 +424,7 @@ struct Adjustment {
         const int64_t rows = z.size(0);
         auto list = [&](const at::Tensor& t, at::ScalarType type, int64_t n) { refuse_unless(t.defined() && t.dim() == 1 && (n < 0 || t.numel() == n) && dense(t, type, z)); };
         refuse_unless(V >= 1 && V <= z.size(1) && rows <= INT32_MAX);
+        if (V > INT32_MAX) throw Refused{PICOSPEC_EUNSUPPORTED};                                    // (the library's sizes have 32 bits)
         B = rows;
         if (seq_off.defined()) {
             list(seq_off, at::kInt, -1);
