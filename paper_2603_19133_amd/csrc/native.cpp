@@ -66,6 +66,18 @@ struct Args {
     void done() const { if (at != n) throw BadArgument("too many arguments"); }
 };
 
+// f(), a call of the library, without the interpreter's lock where this thread has it: a call that waits for room in its stream's queue must not stop other Python threads
+// (the engine runs backward calls without it)
+template <class F>
+int in_library(F f) {
+    if (!PyGILState_Check()) return f();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f();
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
 // Runs `call(args)` - which converts its arguments and returns the C function with them bound - and returns its code.
 template <class F>
 PyObject* enter(PyObject* const* argv, Py_ssize_t n, F call) {
@@ -74,11 +86,7 @@ PyObject* enter(PyObject* const* argv, Py_ssize_t n, F call) {
         Args a{argv, n};
         auto bound = call(a);
         a.done();
-        int rc;
-        Py_BEGIN_ALLOW_THREADS
-        rc = bound();
-        Py_END_ALLOW_THREADS
-        return PyLong_FromLong(rc);
+        return PyLong_FromLong(in_library(bound));
     } catch (const BadArgument& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, e.what());
         return nullptr;
@@ -304,9 +312,10 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
         at::Tensor loss = at::empty({rows}, f32), accept = at::empty({rows}, f32), stats = at::empty({rows, 4}, z.options().dtype(at::kDouble));
         const size_t bytes = picospec_scratch_bytes(PICOSPEC_CALL_DISTILL, dt, (int32_t)rows, 0, (int32_t)V, 0);
         const at::Tensor scratch = bytes ? at::empty({(int64_t)bytes}, z.options().dtype(at::kByte)) : at::Tensor();
-        const int rc = picospec_distill(z.data_ptr(), dt, ld, (int32_t)rows, (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
+        void* const stream = c10::hip::getCurrentHIPStream().stream();
+        const int rc = in_library([&] { return picospec_distill(z.data_ptr(), dt, ld, (int32_t)rows, (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
                                         (int)tail, nullptr, loss.data_ptr<float>(), accept.data_ptr<float>(), stats.data_ptr<double>(), nullptr, 0,
-                                        bytes ? scratch.data_ptr() : nullptr, bytes, c10::hip::getCurrentHIPStream().stream());
+                                        bytes ? scratch.data_ptr() : nullptr, bytes, stream); });
         if (rc != PICOSPEC_OK) throw Refused{rc};
         ctx->save_for_backward({z, idx, prob, count, stats});
         ctx->saved_data["k"] = k;
@@ -335,8 +344,9 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
         if (weight.numel() != z.size(0) || !dense(weight, at::kFloat, z)) throw Refused{PICOSPEC_EINVAL};
         at::Tensor grad = at::empty(z.sizes(), z.options());
         if (z.size(1) > V) grad.slice(1, V).zero_();                                                // (columns behind the vocabulary are not read)
-        const int rc = picospec_distill_grad(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
-                                             (int)tail, weight.data_ptr<float>(), stats.data_ptr<double>(), grad.data_ptr(), z.size(1), c10::hip::getCurrentHIPStream().stream());
+        void* const stream = c10::hip::getCurrentHIPStream().stream();
+        const int rc = in_library([&] { return picospec_distill_grad(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (float)T, idx.data_ptr<int32_t>(), prob.data_ptr<float>(), count.data_ptr<int32_t>(), (int32_t)k,
+                                             (int)tail, weight.data_ptr<float>(), stats.data_ptr<double>(), grad.data_ptr(), z.size(1), stream); });
         TORCH_CHECK(rc == PICOSPEC_OK, "picospec error ", rc, ": ", picospec_strerror(rc));
         out[0] = grad;
         return out;
@@ -463,15 +473,17 @@ struct Adjustment {
     }
     // whole: `out` is new, and rows that no sequence has are zeros in it
     int forward(const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out, bool whole) const {
-        return (whole ? picospec_adjust_whole : picospec_adjust)(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
+        void* const stream = getCurrentHIPStream().stream();
+        return in_library([&] { return (whole ? picospec_adjust_whole : picospec_adjust)(z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
                                data<int32_t>(hist_tok), ld_hist, (int32_t)hist_cap, data<int32_t>(length), data<int32_t>(prompt), repetition.all, presence.all, frequency.all,
                                data<float>(repetition.each), data<float>(presence.each), data<float>(frequency.each), data<int32_t>(bias_off), data<int32_t>(bias_id), data<float>(bias_value), (int32_t)n_bias,
-                               data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, getCurrentHIPStream().stream());
+                               data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, stream); });
     }
     int backward(const at::Tensor& g, int64_t ld_g, const at::Tensor& z, int dt, int64_t ld, int64_t V, at::Tensor& out, int64_t ld_out, bool whole) const {
-        return (whole ? picospec_adjust_grad_whole : picospec_adjust_grad)(g.data_ptr(), ld_g, z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
+        void* const stream = getCurrentHIPStream().stream();
+        return in_library([&] { return (whole ? picospec_adjust_grad_whole : picospec_adjust_grad)(g.data_ptr(), ld_g, z.data_ptr(), dt, ld, (int32_t)z.size(0), (int32_t)V, (int32_t)B, (int32_t)n_draft, data<int32_t>(seq_off), data<int32_t>(draft_tok),
                                     data<int32_t>(hist_tok), ld_hist, (int32_t)hist_cap, data<int32_t>(length), repetition.all, data<float>(repetition.each),
-                                    data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, getCurrentHIPStream().stream());
+                                    data<uint32_t>(mask), ld_mask, (int32_t)n_masks, data<int32_t>(mask_row), out.data_ptr(), ld_out, stream); });
     }
 };
 
@@ -597,7 +609,8 @@ at::Tensor embed(const at::Tensor& table, const at::Tensor& tok, float scale, at
         sizes.push_back(t.d);
         out = at::empty(sizes, table.options());
     }
-    check_code(picospec_embed(table.data_ptr(), t.dt, t.ld, (int32_t)t.V, (int32_t)t.d, data<int32_t>(tok), (int32_t)n, scale, out.data_ptr(), ld_out, getCurrentHIPStream().stream()));
+    void* const stream = getCurrentHIPStream().stream();
+    check_code(in_library([&] { return picospec_embed(table.data_ptr(), t.dt, t.ld, (int32_t)t.V, (int32_t)t.d, data<int32_t>(tok), (int32_t)n, scale, out.data_ptr(), ld_out, stream); }));
     return out;
 }
 
@@ -617,8 +630,9 @@ at::Tensor embed_grad(at::Tensor g, const at::Tensor& tok, int64_t V, float scal
     const Table t = check_table(out);
     const size_t bytes = picospec_workspace_bytes(PICOSPEC_CALL_EMBED_GRAD, dt, (int32_t)n, (int32_t)V, (int32_t)d);
     const at::Tensor scratch = at::empty({(int64_t)std::max<size_t>(bytes, 16)}, g.options().dtype(at::kByte));
-    check_code(picospec_embed_grad(g.data_ptr(), dt, ld, (int32_t)n, data<int32_t>(tok), (int32_t)V, (int32_t)d, scale, accumulate, out.data_ptr(), t.dt, t.ld,
-                                   scratch.data_ptr(), (size_t)scratch.nbytes(), getCurrentHIPStream().stream()));
+    void* const stream = getCurrentHIPStream().stream();
+    check_code(in_library([&] { return picospec_embed_grad(g.data_ptr(), dt, ld, (int32_t)n, data<int32_t>(tok), (int32_t)V, (int32_t)d, scale, accumulate, out.data_ptr(), t.dt, t.ld,
+                                   scratch.data_ptr(), (size_t)scratch.nbytes(), stream); }));
     return out;
 }
 
@@ -681,15 +695,23 @@ PyObject* n_embed_on_tape(PyObject*, PyObject* const* v, Py_ssize_t n) {
 // clip_grad(grads, max_norm, out) -> norm [1] or an error code; lists or tuples of tensors, out None: in place
 PyObject* n_clip_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return answer(v, n, [](Args& a) {
-        PyObject* const grads = a.next();
+        PyObject* const given = a.next();
         const float max_norm = a.f32();
-        PyObject* const outs = a.next();
+        PyObject* const given_outs = a.next();
         a.done();
-        auto sequence = [](PyObject* o) { if (!PyList_Check(o) && !PyTuple_Check(o)) throw BadArgument("a list or tuple of tensors is expected"); return PySequence_Fast_GET_SIZE(o); };
-        const Py_ssize_t count = sequence(grads);
-        refuse_unless(count <= INT32_MAX && (outs == Py_None || sequence(outs) == count));
-        auto at_place = [](PyObject* o, Py_ssize_t i) -> const at::Tensor& {
-            PyObject* t = PySequence_Fast_GET_ITEM(o, i);
+        // (as tuples: a list may be another one after the call, which gives the interpreter's lock up)
+        auto sequence = [](PyObject* o) {
+            if (!PyList_Check(o) && !PyTuple_Check(o)) throw BadArgument("a list or tuple of tensors is expected");
+            PyObject* const t = PySequence_Tuple(o);
+            if (!t) throw BadArgument("");
+            return t;
+        };
+        const THPObjectPtr grads(sequence(given)), outputs(given_outs == Py_None ? nullptr : sequence(given_outs));
+        const bool apart = outputs.get() != nullptr;
+        const Py_ssize_t count = PyTuple_GET_SIZE(grads.get());
+        refuse_unless(count <= INT32_MAX && (!apart || PyTuple_GET_SIZE(outputs.get()) == count));
+        auto at_place = [](const THPObjectPtr& o, Py_ssize_t i) -> const at::Tensor& {
+            PyObject* t = PyTuple_GET_ITEM(o.get(), i);
             if (!THPVariable_Check(t)) throw BadArgument("a list or tuple of tensors is expected");
             return THPVariable_Unpack(t);
         };
@@ -707,8 +729,8 @@ PyObject* n_clip_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
             g.push_back(t.data_ptr());
             numel.push_back(t.numel());
             dtypes.push_back(t.scalar_type() == at::kFloat ? PICOSPEC_F32 : PICOSPEC_BF16);
-            if (outs == Py_None) continue;
-            const at::Tensor& to = at_place(outs, i);
+            if (!apart) continue;
+            const at::Tensor& to = at_place(outputs, i);
             refuse_recorded(to);
             refuse_unless(to.layout() == at::kStrided && to.device() == t.device() && to.sizes() == t.sizes() && to.strides() == t.strides());
             if (to.scalar_type() != t.scalar_type()) throw Refused{PICOSPEC_EDTYPE};
@@ -719,9 +741,10 @@ PyObject* n_clip_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
         at::Tensor norm = at::empty({1}, f32);
         const size_t bytes = picospec_workspace_bytes(PICOSPEC_CALL_CLIP_GRAD, 0, (int32_t)count, 1, 0);
         const at::Tensor scratch = at::empty({(int64_t)std::max<size_t>(bytes, 16)}, f32.dtype(at::kByte));
-        check_code(picospec_clip_grad((int32_t)count, g.data(), outs == Py_None ? nullptr : o.data(), numel.data(), dtypes.data(), max_norm, norm.data_ptr<float>(),
-                                      scratch.data_ptr(), (size_t)scratch.nbytes(), getCurrentHIPStream().stream()));
-        for (Py_ssize_t i = 0; i < count && (outs != Py_None || !std::isinf(max_norm)); ++i) written(at_place(outs == Py_None ? grads : outs, i));
+        void* const stream = getCurrentHIPStream().stream();
+        check_code(in_library([&] { return picospec_clip_grad((int32_t)count, g.data(), apart ? o.data() : nullptr, numel.data(), dtypes.data(), max_norm, norm.data_ptr<float>(),
+                                      scratch.data_ptr(), (size_t)scratch.nbytes(), stream); }));
+        for (Py_ssize_t i = 0; i < count && (apart || !std::isinf(max_norm)); ++i) written(at_place(apart ? outputs : grads, i));
         return THPVariable_Wrap(norm);
     });
 }
