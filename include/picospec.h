@@ -29,7 +29,7 @@
  *
  * Conventions shared by all calls
  *   - Every data pointer is a DEVICE pointer (HBM) unless marked "host".  The caller owns all
- *     buffers; the library neither allocates nor frees nor synchronises.  Work is enqueued on
+ *     buffers; the library neither allocates (but for picospec_clip_grad's list, see there) nor frees nor synchronises.  Work is enqueued on
  *     `stream` (a hipStream_t passed as void*, NULL = the default stream) of the current device
  *     and the call returns at once; outputs are valid once the stream reaches that point.
  *   - Logits are row-major [rows, ld] with ld >= V elements between row starts, dtype
@@ -87,7 +87,7 @@ enum {
     PICOSPEC_EWORKSPACE = -2,  /* a workspace was given that is smaller than picospec_workspace_bytes() says, or misaligned */
     PICOSPEC_EDTYPE = -3,      /* dtype is neither PICOSPEC_F32 nor PICOSPEC_BF16 */
     PICOSPEC_EHIP = -4,        /* a HIP runtime call (launch, attribute) failed */
-    PICOSPEC_EUNSUPPORTED = -5,/* k or V beyond the limits reported by picospec_limit(), or a call larger than a launch can be */
+    PICOSPEC_EUNSUPPORTED = -5,/* k or V beyond the limits reported by picospec_limit(), or a call larger than a launch can be or the host has memory for */
     PICOSPEC_ESCRATCH = -6     /* picospec_verify_sample_static: the rows' segment table exceeds the library's fixed array */
 };
 
@@ -580,7 +580,8 @@ int picospec_embed_grad(const void* grad, int dtype, int64_t ld, int32_t n, cons
  *   norm                                 device, fp32 [1]                                                                             out
  *   workspace: picospec_workspace_bytes(PICOSPEC_CALL_CLIP_GRAD, 0, n_tensors, 1, 0) bytes on a 16-byte boundary, whatever they hold; needed.  Calls that overlap in time must not
  *              share it
- * The host arrays are read before the call returns: a captured call replays on the tensors that it was captured with.
+ * The host arrays are read before the call returns: a captured call replays on the tensors that it was captured with.  Of more than 128 tensors the call keeps a list in host memory
+ * (32 bytes each) until it returns, to see whether any two overlap; no memory for it is PICOSPEC_EUNSUPPORTED.
  */
 int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtypes,
                        float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);

@@ -781,7 +781,7 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
     if (n_tensors > 0 && (!grads || !numel || !dtypes)) return PICOSPEC_EINVAL;
     constexpr size_t kHere = 256;
     Piece here[kHere], *pieces = here;
-    if ((size_t)n_tensors * 2 > kHere && !(pieces = static_cast<Piece*>(std::malloc((size_t)n_tensors * 2 * sizeof(Piece))))) return PICOSPEC_EINVAL;
+    if ((size_t)n_tensors * 2 > kHere && !(pieces = static_cast<Piece*>(std::malloc((size_t)n_tensors * 2 * sizeof(Piece))))) return PICOSPEC_EUNSUPPORTED;
     size_t n_pieces = 0;
     int64_t elements = 0, bytes = 0;
     bool in_place = true;
@@ -959,7 +959,7 @@ const char* picospec_strerror(int code)
         case PICOSPEC_EWORKSPACE: return "workspace smaller than picospec_workspace_bytes() or not on a 16-byte boundary";
         case PICOSPEC_EDTYPE: return "dtype must be PICOSPEC_F32 or PICOSPEC_BF16";
         case PICOSPEC_EHIP: return "HIP runtime call failed";
-        case PICOSPEC_EUNSUPPORTED: return "k or V exceeds picospec_limit(), or a call is larger than a launch can be";
+        case PICOSPEC_EUNSUPPORTED: return "k or V exceeds picospec_limit(), or a call is larger than a launch can be or the host has memory for";
         case PICOSPEC_ESCRATCH: return "the target rows' segment table exceeds the fixed array of picospec_verify_sample_static (picospec_static_scratch_bytes())";
         default: return "unknown picospec error code";
     }
