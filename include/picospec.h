@@ -496,7 +496,7 @@ int picospec_distill_grad(const void* logits, int dtype, int64_t ld, int32_t n_r
  *   z <- z - frequency c - presence                (tokens with c > 0)
  *   z <- z + bias                                  (tokens of the sequence's list)
  *   z <- -inf                                      (tokens that the row's mask does not allow)
- * formed in 64 bits and rounded to the rows' type; tokens that none of it touches keep their bits, NaN among them.  seq_off ascends; rows that no sequence has, because it begins above 0 or ends
+ * formed in 64 bits and rounded to fp32, bf16 rows from there; tokens that none of it touches keep their bits, NaN among them.  seq_off ascends; rows that no sequence has, because it begins above 0 or ends
  * before n_draft (a batch that is padded), are left as they are.
  *   logits [n_rows, ld], out [n_rows, ld_out]: out may be the logits themselves (same pointer and stride; what does not change is not written then), else may not overlap them
  *   draft_tok [n_draft]                                                                                      in
@@ -550,16 +550,16 @@ int picospec_adjust_grad_whole(const void* grad, int64_t ld_grad, const void* lo
                                void* out, int64_t ld_out, void* stream);
 
 /*
- * Token embeddings, what a drafter reads its tokens by: out[i] = scale * table[tok[i]], rounded once (scale 1: the rows' bits); zeros where tok[i] is outside
- * [0, V), as padding is.
+ * Token embeddings, what a drafter reads its tokens by: out[i] = scale * table[tok[i]], an fp32 product, rounded to bf16 from there in bf16 tables (scale 1: the rows' bits); zeros where tok[i] is
+ * outside [0, V), as padding is.
  *   table [V, ld], tok [n] in; out [n, ld_out] in the table's type, may not overlap the table; ld, ld_out >= d; V up to picospec_limit(MAX_V)
  */
 int picospec_embed(const void* table, int dtype, int64_t ld, int32_t V, int32_t d, const int32_t* tok, int32_t n, float scale,
                    void* out, int64_t ld_out, void* stream);
 
 /*
- * Its gradient: table_grad[v] = scale * sum of grad[i] over tok[i] = v, summed in fp32 in an order that tok decides (a call gives the same bits every
- * time) and rounded once; positions whose token is outside [0, V) go nowhere.
+ * Its gradient: table_grad[v] = scale * sum of grad[i] over tok[i] = v, summed and scaled in fp32, in an order that tok decides (a call gives the same bits every
+ * time), and rounded to the table's type from there; positions whose token is outside [0, V) go nowhere.
  *   grad [n, ld] of dtype, tok [n] in, n up to 2^26
  *   accumulate 0: every row of table_grad is written, zeros where a token does not occur; 1: the sums are added to what is there (in fp32, then rounded), other rows stay
  *   table_grad [V, ld_table] of dtype_table, may not overlap grad                                    out
@@ -572,7 +572,7 @@ int picospec_embed_grad(const void* grad, int dtype, int64_t ld, int32_t n, cons
 /*
  * The norm over all gradients of a model, and the gradients scaled to at most max_norm:
  *   norm = sqrt(sum of g^2 over all tensors),  out = g * min(1, max_norm / (norm + 1e-6))
- * Squares are summed in 64 bits in an order that the sizes decide; the factor and the products are formed in 64 bits, too, and rounded to the tensor's type.  With a norm of inf the factor is 0, with NaN NaN.
+ * Squares are summed in 64 bits in an order that the sizes decide; the factor and the products are formed in 64 bits, too, and rounded to fp32, bf16 tensors from there.  With a norm of inf the factor is 0, with NaN NaN.
  *   grads, numel, dtypes [n_tensors]     HOST arrays: device pointers to dense tensors of numel[i] elements, in any order of their elements; empty ones are passed over
  *   out [n_tensors]                      HOST array of device pointers, or NULL: in place, where nothing is read again or written if the factor is 1.  out[i] may be grads[i];
  *                                        otherwise no two of the tensors and outputs may share a byte

@@ -6,8 +6,8 @@
 //   d out / d z = allowed ? (seen ? (z > 0 ? 1 / repetition : repetition) : 1) : 0
 // A workgroup has one sequence and one chunk of the vocabulary.  It counts the history's tokens of its chunk in LDS once, then takes the sequence's rows one by one; a thread has the same ids
 // in every row and keeps a bit for each that is touched.
-// What bounds it: the rows, read once and written once (2432 rows of 151,936 bf16, 1.48 GB: 293 us with nothing to adjust,
-// 5.0 TB/s, where a copy on this card gets 4.9; 310 with histories of up to 16,384 tokens and masks).
+// What bounds it: the rows, read once and written once (2432 rows of 151,936 bf16, 1.48 GB: 272 us with nothing to adjust,
+// 5.4 TB/s, where a copy on this card gets 4.9; 290 with histories of up to 16,384 tokens and masks).
 #include "kernels.hpp"
 #include "vectors.hpp"
 
@@ -336,7 +336,9 @@ AdjustPlan adjust_plan(const AdjustArgs& a, int dtype, int B, int64_t n_rows, bo
     }
     p.chunks = chunks(p.T * p.vectors * N);
     // A sequence's rows shared out, each share counting the history again: where there are fewer than kAdjustGroups workgroups of 256 threads (us, one share / two / four: 8 sequences of 9 rows of 128,256 fp32
-    // 14.2 / 12.5 / 14.2, gradients of 32 sequences of 9.5 rows of 32,000 fp32 27 / 20.5 / 20.4), and where rows are so many that the sequences' ends are far apart (256 of 9.5 rows of 151,936 bf16 309 / 300 / 323;
+    // 14.2 / 12.5 / 14.2, gradients of 32 sequences of 9.5 rows of 32,000 fp32 27 / 20.5 / 20.4).  Two shares of what one makes 1000 to 1800 workgroups of are more than run at once, and take less all the
+    // same, mostly (one / two: 1000 workgroups, 40 sequences of 5.5 rows of 50,001 bf16, 23.8 / 22.7; 1600, 64 of them, 28.2 / 27.8; 1470, 30 of 9.5 rows of 50,001 fp32, 28.8 / 25.8; but 1280, 40 of 5.5 rows
+    // of 32,000 fp32, 16.3 / 17.5).  And where rows are so many that the sequences' ends are far apart (256 of 9.5 rows of 151,936 bf16 309 / 300 / 323;
     // of 5 rows of 75,000 fp32 177 / 182 / 208)
     const int64_t groups = (int64_t)B * p.chunks;
     p.parts = (int)std::min<int64_t>(mean, std::max<int64_t>((kAdjustGroups * 256 / p.T + groups - 1) / groups, mean >= 8 ? 2 : 1));

@@ -813,7 +813,8 @@ int picospec_clip_grad(int32_t n_tensors, const void* const* grads, void* const*
         c.block = clip_block(elements);
         c.in_place = in_place;
         auto go = [&] {
-            // (the second pass begins where the first one ends)
+            // (A launch's second pass goes backwards: where one launch holds all tensors it begins with what the first pass has left in the caches.  Several are taken in the same order in both passes, and blocks
+            // are sized for one: 290 tensors of 0.44 billion bf16, in three launches, are clipped in 525 us where a copy's rate makes it 353, 448 of 65,536 fp32, in four, in 103 where it makes it 48)
             const int64_t kept = bytes > 0 ? (int64_t)((double)kClipCached / (double)bytes * (double)elements) / c.block : 0;
             c.stream = (uint32_t)std::max<int64_t>(blocks - kept, 0);
             const hipError_t e = f(c, (int)std::min<int64_t>(blocks, kClipGroups));

@@ -391,8 +391,10 @@ __global__ __launch_bounds__(kRowThreads) void embed_sum_kernel(const EmbedGradA
     }
 }
 
-// Few positions, in one launch: every workgroup looks its tokens' positions up itself.  777 positions, 50,001 x 501 fp32: 22 us, zeros alone 21; sorted and
-// summed in launches of their own 46.
+// Few positions, in one launch: every workgroup looks its tokens' positions up itself.  777 positions, 50,001 x 501 fp32: 23 us, zeros alone 21; sorted and
+// summed in launches of their own 46.  1024 positions of a Zipf law so / 1025 of it sorted, written and added: 32,000 x 200 fp32 12.5 / 26.4 and 9.7 / 26, 32,000 x 1024 fp32 39.5 / 42.4 and 13.3 / 26.4,
+// 128,256 x 4096 bf16 195.5 / 197.2 and 30.7 / 35.  The other side: half of the 1024 positions one token's, whose rows are added up in one workgroup here: 46.4 / 27.4 and 40.1 / 27.2, 117 / 43.3
+// and 95.8 / 27.2, 342 / 198 and 183 / 34.8.  How tokens spread is not known in front of the launch.
 template <bool BF16, bool OUT16>
 __global__ __launch_bounds__(kRowThreads) void embed_few_kernel(const EmbedGradArgs a, const int32_t* tok, int n, int groups_log2)
 {
